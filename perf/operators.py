@@ -221,12 +221,13 @@ def _rounded(x):
     """Codes [..., dh / 32, 16] (two to a byte), biased exponents [..., dh / 32] and the values they stand for, of x [..., dh].
 
     A block's power of two is the one that brings its largest magnitude into [3.5, 7): the largest code, 6, is then off
-    by no more than half a step of the next power of two's codes.  Codes round to nearest, ties to the even code.
+    by no more than half a step of the next power of two's codes.  (Between 2^-125 and 2^125, so that every value is a normal
+    number of bf16 and fp32.)  Codes round to nearest, ties to the even code.
     """
     x = x.float()
     b = x.reshape(x.shape[:-1] + (x.shape[-1] // 32, 32))
     top = b.abs().amax(-1)
-    e = (((top.view(torch.int32) + 0x200000) >> 23) - 2).clamp(min=1)
+    e = (((top.view(torch.int32) + 0x200000) >> 23) - 2).clamp(min=2, max=252)
     bad = ~torch.isfinite(b).all(-1)
     e = torch.where(bad, 127, e)
     y = b * ((254 - e) << 23).view(torch.float32)[..., None]
@@ -391,7 +392,7 @@ def _exact_values(x):
     b = x.double().reshape(-1, 32)
     frac, power = torch.frexp(b.abs().amax(1))
     e = torch.where(frac >= 0.875, power, power - 1) - 2
-    one = torch.ldexp(torch.ones_like(frac), e.clamp(min=-126))[:, None]
+    one = torch.ldexp(torch.ones_like(frac), e.clamp(min=-125, max=125))[:, None]
     even, odd = (torch.tensor(STEPS[i::2], dtype=torch.float64, device=x.device) for i in (0, 1))
     a = b.abs() / one
     de, do = ((a[..., None] - g).abs() for g in (even, odd))
