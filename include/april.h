@@ -270,6 +270,110 @@ int april_sample_rows_logprobs(april_ctx* ctx, const float* logits, int32_t n_ro
 int april_sample_rows_noalloc(april_ctx* ctx, const float* logits, int32_t n_rows,
                               const int64_t* request_ids, const int32_t* gen_index, int32_t* out_tokens);
 
+/* ------------------------------------------------------------------------------------------
+ * Operators of a 4-bit KV cache on the caller's own device memory: the tables that say where a
+ * token lies, the store, and the attention that reads it.  They need no context: each enqueues
+ * its kernels on `stream` (NULL: the null stream) of the current device and returns; nothing is
+ * allocated or synchronised, so the calls may be captured into a graph.  Pointers are device
+ * memory of that device.  Errors found on the host leave everything untouched, their message is
+ * april_last_error(NULL) of the calling thread; errors in device data end in `status` or in NaN, as
+ * said below, never in an access outside the given arrays.
+ *
+ * The pool: pages of 16 tokens of one sequence, n_pages x n_kv_heads blocks of 17 * head_dim bytes
+ * (april_cache_block_bytes; head_dim 32, 64 or 128; 16-byte aligned).  Keys and values are kept in
+ * blocks of 32 dimensions, MXFP4: 4-bit codes (sign; 0, 0.5, 1, 1.5, 2, 3, 4, 6) times a power of two
+ * that the block shares.  In a page's block of one head:
+ *   keys    [head_dim / 32][16 tokens][16 bytes]   dimension 2 i in the low half of byte i, 2 i + 1 in the high one
+ *   values  the same
+ *   scales  [head_dim / 32][16 tokens][key, value] the power's biased exponent, 2^(e - 127); 255: 32 NaN
+ * The power brings the block's largest magnitude into [3.5, 7) (between 2^-125 and 2^125, so that every value is
+ * a normal number; what lies beyond 6 * 2^125 becomes that), codes are rounded to nearest, ties to even; a block
+ * that holds an infinity or a NaN is stored as NaN.  Uninitialised pages are fine: nothing
+ * is read behind a sequence's length.
+ * The block table: row b holds the pages of sequence b, token p in page p / 16 of the row. */
+#define APRIL_CACHE_PAGE 16
+
+/* Bytes of one (page, KV head) of the pool, 17 * head_dim; APRIL_EINVAL for another head_dim. */
+int april_cache_block_bytes(int32_t head_dim);
+
+/* One iteration's tables from the requests' lengths.  Sequence b holds lens[b] tokens.  new_lens[b] < 0:
+ * it has ended, its pages go onto the stack of free pages (in the order of sequences and of their pages).
+ * Then the others grow by new_lens[b] >= 0 tokens; in the order of sequences each takes the pages that it
+ * lacks from the top of the stack and has them entered in its row of the block table.
+ * lens_out, free_top_out and status may be the arrays of the next call's lens and free_top. */
+typedef struct {
+  int32_t n_seqs;                /* sequences, 1..65536                                        */
+  int32_t max_pages;             /* columns of the block table                                 */
+  int32_t n_pages;               /* pages of the pool = entries of free_pages                  */
+  int32_t n_rows;                /* entries of slot_map and positions                          */
+  int64_t table_stride;          /* elements between rows of the block table                   */
+  const int32_t* lens;           /* [n_seqs]                                                   */
+  const int32_t* new_lens;       /* [n_seqs]                                                   */
+  const int32_t* free_top;       /* [1] free pages on the stack                                */
+  int32_t* block_table;          /* [n_seqs][max_pages], in place                              */
+  int32_t* free_pages;           /* [n_pages] the stack, in place                              */
+  int32_t* lens_out;             /* [n_seqs] (may be lens); 0 for a sequence that has ended    */
+  int32_t* free_top_out;         /* [1] (may be free_top)                                      */
+  int32_t* q_start;              /* [n_seqs + 1] first row of each sequence's new tokens       */
+  int64_t* slot_map;             /* [n_rows] page * 16 + token of each row; -1 behind the last */
+  int32_t* positions;            /* [n_rows] position in its sequence; -1 behind the last      */
+  int32_t* status;               /* [1] 0; 1: too few free pages; 2: a length below zero or beyond the
+                                    block table, more rows than n_rows, or a stack that does not fit its
+                                    array.  Not 0: nothing was entered or taken, lens_out = lens,
+                                    free_top_out = free_top, no rows (q_start 0, slots and positions -1) */
+  void* stream;
+} april_cache_extend_args;
+int april_cache_extend(const april_cache_extend_args* args);
+
+/* Store the keys and values of n_rows tokens at their slots (page * 16 + token, as april_cache_extend writes
+ * them).  Rows whose slot lies outside the pool are left out; two rows with the same slot leave one of them,
+ * or parts of both. */
+typedef struct {
+  int32_t n_pages, n_kv_heads, head_dim, n_rows;
+  int32_t dtype;                 /* APRIL_DTYPE_* of k, v and the values                       */
+  int32_t reserved;              /* 0                                                          */
+  int64_t k_row, k_head, v_row, v_head;   /* elements between rows and heads; dimensions are adjacent.
+                                    Rows of 16-byte aligned heads are read fastest             */
+  const void *k, *v;             /* [n_rows][n_kv_heads][head_dim]                             */
+  void *k_values, *v_values;     /* or NULL: contiguous, what the cache now stands for (rows that are left out: untouched) */
+  const int64_t* slot_map;       /* [n_rows]                                                   */
+  void* pool;
+  void* stream;
+} april_cache_append_args;
+int april_cache_append(const april_cache_append_args* args);
+
+/* Causal attention over the cache, softmax(scale q k) v, bf16, sums in fp32.  The rows
+ * q_start[b] .. q_start[b + 1] - 1 of q are the last tokens of sequence b: row i of c sees the tokens
+ * 0 .. lens[b] - c + i.  (One row: a decode iteration.  As many rows as tokens: a whole prompt.)
+ * n_q_heads / n_kv_heads (at most 16) consecutive query heads share a KV head.
+ * A row that sees no token is 0 and its lse -infinity.  Rows of no sequence are left as they were.  A NaN in the
+ * cache reaches the rows that see it; a page id outside the pool that a sequence's length covers makes its rows NaN,
+ * and so does a length outside 0 .. max_len (or beyond the block table). */
+typedef struct {
+  int32_t n_q_heads, n_kv_heads, head_dim;
+  int32_t n_pages, n_seqs;
+  int32_t max_pages;             /* columns of the block table                                 */
+  int32_t n_rows;                /* rows of q, out and lse                                     */
+  int32_t max_q;                 /* bound on the rows of a sequence (rows beyond it are left as they were) */
+  int32_t max_len;               /* bound on lens.  Both decide how the work is split: tight bounds are faster */
+  float scale;                   /* > 0; 0: 1 / sqrt(head_dim)                                 */
+  int64_t table_stride, q_row, q_head, out_row, out_head;   /* in elements; dimensions are adjacent */
+  const void* q;                 /* bf16 [n_rows][n_q_heads][head_dim], heads 16-byte aligned  */
+  const void* pool;
+  const int32_t* block_table;    /* [n_seqs][max_pages]                                        */
+  const int32_t* lens;           /* [n_seqs] tokens in the cache, those of the rows included   */
+  const int32_t* q_start;        /* [n_seqs + 1], or NULL: row b is sequence b's (n_rows >= n_seqs) */
+  void* out;                     /* bf16, as q (8-byte aligned heads)                          */
+  float* lse;                    /* [n_rows][n_q_heads] log of the sum of exp(scale q k), or NULL */
+  void* workspace;               /* april_cache_attention_workspace bytes, 16-byte aligned; NULL if 0.  Calls that may
+                                    run at the same time need one each                         */
+  int64_t workspace_bytes;
+  void* stream;
+} april_cache_attention_args;
+int april_cache_attention(const april_cache_attention_args* args);
+/* Bytes that a call of these sizes needs (pointers, strides and the stream are not looked at). */
+int64_t april_cache_attention_workspace(const april_cache_attention_args* args);
+
 /* Per-kernel-class timing, measured with HIP events on the context's stream around
  * sampled launches of the real decode loop (every `every`-th iteration; 0 = off).  Two extra
  * classes calibrate the method: "event_pair_no_kernel" is what a pair of event records reads

@@ -8,7 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass, field
-from typing import Dict, List, Optional, Sequence
+from typing import Dict, List, NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -26,7 +26,9 @@ EXPORTS = [
     "april_buffer_import", "april_buffer_drop_kv", "april_buffer_free", "april_update_weights", "april_memory_pause", "april_memory_resume", "april_debug_watch",
     "april_debug_logits", "april_sample_rows", "april_sample_rows_logprobs", "april_sample_rows_noalloc", "april_profile_enable", "april_profile_get",
     "april_profile_reset", "april_get_info", "april_last_error", "april_destroy",
+    "april_cache_block_bytes", "april_cache_extend", "april_cache_append", "april_cache_attention", "april_cache_attention_workspace",
 ]
+APRIL_CACHE_PAGE = 16
 
 
 class AprilError(RuntimeError):
@@ -90,6 +92,26 @@ class april_info(C.Structure):
                                          "kv_bytes_per_token", "expert_bytes")]
 
 
+class april_cache_extend_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seqs", "max_pages", "n_pages", "n_rows")] + [("table_stride", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("lens", "new_lens", "free_top", "block_table", "free_pages", "lens_out", "free_top_out", "q_start",
+                                  "slot_map", "positions", "status", "stream")]
+
+
+class april_cache_append_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_pages", "n_kv_heads", "head_dim", "n_rows", "dtype", "reserved")] + [
+        (n, C.c_int64) for n in ("k_row", "k_head", "v_row", "v_head")] + [
+        (n, C.c_void_p) for n in ("k", "v", "k_values", "v_values", "slot_map", "pool", "stream")]
+
+
+class april_cache_attention_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "n_pages", "n_seqs", "max_pages", "n_rows", "max_q",
+                                         "max_len")] + [("scale", C.c_float)] + [
+        (n, C.c_int64) for n in ("table_stride", "q_row", "q_head", "out_row", "out_head")] + [
+        (n, C.c_void_p) for n in ("q", "pool", "block_table", "lens", "q_start", "out", "lse", "workspace")] + [
+        ("workspace_bytes", C.c_int64), ("stream", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -130,9 +152,15 @@ def load_library():
     lib.april_last_error.restype = C.c_char_p
     lib.april_destroy.argtypes = [vp]
     lib.april_destroy.restype = None
+    lib.april_cache_block_bytes.argtypes = [C.c_int32]
+    lib.april_cache_extend.argtypes = [C.POINTER(april_cache_extend_args)]
+    lib.april_cache_append.argtypes = [C.POINTER(april_cache_append_args)]
+    lib.april_cache_attention.argtypes = [C.POINTER(april_cache_attention_args)]
+    lib.april_cache_attention_workspace.argtypes = [C.POINTER(april_cache_attention_args)]
     for name in EXPORTS:
         if name not in ("april_buffer_free", "april_destroy", "april_last_error"):
             getattr(lib, name).restype = C.c_int
+    lib.april_cache_attention_workspace.restype = C.c_int64
     _lib = lib
     return lib
 
@@ -370,6 +398,163 @@ def april_get_info(ctx) -> dict:
     info = april_info()
     _check(ctx, load_library().april_get_info(ctx, C.byref(info)))
     return {n: int(getattr(info, n)) for n, _ in april_info._fields_}
+
+
+# ---------------------------------------------------------------------------
+# Operators of the 4-bit KV cache, on torch tensors of one GPU (any object with their data_ptr, stride, shape, dtype and
+# device would do).  They are enqueued on torch's current stream of the tensors' device and return at once; what they
+# allocate (results that were not handed in, attention's workspace) comes from torch on that stream, so they may be
+# captured into a graph.
+# ---------------------------------------------------------------------------
+class CacheTables(NamedTuple):
+    """What april_cache_extend leaves, see april.h: all int32 but slot_map (int64)."""
+    lens: object
+    free_top: object
+    q_start: object
+    slot_map: object
+    positions: object
+    status: object
+
+
+def _refuse(text, *args):
+    raise AprilError(APRIL_EINVAL, text % args if args else text)
+
+
+def _want(name, t, dtype, shape, device, strided=False):
+    """t's data pointer, or a refusal: another type, shape (None: any) or device, or not contiguous where it has to be."""
+    if str(t.dtype) != dtype:
+        _refuse("%s: %s wanted, not %s", name, dtype, t.dtype)
+    if len(t.shape) != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
+        _refuse("%s: shape %s wanted, not %s", name, shape, tuple(t.shape))
+    if t.device != device:
+        _refuse("%s is on %s, not on %s", name, t.device, device)
+    if not strided and not t.is_contiguous():
+        _refuse("%s has to be contiguous", name)
+    return t.data_ptr()
+
+
+def _table(t, device):
+    """(pointer, rows, columns, stride) of a block table; its rows may lie apart."""
+    p = _want("block_table", t, "torch.int32", (None, None), device, True)
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        _refuse("block_table: the pages of a sequence have to be adjacent")
+    return p, rows, cols, max(t.stride(0), cols) if rows == 1 else t.stride(0)
+
+
+def _pool(pool):
+    if pool.device.type != "cuda":
+        _refuse("the pool is on %s, not on a GPU", pool.device)
+    p = _want("pool", pool, "torch.uint8", (None, None, None), pool.device)
+    if pool.shape[2] not in (544, 1088, 2176):
+        _refuse("pool: blocks of %d bytes, not 17 * head_dim for a head_dim of 32, 64 or 128", pool.shape[2])
+    return p, pool.shape[0], pool.shape[1], pool.shape[2] // 17, pool.device
+
+
+def _strided(name, t):
+    """Strides of rows and heads; the dimensions of a head have to be adjacent."""
+    if t.stride(2) != 1 and t.shape[2] > 1:
+        _refuse("%s: the dimensions of a head have to be adjacent", name)
+    return t.stride(0), t.stride(1)
+
+
+def _enqueue(call, args, device):
+    """Call with the stream that torch works on for `device`, the device being the current one meanwhile."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        args.stream = torch.cuda.current_stream().cuda_stream
+        return _check(None, call(C.byref(args)))
+    with torch.cuda.device(device):
+        args.stream = torch.cuda.current_stream().cuda_stream
+        return _check(None, call(C.byref(args)))
+
+
+def april_cache_block_bytes(head_dim: int) -> int:
+    return _check(None, load_library().april_cache_block_bytes(head_dim))
+
+
+def make_cache_pool(n_pages: int, n_kv_heads: int, head_dim: int, device="cuda"):
+    """A pool of n_pages pages of 16 tokens, uninitialised: nothing reads what has not been stored."""
+    import torch
+    return torch.empty((n_pages, n_kv_heads, april_cache_block_bytes(head_dim)), dtype=torch.uint8, device=device)
+
+
+def april_cache_extend(lens, new_lens, block_table, free_pages, free_top, n_rows: int, out: Optional[Sequence] = None) -> CacheTables:
+    """Tables of one iteration from the requests' lengths: sequences of new_lens < 0 give their pages back, the others grow.
+
+    lens, new_lens [n_seqs], free_pages [n_pages], free_top [1]: int32; block_table [n_seqs, max_pages]: int32, in place, as
+    free_pages.  out: an earlier call's result (or six tensors in its order) to write into; its lens and free_top may be
+    the arguments themselves.
+    """
+    import torch
+    dev = lens.device
+    if dev.type != "cuda":
+        _refuse("lens is on %s, not on a GPU", dev)
+    n = lens.shape[0] if lens.dim() == 1 else _refuse("lens: one dimension wanted")
+    table, rows, cols, stride = _table(block_table, dev)
+    if rows != n:
+        _refuse("block_table: %d rows for %d sequences", rows, n)
+    if out is None:
+        e = lambda *s, t=torch.int32: torch.empty(s, dtype=t, device=dev)  # noqa: E731
+        out = CacheTables(e(n), e(1), e(n + 1), e(n_rows, t=torch.int64), e(n_rows), e(1))
+    i32, o = "torch.int32", out
+    args = april_cache_extend_args(
+        n, cols, free_pages.shape[0], n_rows, stride, _want("lens", lens, i32, (n,), dev), _want("new_lens", new_lens, i32, (n,), dev),
+        _want("free_top", free_top, i32, (1,), dev), table, _want("free_pages", free_pages, i32, (None,), dev),
+        _want("out.lens", o[0], i32, (n,), dev), _want("out.free_top", o[1], i32, (1,), dev), _want("out.q_start", o[2], i32, (n + 1,), dev),
+        _want("out.slot_map", o[3], "torch.int64", (n_rows,), dev), _want("out.positions", o[4], i32, (n_rows,), dev),
+        _want("out.status", o[5], i32, (1,), dev))
+    _enqueue(load_library().april_cache_extend, args, dev)
+    return out if isinstance(out, CacheTables) else CacheTables(*out)
+
+
+def april_cache_append(pool, k, v, slot_map, k_values=None, v_values=None) -> None:
+    """Store k and v [n_rows, n_kv_heads, head_dim] (bf16 or fp32) in the pool at slot_map [n_rows] (int64); rows whose slot lies
+    outside the pool are left out.  k_values, v_values: contiguous, of k's type: what the cache now stands for."""
+    p, pages, heads, dh, dev = _pool(pool)
+    t = str(k.dtype)
+    if t not in ("torch.bfloat16", "torch.float32"):
+        _refuse("k: bfloat16 or float32 wanted, not %s", t)
+    shape = (slot_map.shape[0], heads, dh)
+    args = april_cache_append_args(
+        pages, heads, dh, shape[0], APRIL_DTYPE_BF16 if t == "torch.bfloat16" else APRIL_DTYPE_FP32, 0, *_strided("k", k), *_strided("v", v),
+        _want("k", k, t, shape, dev, True), _want("v", v, t, shape, dev, True),
+        None if k_values is None else _want("k_values", k_values, t, shape, dev),
+        None if v_values is None else _want("v_values", v_values, t, shape, dev), _want("slot_map", slot_map, "torch.int64", (None,), dev), p)
+    _enqueue(load_library().april_cache_append, args, dev)
+
+
+def april_cache_attention(q, pool, block_table, lens, max_len: int, *, q_start=None, max_q: int = 1, scale: float = 0.0, out=None, lse=None,
+                          workspace=None):
+    """Causal attention of q [n_rows, n_q_heads, head_dim] (bf16) over the cache: rows q_start[b] .. q_start[b + 1] - 1 are the last tokens
+    of sequence b (q_start None: row b).  lens [n_seqs]: tokens in the cache, those of the rows included; max_len, max_q: bounds on
+    lens and on a sequence's rows.  lse: fp32 [n_rows, n_q_heads], written if given.  Returns out (empty rows behind the
+    last sequence are left as they were; in a new `out` they are undefined)."""
+    import torch
+    p, pages, heads, dh, dev = _pool(pool)
+    if q.dim() != 3:
+        _refuse("q: [rows, heads, head_dim] wanted")
+    shape, n = tuple(q.shape), lens.shape[0]
+    qp = _want("q", q, "torch.bfloat16", (None, None, dh), dev, True)
+    table, rows, cols, stride = _table(block_table, dev)
+    if rows != n:
+        _refuse("block_table: %d rows for %d sequences", rows, n)
+    if out is None:
+        out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+    args = april_cache_attention_args(
+        shape[1], heads, dh, pages, n, cols, shape[0], max_q, max_len, scale, stride, *_strided("q", q), *_strided("out", out),
+        qp, p, table, _want("lens", lens, "torch.int32", (n,), dev),
+        None if q_start is None else _want("q_start", q_start, "torch.int32", (n + 1,), dev), _want("out", out, "torch.bfloat16", shape, dev, True),
+        None if lse is None else _want("lse", lse, "torch.float32", shape[:2], dev))
+    lib = load_library()
+    need = _check(None, lib.april_cache_attention_workspace(C.byref(args)))
+    if need and workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    if workspace is not None:
+        args.workspace = _want("workspace", workspace, "torch.uint8", (None,), dev)
+        args.workspace_bytes = workspace.shape[0]
+    _enqueue(lib.april_cache_attention, args, dev)
+    return out
 
 
 # ---------------------------------------------------------------------------

@@ -24,6 +24,20 @@ namespace {
 
 thread_local std::string g_init_error;
 
+}  // namespace
+
+int april::fail_no_ctx(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  g_init_error = buf;
+  return code;
+}
+
+namespace {
+
 double now_s() {
   return std::chrono::duration<double>(std::chrono::steady_clock::now().time_since_epoch()).count();
 }

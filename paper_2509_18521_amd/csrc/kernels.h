@@ -12,6 +12,9 @@
 
 namespace april {
 
+// Leaves the message that april_last_error(NULL) returns on this thread; returns `code`.
+int fail_no_ctx(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+
 struct RowCtx {
   const int* row_slot;
   const int* row_pos;

@@ -1,0 +1,116 @@
+"""Refusals of the 4-bit cache's operators: found on the host, before anything is enqueued (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+import paper_2509_18521_amd as ap
+from paper_2509_18521_amd import binding
+
+P = 1 << 20                                     # an address that is never read: every call here is refused first
+
+
+def attention_args(**over):
+    a = dict(n_q_heads=8, n_kv_heads=2, head_dim=64, n_pages=9, n_seqs=3, max_pages=4, n_rows=3, max_q=1, max_len=60, scale=0.0, table_stride=4,
+             q_row=512, q_head=64, out_row=512, out_head=64, q=P, pool=P, block_table=P, lens=P, q_start=None, out=P, lse=None, workspace=P,
+             workspace_bytes=1 << 40, stream=None)
+    assert set(over) <= set(a)
+    return ap.april_cache_attention_args(**{**a, **over})
+
+
+def append_args(**over):
+    a = dict(n_pages=9, n_kv_heads=2, head_dim=64, n_rows=3, dtype=1, reserved=0, k_row=128, k_head=64, v_row=128, v_head=64, k=P, v=P, k_values=None,
+             v_values=None, slot_map=P, pool=P, stream=None)
+    assert set(over) <= set(a)
+    return ap.april_cache_append_args(**{**a, **over})
+
+
+def extend_args(**over):
+    a = dict(n_seqs=3, max_pages=4, n_pages=9, n_rows=5, table_stride=4, lens=P, new_lens=P, free_top=P, block_table=P, free_pages=P, lens_out=P,
+             free_top_out=P, q_start=P, slot_map=P, positions=P, status=P, stream=None)
+    assert set(over) <= set(a)
+    return ap.april_cache_extend_args(**{**a, **over})
+
+
+def refused(call, args):
+    rc = call(None if args is None else C.byref(args))
+    assert rc == ap.APRIL_EINVAL
+    return ap.load_library().april_last_error(None).decode()
+
+
+@pytest.mark.parametrize("over", [
+    dict(head_dim=80), dict(head_dim=0), dict(n_q_heads=7), dict(n_q_heads=34), dict(n_kv_heads=0), dict(n_q_heads=-8), dict(n_pages=0), dict(n_seqs=-1),
+    dict(n_rows=-1), dict(max_pages=0), dict(max_q=0), dict(max_len=-1), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
+    dict(q=None), dict(pool=None), dict(block_table=None), dict(lens=None), dict(out=None), dict(n_rows=2), dict(q=P + 8), dict(q_row=513),
+    dict(q_head=68), dict(pool=P + 8), dict(out=P + 4), dict(out_row=514), dict(table_stride=3)])
+def test_attention(over):
+    assert "april_cache_attention" in refused(ap.load_library().april_cache_attention, attention_args(**over))
+
+
+def test_attention_needs_its_workspace():
+    lib = ap.load_library()
+    a = attention_args(max_pages=4096, table_stride=4096, max_len=60000)
+    need = lib.april_cache_attention_workspace(C.byref(a))
+    assert need >= 0
+    if need:
+        for over in (dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=P + 4)):
+            assert "workspace" in refused(lib.april_cache_attention, attention_args(max_pages=4096, table_stride=4096, max_len=60000, **over))
+    assert "head_dim" in refused(lib.april_cache_attention_workspace, attention_args(head_dim=96))
+
+
+@pytest.mark.parametrize("over", [
+    dict(head_dim=48), dict(n_pages=0), dict(n_kv_heads=0), dict(n_rows=-1), dict(dtype=2), dict(reserved=1), dict(k=None), dict(v=None), dict(slot_map=None),
+    dict(pool=None), dict(pool=P + 4), dict(slot_map=P + 4), dict(k=P + 1), dict(v=P + 1), dict(dtype=0, k=P + 2), dict(k_values=P + 8), dict(v_values=P + 8)])
+def test_append(over):
+    assert "april_cache_append" in refused(ap.load_library().april_cache_append, append_args(**over))
+
+
+@pytest.mark.parametrize("over", [
+    dict(n_seqs=0), dict(n_seqs=65537), dict(max_pages=0), dict(max_pages=(1 << 27) + 1), dict(n_pages=0), dict(n_rows=-1), dict(table_stride=3), dict(slot_map=P + 4)] +
+    [{n: None} for n in ("lens", "new_lens", "free_top", "block_table", "free_pages", "lens_out", "free_top_out", "q_start", "slot_map", "positions", "status")])
+def test_extend(over):
+    assert "april_cache_extend" in refused(ap.load_library().april_cache_extend, extend_args(**over))
+
+
+def test_null_arguments():
+    lib = ap.load_library()
+    for name in ("april_cache_extend", "april_cache_append", "april_cache_attention", "april_cache_attention_workspace"):
+        assert "null argument" in refused(getattr(lib, name), None)
+
+
+def test_nothing_to_do_is_no_error():
+    lib = ap.load_library()
+    assert lib.april_cache_append(C.byref(append_args(n_rows=0, k=None, v=None, slot_map=None))) == 0
+    assert lib.april_cache_attention(C.byref(attention_args(n_rows=0, n_seqs=0, q=None, out=None))) == 0
+
+
+def test_block_bytes():
+    assert [ap.april_cache_block_bytes(d) for d in (32, 64, 128)] == [544, 1088, 2176]
+    with pytest.raises(ap.AprilError) as e:
+        ap.april_cache_block_bytes(256)
+    assert e.value.code == ap.APRIL_EINVAL
+
+
+def test_the_binding_refuses_tensors_that_are_not_on_a_gpu_or_of_another_kind():
+    import torch
+    t = lambda *s, d=torch.int32: torch.zeros(s, dtype=d)  # noqa: E731
+    with pytest.raises(ap.AprilError, match="not on a GPU"):
+        ap.april_cache_extend(t(3), t(3), t(3, 4), t(9), t(1), 5)
+    with pytest.raises(ap.AprilError, match="not on a GPU"):
+        ap.april_cache_append(t(2, 2, 544, d=torch.uint8), t(3, 2, 32, d=torch.float32), t(3, 2, 32, d=torch.float32), t(3, d=torch.int64))
+    with pytest.raises(ap.AprilError, match="not on a GPU"):
+        ap.april_cache_attention(t(3, 2, 32, d=torch.bfloat16), t(2, 2, 544, d=torch.uint8), t(3, 4), t(3), 60)
+    cpu = torch.device("cpu")
+    with pytest.raises(ap.AprilError, match="torch.int32 wanted"):
+        binding._want("x", t(3, d=torch.int64), "torch.int32", (3,), cpu)
+    with pytest.raises(ap.AprilError, match="shape"):
+        binding._want("x", t(3), "torch.int32", (4,), cpu)
+    with pytest.raises(ap.AprilError, match="contiguous"):
+        binding._want("x", t(6)[::2], "torch.int32", (3,), cpu)
+    with pytest.raises(ap.AprilError, match="adjacent"):
+        binding._table(t(4, 3).t(), cpu)
+    with pytest.raises(ap.AprilError, match="adjacent"):
+        binding._strided("x", t(3, 32, 2).transpose(1, 2))
+
+
+def test_struct_layouts():
+    assert (C.sizeof(ap.april_cache_extend_args), C.sizeof(ap.april_cache_append_args), C.sizeof(ap.april_cache_attention_args)) == (120, 112, 160)

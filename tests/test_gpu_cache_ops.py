@@ -1,0 +1,621 @@
+"""The 4-bit cache's operators against the plain cache in 64 bits."""
+import numpy as np
+import pytest
+
+from gpu_common import have_gpu
+from oracle import kv_cache as kc
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not have_gpu():
+        pytest.skip("no GPU")
+
+
+def ap():
+    import paper_2509_18521_amd
+    return paper_2509_18521_amd
+
+
+def dev(a, dtype=None):
+    import torch
+    return torch.as_tensor(np.ascontiguousarray(a), device="cuda").to(dtype or torch.from_numpy(np.asarray(a)[:0]).dtype)
+
+
+def i32(a):
+    import torch
+    return torch.tensor(a, dtype=torch.int32, device="cuda")
+
+
+def bf16(a):
+    """(tensor, its values in 64 bits)."""
+    import torch
+    t = torch.as_tensor(np.asarray(a, dtype=np.float32)).bfloat16().cuda()
+    return t, t.double().cpu().numpy()
+
+
+def host(t):
+    return t.double().cpu().numpy() if t.is_floating_point() else t.cpu().numpy()
+
+
+# --- store ---------------------------------------------------------------------------------------------------------------
+
+
+def hard_rows(rng, rows, heads, dh, dtype):
+    """Ordinary values, and blocks where rounding can go wrong."""
+    x = rng.standard_normal((rows, heads, dh)).astype(np.float32)
+    for r in range(rows):
+        kind = r % 12
+        b = slice(32 * (r % (dh // 32)), 32 * (r % (dh // 32)) + 32)
+        if kind == 1:
+            x[r, :, b] = 0.0
+        elif kind == 2:
+            x[r, :, b] = -0.0
+        elif kind == 3:                                        # ties: multiples of a quarter step, largest 6
+            x[r, :, b] = rng.integers(-24, 25, size=(heads, 32)) * 0.25
+        elif kind == 4:                                        # either side of the power's border
+            x[r, :, b] = np.clip(x[r, :, b], -1, 1)
+            x[r, :, b.start] = np.float32(1.75) if heads % 2 else np.nextafter(np.float32(1.75), np.float32(0))
+        elif kind == 5:
+            x[r, :, b] *= np.float32(2.0 ** 120)
+        elif kind == 6:
+            x[r, :, b] *= np.float32(2.0 ** -126)
+        elif kind == 7:
+            x[r, 0, b.start + 5] = np.inf
+        elif kind == 8:
+            x[r, -1, b.start + 31] = -np.inf
+        elif kind == 9:
+            x[r, 0, b.start] = np.nan
+        elif kind == 10:                                       # one strong dimension
+            x[r, :, b.start + 3] = 200.0
+        elif kind == 11:
+            x[r, :, b.start] = np.finfo(np.float32).max if dtype == "f32" else 3.3e38
+    return x
+
+
+@pytest.mark.parametrize("rows,heads,dh,dtype", [(1, 1, 32, "bf16"), (1, 3, 128, "f32"), (37, 2, 64, "bf16"), (50, 5, 32, "f32"), (131, 8, 128, "bf16"),
+                                                 (48, 4, 64, "f32")])
+def test_store_bits_and_values(rows, heads, dh, dtype):
+    import torch
+    rng = np.random.default_rng([rows, heads, dh])
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    k, v = (torch.as_tensor(hard_rows(rng, rows, heads, dh, dtype)).to(t).cuda() for _ in range(2))
+    n_pages = rows // 16 + 5
+    slots = rng.permutation(n_pages * 16)[:rows].astype(np.int64)
+    if rows > 3:
+        slots[1], slots[2] = -1, n_pages * 16
+    start = rng.integers(0, 256, size=(n_pages, heads, 17 * dh), dtype=np.uint8)
+    pool = dev(start)
+    kv, vv = torch.full_like(k, 7.0), torch.full_like(v, 7.0)
+    ap().april_cache_append(pool, k, v, dev(slots), k_values=kv, v_values=vv)
+    want = start.copy()
+    kc.store(want, host(k), host(v), slots)
+    assert np.array_equal(host(pool), want)
+    for x, got in ((k, kv), (v, vv)):
+        y = kc.rounded(host(x))
+        y[(slots < 0) | (slots >= n_pages * 16)] = 7.0
+        assert np.array_equal(host(got), y, equal_nan=True)
+    again = dev(start)
+    ap().april_cache_append(again, k, v, dev(slots))            # without the values
+    assert np.array_equal(host(again), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_store_from_parts_of_a_wider_row(dtype):
+    """Keys and values inside the rows of a projection, at odd offsets too (heads that are not 16-byte aligned)."""
+    import torch
+    rng = np.random.default_rng(5)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    for off, heads, dh in ((0, 2, 64), (1, 3, 32), (8, 2, 128), (4, 1, 128)):
+        wide = torch.as_tensor(rng.standard_normal((21, off + 2 * heads * dh + 3)), dtype=t).cuda()
+        k = wide[:, off:off + heads * dh].unflatten(1, (heads, dh))
+        v = wide[:, off + heads * dh:off + 2 * heads * dh].unflatten(1, (heads, dh))
+        v = v.flip(0).contiguous().transpose(0, 1).contiguous().transpose(0, 1) if off == 8 else v      # heads outermost
+        slots = rng.permutation(32)[:21].astype(np.int64)
+        pool = torch.zeros((2, heads, 17 * dh), dtype=torch.uint8, device="cuda")
+        ap().april_cache_append(pool, k, v, dev(slots))
+        want = np.zeros((2, heads, 17 * dh), dtype=np.uint8)
+        kc.store(want, host(k), host(v), slots)
+        assert np.array_equal(host(pool), want), (off, heads, dh)
+
+
+# --- tables --------------------------------------------------------------------------------------------------------------
+
+
+def run_extend(lens, new, table, free, cols, n_pages, n_rows, out=None, **kw):
+    import torch
+    n = len(lens)
+    tab = torch.full((n, cols + kw.get("gap", 0)), -9, dtype=torch.int32, device="cuda")[:, :cols]
+    for b, t in enumerate(table):
+        tab[b, :len(t)] = i32(t)
+    stack = torch.full((n_pages,), -7, dtype=torch.int32, device="cuda")
+    stack[:len(free)] = i32(free)
+    before = host(tab).copy(), host(stack).copy()
+    got = ap().april_cache_extend(i32(lens), i32(new), tab, stack, i32([kw.get("top", len(free))]), n_rows, out=out)
+    return got, tab, stack, before
+
+
+@pytest.mark.parametrize("n,old_hi,new_hi,n_rows,gap", [(1, 0, 1, 1, 0), (1, 40, 1, 4, 0), (5, 100, 40, 300, 3), (64, 3000, 1, 64, 0), (300, 70, 60, 20000, 1), (1024, 33, 3, 4096, 0),
+                                                        (1025, 20, 20, 30000, 0), (2500, 50, 2, 4000, 5)])
+def test_tables(n, old_hi, new_hi, n_rows, gap):
+    rng = np.random.default_rng([n, old_hi, new_hi])
+    lens = rng.integers(0, old_hi + 1, size=n).tolist()
+    new = rng.integers(0, new_hi + 1, size=n).tolist()
+    for b in rng.permutation(n)[:n // 9]:
+        new[b] = -int(rng.integers(1, 5))
+    if n > 2:
+        lens[1], new[1], lens[2] = 16, 0, 32                    # whole pages, and nothing new
+    held = [-(-x // 16) for x in lens]
+    cols = max(-(-(x + max(a, 0)) // 16) for x, a in zip(lens, new)) + 1
+    lack = sum(max(0, -(-(x + a) // 16) - -(-x // 16)) for x, a in zip(lens, new) if a >= 0)
+    n_pages = sum(held) + max(lack, 1)
+    order = rng.permutation(n_pages).tolist()
+    table, at = [], 0
+    for h in held:
+        table.append(order[at:at + h])
+        at += h
+    free = order[at:]
+    got, tab, stack, before = run_extend(lens, new, table, free, cols, n_pages, n_rows, gap=gap)
+    ref_table, ref_free = [list(t) for t in table], list(free)
+    w_lens, starts, slots, pos, status = kc.extend(lens, new, ref_table, ref_free, cols, n_pages, n_rows)
+    assert status == 0 and int(got.status) == 0
+    assert host(got.lens).tolist() == w_lens and host(got.q_start).tolist() == starts and int(got.free_top) == len(ref_free)
+    assert host(got.slot_map).tolist() == slots and host(got.positions).tolist() == pos
+    assert host(stack)[:len(ref_free)].tolist() == ref_free
+    for b in range(n):
+        row = host(tab)[b] if n < 400 else None
+        if row is not None and new[b] >= 0:
+            assert row[:len(ref_table[b])].tolist() == ref_table[b] and np.all(row[len(ref_table[b]):] == -9)
+    want = before[0].copy()
+    for b in range(n):
+        if new[b] >= 0:
+            want[b, :len(ref_table[b])] = ref_table[b]
+    assert np.array_equal(host(tab), want)
+
+
+@pytest.mark.parametrize("what,status", [("pages", 1), ("rows", 2), ("negative", 2), ("long", 2), ("grown", 2), ("top", 2), ("top-", 2), ("stack", 2)])
+@pytest.mark.parametrize("n", [6, 1100])
+@pytest.mark.parametrize("rows", [200, 9000])
+def test_refused_tables_change_nothing(what, status, n, rows):
+    lens, new = [5] * n, [1] * n
+    cols, free = 4, list(range(n, n + 40))
+    kw = {}
+    new[1] = -1                                                 # would give a page back
+    if what == "pages":
+        for b in range(3):
+            new[b] = 50
+        free = [n, n + 1]
+    elif what == "rows":
+        rows = sum(max(a, 0) for a in new) - 1
+    elif what == "negative":
+        lens[n - 1] = -3
+    elif what == "long":
+        lens[n - 1] = cols * 16 + 1
+    elif what == "grown":
+        new[2] = cols * 16
+    elif what == "top":
+        kw["top"] = n + 41
+    elif what == "top-":
+        kw["top"] = -1
+    elif what == "stack":                                       # the page given back has no place on the stack
+        kw["top"] = n + 40
+    if what != "rows":
+        rows = max(rows, sum(max(a, 0) for a in new))
+    table = [[b] for b in range(n)]
+    got, tab, stack, before = run_extend(lens, new, table, free, cols, n + 40, rows, **kw)
+    assert int(got.status) == status
+    assert host(got.lens).tolist() == lens and int(got.free_top) == kw.get("top", len(free)) and not host(got.q_start).any()
+    assert np.all(host(got.slot_map) == -1) and np.all(host(got.positions) == -1)
+    assert np.array_equal(host(tab), before[0]) and np.array_equal(host(stack), before[1])
+
+
+# --- attention -----------------------------------------------------------------------------------------------------------
+
+
+class Cache:
+    """A pool whose pages hold random bytes where nothing is stored, and the sequences' keys and values as it stands for them."""
+
+    def __init__(self, rng, lens, heads, dh, cols=None, spare=3, strong=0.6):
+        import torch
+        held = [-(-max(n, 0) // 16) for n in lens]
+        n_pages = sum(held) + spare
+        self.cols = cols or max(max(held), 1)
+        order = rng.permutation(n_pages)
+        self.table = rng.integers(-1000, 1000, size=(len(lens), self.cols)).astype(np.int32)       # garbage behind a sequence's pages
+        self.pool = dev(rng.integers(0, 256, size=(n_pages, heads, 17 * dh), dtype=np.uint8))
+        self.pool[:, :, 16 * dh:] = 255                        # NaN wherever nothing has been stored
+        self.k, self.v, slots, at = [], [], [], 0
+        for b, n in enumerate(lens):
+            self.table[b, :held[b]] = order[at:at + held[b]]
+            at += held[b]
+            k = rng.standard_normal((max(n, 0), heads, dh)) * np.exp(strong * rng.standard_normal((1, heads, dh)))
+            self.k.append(k)
+            self.v.append(rng.standard_normal((max(n, 0), heads, dh)))
+            slots += [int(self.table[b, t // 16]) * 16 + t % 16 for t in range(max(n, 0))]
+        k, v = (torch.as_tensor(np.concatenate(x), dtype=torch.bfloat16).cuda() for x in (self.k, self.v))
+        kv, vv = torch.empty_like(k), torch.empty_like(v)
+        if len(slots):
+            ap().april_cache_append(self.pool, k, v, dev(np.array(slots, dtype=np.int64)), k_values=kv, v_values=vv)
+        parts = np.cumsum([max(n, 0) for n in lens])[:-1]
+        self.k, self.v = np.split(host(kv), parts), np.split(host(vv), parts)
+        self.lens = lens
+
+
+def check_attention(out, lse, q, starts, cache, scale, seqs=None, rows=None):
+    """Errors allowed: weights are rounded to bf16 (half a step, 2^-8 of each: 2^-8 of the mean of |v|) as is the result (2^-8 of it); scores are
+    sums of dh products in fp32, n rounding steps of 2^-24 of sum |q k| each, and the exponentials' and their sum's own."""
+    half, u = 2.0 ** -8, 2.0 ** -24
+    for b in range(len(cache.lens)) if seqs is None else seqs:
+        r = slice(starts[b], starts[b + 1])
+        x = q[r]
+        if x.shape[0] == 0:
+            continue
+        want, wl, spread = kc.attention(x, cache.k[b], cache.v[b], scale)
+        n, dh = cache.k[b].shape[0], x.shape[2]
+        top = 0.0
+        if n:
+            g = x.shape[1] // cache.k[b].shape[1]
+            top = scale * max(float((np.abs(cache.k[b][:, h // g]) @ np.abs(x[:, h]).T).max()) for h in range(x.shape[1]))
+        score = (2 * dh + 8) * u * top + 4 * u                  # of a score, and of its exponential's relative value
+        if rows is not None:
+            x, want, wl, spread = x[:rows], want[:rows], wl[:rows], spread[:rows]
+        m = want.shape[0]
+        tol = half * (spread + np.abs(want)) + (2 * score + 2 * n * u) * spread + 1e-30
+        got = out[r][:m]
+        assert np.all(np.abs(got - want) <= tol * 1.001), (b, float(np.max(np.abs(got - want) / tol)))
+        if lse is not None:
+            gl = lse[r][:m]
+            empty = np.isneginf(wl)
+            assert np.array_equal(np.isneginf(gl), empty)
+            assert np.all(np.abs(gl - wl)[~empty] <= (score + n * u + 4 * u * (1 + np.abs(wl)))[~empty]), (b, float(np.max(np.abs(gl - wl)[~empty])))
+
+
+def attend(cache, q, starts, scale=0.0, max_len=None, max_q=None, **kw):
+    import torch
+    heads = q.shape[1]
+    lse = torch.full((q.shape[0], heads), 5.0, device="cuda")
+    out = torch.full(tuple(q.shape), 5.0, dtype=torch.bfloat16, device="cuda")
+    counts = np.diff(starts)
+    one = np.all(counts == 1) and kw.pop("no_start", True)
+    ap().april_cache_attention(q, cache.pool, dev(cache.table), i32(cache.lens), max_len if max_len is not None else max(max(cache.lens), 0),
+                               q_start=None if one else i32(starts), max_q=max_q or int(max(counts.max(), 1)), scale=scale, out=out, lse=lse)
+    return host(out), host(lse), out, lse
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(14, 2, 64), (32, 8, 128), (4, 4, 32), (8, 1, 128), (16, 1, 64), (5, 1, 128), (21, 3, 32), (6, 2, 64)])
+@pytest.mark.parametrize("lens", [[1], [0], [16, 17, 15, 31, 32, 33], [129, 0, 64, 500, 1]])
+def test_one_row_a_sequence(hq, hkv, dh, lens):
+    rng = np.random.default_rng([hq, dh, len(lens)])
+    cache = Cache(rng, lens, hkv, dh)
+    q, qv = bf16(rng.standard_normal((len(lens), hq, dh)) * 2)
+    out, lse, _, _ = attend(cache, q, np.arange(len(lens) + 1))
+    check_attention(out, lse, qv, np.arange(len(lens) + 1), cache, 1 / np.sqrt(dh))
+
+
+@pytest.mark.parametrize("hq,hkv,dh,lens", [(32, 8, 128, [4096, 1024, 2047]), (7, 1, 64, [5000, 3, 1025]), (8, 2, 128, [9001]), (4, 4, 32, [6000, 4097]), (16, 1, 128, [4200])])
+def test_one_row_over_long_contexts(hq, hkv, dh, lens):
+    rng = np.random.default_rng([hq, dh, lens[0]])
+    cache = Cache(rng, lens, hkv, dh, cols=700)
+    q, qv = bf16(rng.standard_normal((len(lens), hq, dh)) * 2)
+    for max_len in (max(lens), 11200):                          # a loose bound splits the work otherwise
+        out, lse, _, _ = attend(cache, q, np.arange(len(lens) + 1), max_len=max_len)
+        check_attention(out, lse, qv, np.arange(len(lens) + 1), cache, 1 / np.sqrt(dh))
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(20, 4, 64), (32, 8, 128), (8, 8, 32), (16, 1, 128), (14, 2, 64), (3, 1, 128)])
+@pytest.mark.parametrize("lens,counts", [([40, 5, 0, 333, 64], [2, 5, 1, 4, 0]), ([70, 1000, 17], [9, 1, 17]), ([200, 130, 1, 64], [200, 130, 1, 64]),
+                                         ([5, 300], [9, 100])])
+def test_several_rows_a_sequence(hq, hkv, dh, lens, counts):
+    """Drafted tokens, pieces of prompts, whole prompts; more rows than tokens (the first see nothing); sequences without rows."""
+    rng = np.random.default_rng([hq, dh, lens[0]])
+    cache = Cache(rng, lens, hkv, dh)
+    starts = np.concatenate([[0], np.cumsum(counts)])
+    q, qv = bf16(rng.standard_normal((starts[-1] + 3, hq, dh)) * 2)          # three rows of padding
+    out, lse, _, _ = attend(cache, q, starts)
+    check_attention(out, lse, qv, starts, cache, 1 / np.sqrt(dh))
+    assert np.all(out[starts[-1]:] == 5.0) and np.all(lse[starts[-1]:] == 5.0)
+
+
+@pytest.mark.parametrize("hq,hkv,dh,lens,counts", [(32, 8, 128, [1500, 700], [1500, 300]), (14, 2, 64, [4300], [90]), (4, 4, 32, [2100, 2], [700, 2]),
+                                                   (16, 1, 128, [6000], [33])])
+def test_many_rows_over_long_contexts(hq, hkv, dh, lens, counts):
+    """Of every sequence the rows at the ends and some between are compared."""
+    rng = np.random.default_rng([hq, dh, lens[0], 1])
+    cache = Cache(rng, lens, hkv, dh)
+    starts = np.concatenate([[0], np.cumsum(counts)])
+    q, qv = bf16(rng.standard_normal((starts[-1], hq, dh)) * 2)
+    out, lse, _, _ = attend(cache, q, starts)
+    for b, (n, c) in enumerate(zip(lens, counts)):
+        for i in sorted({0, 1, c // 3, c - 1} & set(range(c))):
+            sub = type("S", (), dict(lens=[n], k=[cache.k[b][:n - c + i + 1]], v=[cache.v[b][:n - c + i + 1]]))
+            r = starts[b] + i
+            check_attention(out[r:r + 1], lse[r:r + 1], qv[r:r + 1], [0, 1], sub, 1 / np.sqrt(dh))
+
+
+def test_strides_scale_and_first_rows():
+    """Queries and results inside wider rows, heads outermost, a block table's rows apart, q_start that begins behind row 0."""
+    import torch
+    rng = np.random.default_rng(11)
+    lens, counts, hq, hkv, dh = [90, 33, 47], [1, 3, 2], 6, 2, 64
+    cache = Cache(rng, lens, hkv, dh)
+    starts = np.concatenate([[0], np.cumsum(counts)]) + 2
+    q, qv = bf16(rng.standard_normal((9, hq, dh)))
+    wide_q = torch.zeros((9, hq + 3, dh + 8), dtype=torch.bfloat16, device="cuda")
+    wide_q[:, 2:2 + hq, 8:] = q
+    out = torch.full((hq, 9, dh + 4), 5.0, dtype=torch.bfloat16, device="cuda").transpose(0, 1)[..., 4:]
+    table = torch.full((3, cache.cols + 9), 12345, dtype=torch.int32, device="cuda")[:, 5:5 + cache.cols]
+    table.copy_(dev(cache.table))
+    lse = torch.full((9, hq), 5.0, device="cuda")
+    got = ap().april_cache_attention(wide_q[:, 2:2 + hq, 8:], cache.pool, table, i32(lens), 90, q_start=i32(starts), max_q=3, scale=0.31, out=out, lse=lse)
+    assert got is out
+    check_attention(host(out), host(lse), qv, starts, cache, float(np.float32(0.31)))
+    assert np.all(host(out)[[0, 1, 8]] == 5.0) and np.all(host(lse)[[0, 1, 8]] == 5.0)
+
+
+@pytest.mark.parametrize("count", [1, 3, 40])
+def test_nan_reaches_the_rows_that_see_it_and_no_others(count):
+    """A block of NaN keys, one of NaN values, one of each far back, in each of 40 tokens' places: per row and dimension as in the plain form."""
+    import torch
+    rng = np.random.default_rng(13)
+    lens, hq, hkv, dh = [64, 50, 300], 8, 2, 128
+    cache = Cache(rng, lens, hkv, dh)
+    q, qv = bf16(rng.standard_normal((3 * count, hq, dh)))
+    starts = np.arange(4) * count
+    where = [(0, 63, 0, 1, 2), (1, 49 - count // 2, 1, 0, 1), (2, 5, 1, 1, 3), (0, 64 - count, 1, 0, 0)]   # sequence, token, key | value, head, block
+    for b, t, value, h, blk in where:
+        cache.pool[int(cache.table[b, t // 16]), h, 16 * dh + (blk * 16 + t % 16) * 2 + value] = 255
+        (cache.v if value else cache.k)[b][t, h, 32 * blk:32 * blk + 32] = np.nan
+    out, lse, _, _ = attend(cache, q, starts)
+    for b in range(3):
+        with np.errstate(invalid="ignore"):
+            want, wl, _ = kc.attention(qv[starts[b]:starts[b + 1]], cache.k[b], cache.v[b], 1 / np.sqrt(dh))
+        r = slice(starts[b], starts[b + 1])
+        assert np.array_equal(np.isnan(out[r]), np.isnan(want)), b
+        assert np.array_equal(np.isnan(lse[r]), np.isnan(wl)), b
+        fine = ~np.isnan(want)
+        assert np.all(np.abs(out[r] - want)[fine] < 0.05)
+
+
+@pytest.mark.parametrize("count,lens", [(1, [700, 40, 33]), (2, [700, 40, 33]), (50, [700, 400, 333]), (1, [5000, 40, 33])])
+def test_bad_pages_and_lengths_make_nan_of_their_own_rows(count, lens):
+    """Page ids outside the pool, lengths below zero, beyond the bound, beyond the block table: no access outside the arrays, NaN rows."""
+    rng = np.random.default_rng(17)
+    hq, hkv, dh = 8, 2, 64
+    starts = np.arange(4) * count
+    for page, at in ((1 << 30, 0), (-1, 1), (-(1 << 31), 2), (10 ** 6, 0)):
+        cache = Cache(rng, lens, hkv, dh)
+        q, qv = bf16(rng.standard_normal((3 * count, hq, dh)))
+        cache.table[0, at] = page
+        out, lse, _, _ = attend(cache, q, starts)
+        assert np.all(np.isnan(out[:count])) and np.all(np.isnan(lse[:count]))
+        check_attention(out, lse, qv, starts, cache, 1 / np.sqrt(dh), seqs=[1, 2])
+    for length in (-1, lens[0] + 1, 1 << 30, -(1 << 31)):
+        cache = Cache(rng, lens, hkv, dh)
+        q, qv = bf16(rng.standard_normal((3 * count, hq, dh)))
+        cache.lens = [length] + lens[1:]
+        out, lse, _, _ = attend(cache, q, starts, max_len=lens[0])
+        assert np.all(np.isnan(out[:count])) and np.all(np.isnan(lse[:count]))
+        check_attention(out, lse, qv, starts, cache, 1 / np.sqrt(dh), seqs=[1, 2])
+    cache = Cache(rng, lens, hkv, dh)
+    cache.lens = [cache.cols * 16 + 1] + lens[1:]
+    out, lse, _, _ = attend(cache, q, starts, max_len=1 << 20)
+    assert np.all(np.isnan(out[:count])) and np.all(np.isnan(lse[:count]))
+    check_attention(out, lse, qv, starts, cache, 1 / np.sqrt(dh), seqs=[1, 2])
+
+
+def test_first_rows_that_do_not_fit_are_not_followed():
+    """q_start outside the rows, and not ascending: nothing outside the arrays is touched, the sequences that fit are right."""
+    rng = np.random.default_rng(19)
+    lens, hq, hkv, dh = [60, 50, 40, 30], 4, 1, 64
+    cache = Cache(rng, lens, hkv, dh)
+    q, qv = bf16(rng.standard_normal((12, hq, dh)))
+    for starts, good in (([0, 3, 2, 5, 7], []), ([-4, 2, 5, 9, 40], [1, 2]), ([100, 200, 300, 400, 500], []), ([0, 1, 3, 1 << 30, -5], [0, 1])):
+        for max_q in (3, 12):
+            out, lse, _, _ = attend(cache, q, np.array(starts), max_q=max_q)
+            check_attention(out, lse, qv, starts, cache, 1 / np.sqrt(dh), seqs=good, rows=max_q)
+
+
+def test_large_scores_and_equal_ones():
+    """Scores of a few hundred (one token takes all), all alike (a plain mean), and queries of zero."""
+    rng = np.random.default_rng(23)
+    lens, hq, hkv, dh = [200, 77, 1000], 8, 2, 128
+    cache = Cache(rng, lens, hkv, dh)
+    x = rng.standard_normal((3, hq, dh))
+    x[0] *= 200
+    x[1] = 0
+    q, qv = bf16(x)
+    out, lse, _, _ = attend(cache, q, np.arange(4))
+    check_attention(out, lse, qv, np.arange(4), cache, 1 / np.sqrt(dh))
+
+
+def test_pool_beyond_four_gigabytes():
+    """Pages at the far end of a pool of 5 GB, and slots that pass 32 bits in bytes."""
+    import torch
+    rng = np.random.default_rng(29)
+    hq, hkv, dh, n = 8, 4, 128, 45
+    n_pages = 5 * (1 << 30) // (hkv * 17 * dh)
+    pool = torch.empty((n_pages, hkv, 17 * dh), dtype=torch.uint8, device="cuda")
+    pages = [n_pages - 1, n_pages - 70000, n_pages - 3]
+    slots = np.array([pages[t // 16] * 16 + t % 16 for t in range(n)], dtype=np.int64)
+    k, v = (torch.randn((n, hkv, dh), device="cuda").bfloat16() for _ in range(2))
+    kv, vv = torch.empty_like(k), torch.empty_like(v)
+    ap().april_cache_append(pool, k, v, dev(slots), k_values=kv, v_values=vv)
+    cache = type("C", (), dict(lens=[n], k=[host(kv)], v=[host(vv)]))
+    for count in (1, 30):
+        q, qv = bf16(rng.standard_normal((count, hq, dh)))
+        out = ap().april_cache_attention(q, pool, i32([pages]), i32([n]), n, q_start=i32([0, count]), max_q=count)
+        check_attention(host(out), None, qv, [0, count], cache, 1 / np.sqrt(dh))
+
+
+@pytest.mark.parametrize("count", [1, 60])
+def test_same_bits_each_time_and_whatever_the_batch_holds_besides(count):
+    rng = np.random.default_rng(31)
+    hq, hkv, dh, lens = 16, 4, 128, [3000, 200, 4500, 700]
+    cache = Cache(rng, lens, hkv, dh)
+    q, _ = bf16(rng.standard_normal((4 * count, hq, dh)))
+    a = attend(cache, q, np.arange(5) * count)
+    for _ in range(3):
+        b = attend(cache, q, np.arange(5) * count)
+        assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+
+
+# --- streams, graphs, the three together -------------------------------------------------------------------------------------
+
+
+def test_two_streams_at_once():
+    import torch
+    rng = np.random.default_rng(37)
+    hq, hkv, dh = 16, 4, 128
+    caches = [Cache(rng, lens, hkv, dh) for lens in ([6000, 20], [100, 5000])]
+    qs = [bf16(rng.standard_normal((2, hq, dh))) for _ in caches]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in caches]
+    got = [[], []]
+    for _ in range(5):
+        for i, (c, (q, _)) in enumerate(zip(caches, qs)):
+            with torch.cuda.stream(streams[i]):
+                lse = torch.empty((2, hq), device="cuda")
+                got[i].append((ap().april_cache_attention(q, c.pool, dev(c.table), i32(c.lens), 6000, lse=lse), lse))
+    torch.cuda.synchronize()
+    for i, c in enumerate(caches):
+        for out, lse in got[i]:
+            check_attention(host(out), host(lse), qs[i][1], np.arange(3), c, 1 / np.sqrt(dh))
+
+
+class Rollouts:
+    """Sequences that grow, end and start again, by the operators and by the plain cache."""
+
+    def __init__(self, seed, n, hq, hkv, dh, cols, n_pages, n_rows):
+        import torch
+        self.rng = np.random.default_rng(seed)
+        self.n, self.hq, self.hkv, self.dh, self.cols, self.n_pages, self.n_rows = n, hq, hkv, dh, cols, n_pages, n_rows
+        order = self.rng.permutation(n_pages)
+        self.free, self.table, self.lens = order.tolist(), [[] for _ in range(n)], [0] * n
+        self.keys, self.values = [np.zeros((0, hkv, dh)) for _ in range(n)], [np.zeros((0, hkv, dh)) for _ in range(n)]
+        self.d_lens, self.d_top, self.d_free = i32([0] * n), i32([n_pages]), i32(self.free)
+        self.d_table = torch.zeros((n, cols), dtype=torch.int32, device="cuda")
+        self.pool = torch.full((n_pages, hkv, 17 * dh), 255, dtype=torch.uint8, device="cuda")
+        e = lambda *s, t=torch.int32: torch.zeros(s, dtype=t, device="cuda")  # noqa: E731
+        self.tables = ap().CacheTables(self.d_lens, self.d_top, e(n + 1), e(n_rows, t=torch.int64), e(n_rows), e(1))      # in place
+        self.new = e(n)
+        self.k, self.v = (torch.zeros((n_rows, hkv, dh), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        self.q, self.out = (torch.zeros((n_rows, hq, dh), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        self.lse = torch.zeros((n_rows, hq), device="cuda")
+
+    def enqueue(self, max_q):
+        t = ap().april_cache_extend(self.d_lens, self.new, self.d_table, self.d_free, self.d_top, self.n_rows, out=self.tables)
+        ap().april_cache_append(self.pool, self.k, self.v, t.slot_map)
+        ap().april_cache_attention(self.q, self.pool, self.d_table, t.lens, self.cols * 16, q_start=t.q_start, max_q=max_q, out=self.out, lse=self.lse)
+
+    def inputs(self, new):
+        import torch
+        self.new.copy_(i32(new))
+        for t in (self.k, self.v, self.q):
+            t.copy_(torch.as_tensor(self.rng.standard_normal(tuple(t.shape)), dtype=torch.bfloat16))
+        self.out.fill_(5.0)
+        self.lse.fill_(5.0)
+
+    def check(self, new, status=0):
+        lens, starts, slots, pos, st = kc.extend(self.lens, new, self.table, self.free, self.cols, self.n_pages, self.n_rows)
+        t = self.tables
+        assert st == status == int(t.status)
+        assert host(t.lens).tolist() == lens and host(t.slot_map).tolist() == slots and host(t.positions).tolist() == pos
+        assert int(t.free_top) == len(self.free)
+        k, v = kc.rounded(host(self.k)), kc.rounded(host(self.v))
+        for b in range(self.n):
+            if st == 0 and new[b] < 0:
+                self.keys[b], self.values[b], self.table[b] = self.keys[b][:0], self.values[b][:0], []
+            self.keys[b] = np.concatenate([self.keys[b], k[starts[b]:starts[b + 1]]])
+            self.values[b] = np.concatenate([self.values[b], v[starts[b]:starts[b + 1]]])
+        self.lens = lens
+        view = type("S", (), dict(lens=lens, k=self.keys, v=self.values))
+        check_attention(host(self.out), host(self.lse), host(self.q), starts, view, 1 / np.sqrt(self.dh))
+        assert np.all(host(self.out)[starts[-1]:] == 5.0) and np.all(host(self.lse)[starts[-1]:] == 5.0)
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(14, 2, 64), (8, 2, 128), (4, 4, 32)])
+def test_rollouts_admitted_grown_and_ended(hq, hkv, dh):
+    """Prompts admitted, tokens decoded one and a few at a time, sequences ended and replaced, a step refused for lack of pages."""
+    r = Rollouts([hq, dh], 5, hq, hkv, dh, cols=12, n_pages=26, n_rows=96)
+    steps = [[17, 40, 1, 0, 33], [1] * 5, [1] * 5, [1, -1, 1, 1, 1], [3, 16, 1, 0, 2], [1, 1, -1, -1, 1], [1, 1, 31, 1, 1], [5] * 5]
+    for new in steps:
+        r.inputs(new)
+        r.enqueue(max(new))
+        r.check(new)
+    new = [96, 0, 0, 0, 0]                                      # a table row's worth, but too few pages are left
+    for b in range(1, 5):
+        while len(r.free) > 2 and (r.lens[b] + 16) <= r.cols * 16:
+            grow = [0] * 5
+            grow[b] = 16
+            r.inputs(grow)
+            r.enqueue(16)
+            r.check(grow)
+    r.inputs(new)
+    r.enqueue(96)
+    r.check(new, status=1)
+    r.inputs([1] + [0] * 4)
+    r.enqueue(1)
+    r.check([1] + [0] * 4)
+
+
+def test_captured_iterations_with_eager_ones_between():
+    """Two graphs of the three operators (one row a sequence; up to 8), replayed with eager iterations and other work between."""
+    import torch
+    r = Rollouts(41, 4, 14, 2, 64, cols=40, n_pages=200, n_rows=32)
+    r.inputs([8] * 4)
+    r.enqueue(8)
+    r.check([8] * 4)
+    state = [t.clone() for t in (r.d_lens, r.d_top, r.d_free, r.d_table, r.pool)]
+    side = torch.cuda.Stream()
+    graphs = []
+    for max_q in (1, 8):
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            r.enqueue(max_q)                                    # warm up
+        torch.cuda.current_stream().wait_stream(side)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            r.enqueue(max_q)
+        graphs.append(g)
+    for t, s in zip((r.d_lens, r.d_top, r.d_free, r.d_table, r.pool), state):
+        t.copy_(s)
+    for i in range(9):
+        which = i % 3
+        new = [1, 1, 1, 1] if which == 0 else [int(x) for x in r.rng.integers(0, 9, size=4)]
+        if i == 4:
+            new[2] = -1
+        r.inputs(new)
+        if which == 2:
+            r.enqueue(8)
+        else:
+            graphs[which].replay()
+        torch.cuda.synchronize()
+        r.check(new)
+        torch.randn(1 << 20, device="cuda").sum().item()
+
+
+def test_refused_tensors():
+    import torch
+    z = lambda *s, d=torch.int32: torch.zeros(s, dtype=d, device="cuda")  # noqa: E731
+    pool, q = z(4, 2, 1088, d=torch.uint8), z(3, 8, 64, d=torch.bfloat16)
+    bad = [lambda: ap().april_cache_attention(q.float(), pool, z(3, 4), z(3), 60),
+           lambda: ap().april_cache_attention(q, pool[:, :, :1000], z(3, 4), z(3), 60),
+           lambda: ap().april_cache_attention(q, pool, z(2, 4), z(3), 60),
+           lambda: ap().april_cache_attention(q, pool, z(3, 4), z(3, d=torch.int64), 60),
+           lambda: ap().april_cache_attention(q, pool, z(3, 4).cpu(), z(3), 60),
+           lambda: ap().april_cache_attention(q, pool, z(3, 4), z(3), 60, q_start=z(3)),
+           lambda: ap().april_cache_attention(q, pool, z(3, 4), z(3), 60, out=z(3, 8, 32, d=torch.bfloat16)),
+           lambda: ap().april_cache_attention(q[:, :7], pool, z(3, 4), z(3), 60),
+           lambda: ap().april_cache_attention(q, pool, z(3, 4), z(3), 60, max_q=0),
+           lambda: ap().april_cache_append(pool, z(3, 2, 64, d=torch.float16), z(3, 2, 64, d=torch.float16), z(3, d=torch.int64)),
+           lambda: ap().april_cache_append(pool, z(3, 2, 64, d=torch.float32), z(3, 2, 64, d=torch.bfloat16), z(3, d=torch.int64)),
+           lambda: ap().april_cache_append(pool, z(3, 2, 64, d=torch.float32), z(3, 2, 64, d=torch.float32), z(4, d=torch.int64)),
+           lambda: ap().april_cache_append(pool, z(3, 64, 2, d=torch.float32).transpose(1, 2), z(3, 2, 64, d=torch.float32), z(3, d=torch.int64)),
+           lambda: ap().april_cache_extend(z(3), z(4), z(3, 4), z(9), z(1), 5),
+           lambda: ap().april_cache_extend(z(3), z(3), z(3, 4), z(9), z(2), 5)]
+    for call in bad:
+        with pytest.raises(ap().AprilError) as e:
+            call()
+        assert e.value.code == ap().APRIL_EINVAL
