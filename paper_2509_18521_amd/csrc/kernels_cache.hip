@@ -1,4 +1,5 @@
 // Kernels of the 4-bit KV cache (gfx950): tables from request lengths, the store, the attention that reads it.
+#include <algorithm>
 #include <tuple>
 
 #include "cache.h"
@@ -326,10 +327,394 @@ __global__ __launch_bounds__(64) void cache_attn_simple_kernel(CacheAttn a, int 
 
 }  // namespace
 
-size_t cache_attention_workspace(const CacheAttn&, int) { return 0; }
+// ---------------------------------------------------------------------------
+// Attention of few rows: one workgroup (4 wavefronts) per (sequence, KV head, split of the context), up to 16 CT columns
+// (row of the sequence, query head of the KV head).  The wavefronts take the split's tiles of 32 tokens in turn, each with an online
+// softmax in registers; they meet in LDS, the splits of a context in a second small kernel, both in a fixed order.
+//
+// Products on v_mfma_f32_16x16x32_bf16, transposed, so that the scores' accumulators are the probabilities' operand:
+//   S^T[token, column] = K . Q^T,  O^T[dim, column] = V^T . P^T.
+// K: the order of a contraction is free, so lane (token t, g) takes the dimensions g dh / 4 .. of its token, which lie together
+// with one scale (dh 128: exactly a block of 32), and Q is loaded in the same order; codes become bf16 in
+// registers, exactly.  (A scaled product straight from the codes, v_mfma_scale_f32_16x16x128_f8f6f4 with Q split into two e4m3
+// terms, was tried: its sums keep about 17 bits, 4.5e-6 of a score against 8e-9 here, and a short row's lse showed it.)
+// V: a fragment wants 8 tokens of one dimension, the store 32 dimensions of one token (so that a token is appended without
+// touching its neighbours): lanes open the blocks that they loaded into a tile of LDS, [token][dim], and
+// read it back transposed (ds_read_b64_tr_b16).  Rows of dh + 16 elements put the 8 rows of a read on different banks.
+// ---------------------------------------------------------------------------
+namespace {
+
+constexpr int CA_WAVES = 4, CA_MOST = 4096;      // tokens of a split, at most: a lane holds 4 page ids
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+// Four rows (tokens) of 16 bf16 columns each; lane i of 16 points at row i / 4, columns 4 (i % 4).. and gets column i, rows 0..3.
+__device__ inline bf16x4 read_transposed(const bf16_t* p) {
+  union { s16x4 s; bf16x4 b; } u;
+#if defined(__HIP_DEVICE_COMPILE__)
+  u.s = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p));
+#else
+  u.b = *reinterpret_cast<const bf16x4*>(p);
+#endif
+  return u.b;
+}
+
+struct Split { int chunk, n; };                  // tokens of a split, splits of the longest context
+
+template <int DH> struct KRaw;
+template <> struct KRaw<32> { typedef unsigned type; };
+template <> struct KRaw<64> { typedef uint2 type; };
+template <> struct KRaw<128> { typedef uint4 type; };
+template <int DH> __device__ inline unsigned k_word(const typename KRaw<DH>::type& r, int c) {
+  if constexpr (DH == 32) return r;
+  else if constexpr (DH == 64) return c ? r.y : r.x;
+  else return c == 0 ? r.x : c == 1 ? r.y : c == 2 ? r.z : r.w;
+}
+
+// Partial results of a split: per (row, head) maximum and sum, then the unnormalised output.
+__device__ inline float* part_ml(const CacheAttn& a, int split, int r, int h) { return a.ws + (((size_t)split * a.n_rows + r) * a.Hq + h) * 2; }
+template <int DH> __device__ inline float* part_o(const CacheAttn& a, int n_splits, int split, int r, int h) {
+  return a.ws + (size_t)n_splits * a.n_rows * a.Hq * 2 + (((size_t)split * a.n_rows + r) * a.Hq + h) * DH;
+}
+
+template <int DH, int CT>
+__global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_kernel(CacheAttn a, Split sp) {
+  constexpr int KC = DH / 32, DT = DH / 16, NV = DH == 128 ? 2 : 1;
+  constexpr int VS = DH + 16, OS = DH + 4;            // row strides in LDS: opened values, merged outputs
+  constexpr int REC = CT * 16 * (2 + OS);             // floats of a wavefront's result
+  constexpr int REGION = REC * 4 > 32 * VS * 2 ? REC * 4 : 32 * VS * 2;
+  constexpr float RESCALE = 8.0f;
+  typedef typename KRaw<DH>::type kraw_t;
+  __shared__ __align__(16) unsigned char lds[CA_WAVES][REGION];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane & 15, g = lane >> 4;
+  const int G = a.Hq / a.Hkv;
+  // KV heads go round first: the heads of one sequence on different XCDs; splits last: only long contexts have the later ones
+  const int kvh = (int)(blockIdx.x % a.Hkv), rest = (int)(blockIdx.x / a.Hkv), b = rest % a.n_seqs, split = rest / a.n_seqs;
+  const int first = a.q_start != nullptr ? a.q_start[b] : b, count = a.q_start != nullptr ? a.q_start[b + 1] - first : 1;
+  const int len_raw = a.lens[b];
+  if (first < 0 || count <= 0 || first >= a.n_rows) return;
+  const int nq = min(min(count, a.max_q), a.n_rows - first);
+  bool bad = len_raw < 0 || len_raw > a.max_len;
+  const int len = bad ? 0 : len_raw;
+  const int t_begin = split * sp.chunk;
+  if (split > 0 && t_begin >= len) return;
+  const int n_splits = max(1, (len + sp.chunk - 1) / sp.chunk);
+  const int t_end = min(len, t_begin + sp.chunk), n_tiles = (t_end - t_begin + 31) >> 5, n_pages = (t_end - t_begin + 15) >> 4;
+
+  // page ids of the split, one per lane and register; ids outside the pool are noticed and not followed
+  const int* bt = a.block_table + (size_t)b * a.table_stride + (t_begin >> 4);
+  int my_page[CA_MOST / 1024];
+#pragma unroll
+  for (int q = 0; q < CA_MOST / 1024; ++q) {
+    const int i = q * 64 + lane;
+    my_page[q] = n_pages > 0 && (q == 0 || q * 64 < n_pages) ? bt[i < n_pages ? i : n_pages - 1] : 0;
+    const bool out = (unsigned)my_page[q] >= (unsigned)a.n_pages;
+    bad |= __any(out);
+    if (out) my_page[q] = 0;
+  }
+
+  // what this lane takes of a page's block: keys, their scale; values, theirs
+  const int kblk = g * DH / 128, kbyte = (g * (DH / 4) % 32) / 2;
+  const int off_k = cache_code_off(DH, 0, kblk, hh) + kbyte, off_ks = cache_scale_off(DH, 0, kblk, hh);
+  const int vblk = DH == 128 ? g : DH == 64 ? g & 1 : 0;
+  const int vpage = DH == 128 ? 0 : DH == 64 ? g >> 1 : g & 1;            // (dh 128: both pages, one after the other)
+  const int off_v = cache_code_off(DH, 1, vblk, hh), off_vs = cache_scale_off(DH, 1, vblk, hh);
+  constexpr int R = 2;                                // tiles in flight
+  kraw_t kr[R][2];
+  uint4 vr[R][NV];
+  unsigned ks[R][2], vs[R][NV];
+  auto request = [&](int u, int i) {
+    const int tile = min(wave + i * CA_WAVES, n_tiles - 1);
+    const unsigned char* base[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int pl = __builtin_amdgcn_readfirstlane(min(2 * tile + p, n_pages - 1));
+      int page = __builtin_amdgcn_readlane(my_page[0], pl & 63);
+#pragma unroll
+      for (int q = 1; q < CA_MOST / 1024; ++q)
+        if ((pl >> 6) == q) page = __builtin_amdgcn_readlane(my_page[q], pl & 63);
+      base[p] = a.pool + ((size_t)page * a.Hkv + kvh) * cache_block_bytes(DH);
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      kr[u][p] = *reinterpret_cast<const kraw_t*>(base[p] + off_k);
+      if constexpr (DH == 128) {
+        vr[u][p] = *reinterpret_cast<const uint4*>(base[p] + off_v);
+        ks[u][p] = *reinterpret_cast<const unsigned short*>(base[p] + off_ks);       // key's and value's scale
+      } else {
+        ks[u][p] = base[p][off_ks];
+      }
+    }
+    if constexpr (DH != 128) {
+      const unsigned char* vb = vpage ? base[1] : base[0];
+      vr[u][0] = *reinterpret_cast<const uint4*>(vb + off_v);
+      vs[u][0] = vb[off_vs];
+    }
+  };
+  const int cnt = n_tiles > wave ? (n_tiles - wave + CA_WAVES - 1) / CA_WAVES : 0;
+#pragma unroll
+  for (int u = 0; u < R; ++u)
+    if (u < cnt) request(u, u);
+
+  // queries, and the tokens that each column sees
+  bf16x8 qf[CT][KC];
+  int vis[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int col = ct * 16 + hh, i = col / G, h = col - i * G;
+    const bool used = i < nq;
+    vis[ct] = used ? len - count + i + 1 : 0;
+    const bf16_t* q = a.q + (first + (used ? i : 0)) * a.q_row + (kvh * G + h) * a.q_head + g * (DH / 4);
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      const bf16x8 v = *reinterpret_cast<const bf16x8*>(q + 8 * c);
+      qf[ct][c] = used ? v : bf16x8{};
+    }
+  }
+  const int vis_min = len - count + 1;                // what the sequence's first row sees
+  float m_run[CT], l_run[CT];
+  unsigned poison[CT];                                // bit: this column sees a NaN among the values of that block
+  f32x4 oacc[CT][DT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    m_run[ct] = -INFINITY; l_run[ct] = 0.f; poison[ct] = bad ? 15u : 0u;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) oacc[ct][d] = f32x4{};
+  }
+  bf16_t* vl = reinterpret_cast<bf16_t*>(lds[wave]);
+
+  auto compute = [&](int u, int i) {
+    const int t0 = t_begin + (wave + i * CA_WAVES) * 32;
+    // values into LDS: zeros behind the context's end (what lies there is anything) and for blocks of NaN, which would reach
+    // columns that do not see them; the columns that do are marked
+#pragma unroll
+    for (int p = 0; p < NV; ++p) {
+      __builtin_amdgcn_sched_barrier(0);
+      const int row = (DH == 128 ? p : vpage) * 16 + hh;
+      uint4 c = vr[u][p];
+      unsigned e = DH == 128 ? ks[u][p] >> 8 : vs[u][p];
+      if (t0 + 32 > len && t0 + row >= len) { c = uint4{0, 0, 0, 0}; e = 127; }
+      const unsigned long long nan = __ballot(e == 255);
+      if (nan) {
+        if (e == 255) { c = uint4{0, 0, 0, 0}; e = 127; }
+        int g4 = 4 * g;
+        asm volatile("" : "+v"(g4));                   // (nothing of this is to be computed ahead, in registers of the loop)
+#pragma clang loop unroll(disable)
+        for (int j = 0; j < 4; ++j)
+#pragma clang loop unroll(disable)
+          for (int pg = DH == 128 ? p : 0; pg < (DH == 128 ? p + 1 : 2); ++pg)
+#pragma clang loop unroll(disable)
+            for (int blk = 0; blk < KC; ++blk) {
+              const int at = g4 + j + 16 * (DH == 128 ? blk : pg * KC + blk), t = t0 + pg * 16 + g4 + j;
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct)
+                if ((nan >> at & 1) && t < vis[ct]) poison[ct] |= 1u << blk;
+            }
+      }
+      if (DH > 32 || g < 2) {
+        bf16_t* to = vl + row * VS + vblk * 32;
+        *reinterpret_cast<bf16x8*>(to) = cache_open(c.x, e);
+        *reinterpret_cast<bf16x8*>(to + 8) = cache_open(c.y, e);
+        *reinterpret_cast<bf16x8*>(to + 16) = cache_open(c.z, e);
+        *reinterpret_cast<bf16x8*>(to + 24) = cache_open(c.w, e);
+      }
+    }
+    f32x4 sacc[CT][2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      __builtin_amdgcn_sched_barrier(0);               // (one page's opened fragments at a time: registers)
+      const unsigned e = DH == 128 ? ks[u][p] & 255 : ks[u][p];
+      bf16x8 kf[KC];
+#pragma unroll
+      for (int c = 0; c < KC; ++c) kf[c] = cache_open(k_word<DH>(kr[u][p], c), e);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        sacc[ct][p] = f32x4{};
+#pragma unroll
+        for (int c = 0; c < KC; ++c) sacc[ct][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[c], qf[ct][c], sacc[ct][p], 0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // Softmax in base 2; the running maximum may lag by 2^8 (probabilities then reach 256, which costs no precision), so that a
+    // tile seldom needs a shuffle.  Probabilities are rounded to bf16 for the second product, their sum is not.
+    bf16x8 pf[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      float s[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] = sacc[ct][e >> 2][e & 3];
+      if (t0 + 32 > vis_min) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (t0 + (e >> 2) * 16 + 4 * g + (e & 3) >= vis[ct]) s[e] = -INFINITY;
+      }
+      float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7]))) * a.c2;
+      if (__any(mx > m_run[ct] + RESCALE)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const bool grow = mx > m_run[ct] + RESCALE;
+        const float corr = grow ? __builtin_amdgcn_exp2f(m_run[ct] - mx) : 1.0f;
+        m_run[ct] = grow ? mx : m_run[ct];
+        l_run[ct] *= corr;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) oacc[ct][d] *= corr;
+      }
+      const float m = m_run[ct] == -INFINITY ? 0.f : m_run[ct];          // nothing seen yet: exponentials of -inf
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float pe = __builtin_amdgcn_exp2f(__fmaf_rn(s[e], a.c2, -m));
+        sum[e & 1] += pe;
+        pf[ct][e] = (bf16_t)pe;
+      }
+      l_run[ct] += sum[0] + sum[1];
+    }
+    asm volatile("" ::: "memory");                     // (LDS serves a wavefront's accesses in their order)
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      if (d % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+      const bf16_t* at = vl + (4 * g + (hh >> 2)) * VS + d * 16 + 4 * (hh & 3);
+      union { bf16x4 h[2]; bf16x8 v; } vf;
+      vf.h[0] = read_transposed(at);
+      vf.h[1] = read_transposed(at + 16 * VS);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) oacc[ct][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, pf[ct], oacc[ct][d], 0, 0, 0);
+    }
+    asm volatile("" ::: "memory");
+  };
+  int i = 0;
+  for (; i + 2 * R <= cnt; i += R) {
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+      compute(u, i + u);
+      __builtin_amdgcn_sched_barrier(0);
+      request(u, i + R + u);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < 2 * R - 1; ++q)
+    if (i + q < cnt) {
+      compute(q % R, i + q);
+      if (q < R - 1 && i + q + R < cnt) request(q % R, i + q + R);
+    }
+
+  // the wavefronts meet: each publishes (m, l, O), then merges its share of the columns' outputs
+  float* mine = reinterpret_cast<float*>(lds[wave]);
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    unsigned p = poison[ct];
+    p |= __shfl_xor((int)p, 16, 64);
+    p |= __shfl_xor((int)p, 32, 64);
+    float l = l_run[ct];
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (bad) l = NAN;
+    if (g == 0) { mine[ct * 16 + hh] = m_run[ct]; mine[CT * 16 + ct * 16 + hh] = l; }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      f32x4 o = oacc[ct][d];
+      if (p >> (d / 2) & 1) o = f32x4{NAN, NAN, NAN, NAN};
+      *reinterpret_cast<f32x4*>(mine + CT * 32 + (ct * 16 + hh) * OS + d * 16 + 4 * g) = o;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int col = ct * 16 + hh, qi = col / G, h = kvh * G + col - qi * G, r = first + qi;
+    float M = -INFINITY, wgt[CA_WAVES], lsum = 0.f;
+#pragma unroll
+    for (int w = 0; w < CA_WAVES; ++w) M = fmaxf(M, reinterpret_cast<const float*>(lds[w])[col]);
+    const float Mu = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int w = 0; w < CA_WAVES; ++w) {
+      const float* p = reinterpret_cast<const float*>(lds[w]);
+      wgt[w] = __builtin_amdgcn_exp2f(p[col] - Mu);
+      lsum += wgt[w] * p[CT * 16 + col];
+    }
+    const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;
+    if (qi >= nq) continue;
+    for (int d = wave; d < DT; d += CA_WAVES) {
+      f32x4 o = f32x4{};
+#pragma unroll
+      for (int w = 0; w < CA_WAVES; ++w) o += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds[w]) + CT * 32 + col * OS + d * 16 + 4 * g) * wgt[w];
+      if (n_splits == 1) {
+        bf16x4 ob;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ob[e] = (bf16_t)(o[e] * inv);
+        *reinterpret_cast<bf16x4*>(a.out + r * a.out_row + h * a.out_head + d * 16 + 4 * g) = ob;
+      } else {
+        *reinterpret_cast<f32x4*>(part_o<DH>(a, sp.n, split, r, h) + d * 16 + 4 * g) = o;
+      }
+    }
+    if (wave == 0 && g == 0) {
+      if (n_splits > 1) *reinterpret_cast<float2*>(part_ml(a, split, r, h)) = float2{M, lsum};
+      else if (a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = lsum == 0.f ? -INFINITY : (M + log2f(lsum)) * 0.6931471805599453f;
+    }
+  }
+}
+
+// Joins the splits of the contexts that have several, in their order: a workgroup per row, 4 dimensions per thread.
+template <int DH>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheAttn a, Split sp) {
+  const int b = blockIdx.x / a.max_q, i = blockIdx.x % a.max_q;
+  const int first = a.q_start != nullptr ? a.q_start[b] : b, count = a.q_start != nullptr ? a.q_start[b + 1] - first : 1, r = first + i;
+  const int len = a.lens[b];
+  if (first < 0 || i >= count || r >= a.n_rows || len < 0 || len > a.max_len || len <= sp.chunk) return;
+  const int n_splits = (len + sp.chunk - 1) / sp.chunk;
+  for (int e = threadIdx.x; e < a.Hq * (DH / 4); e += 256) {
+    const int h = e / (DH / 4), d = 4 * (e % (DH / 4));
+    float M = -INFINITY, lsum = 0.f;
+    for (int s = 0; s < n_splits; ++s) M = fmaxf(M, part_ml(a, s, r, h)[0]);
+    const float Mu = M == -INFINITY ? 0.f : M;
+    f32x4 o = f32x4{};
+    for (int s = 0; s < n_splits; ++s) {
+      const float2 ml = *reinterpret_cast<const float2*>(part_ml(a, s, r, h));
+      const float w = __builtin_amdgcn_exp2f(ml.x - Mu);
+      lsum += w * ml.y;
+      o += *reinterpret_cast<const f32x4*>(part_o<DH>(a, sp.n, s, r, h) + d) * w;
+    }
+    const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;
+    bf16x4 ob;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) ob[q] = (bf16_t)(o[q] * inv);
+    *reinterpret_cast<bf16x4*>(a.out + r * a.out_row + h * a.out_head + d) = ob;
+    if (d == 0 && a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = lsum == 0.f ? -INFINITY : (M + log2f(lsum)) * 0.6931471805599453f;
+  }
+}
+
+// Splits of the longest context: enough workgroups to fill the chip, a wavefront at least two tiles.
+Split split_of(const CacheAttn& a) {
+  const long long groups = (long long)a.n_seqs * a.Hkv;
+  long long n = std::max<long long>((1024 + groups - 1) / std::max<long long>(groups, 1), (a.max_len + CA_MOST - 1) / CA_MOST);
+  n = std::max<long long>(1, std::min<long long>(n, (a.max_len + 255) / 256));
+  Split s;
+  s.chunk = (int)(((a.max_len + n - 1) / n + 127) / 128 * 128);
+  s.chunk = std::max(128, std::min(s.chunk, CA_MOST));
+  s.n = std::max(1, (a.max_len + s.chunk - 1) / s.chunk);
+  return s;
+}
+bool few_rows(const CacheAttn& a) { return (long long)a.max_q * (a.Hq / a.Hkv) <= 32; }
+
+template <int DH> hipError_t attention(hipStream_t st, const CacheAttn& a) {
+  if (!few_rows(a)) return launch(cache_attn_simple_kernel, dim3(a.n_seqs * a.max_q, a.Hq), dim3(64), st, a, DH);
+  const Split sp = split_of(a);
+  const dim3 grid((unsigned)a.Hkv * a.n_seqs * sp.n);
+  hipError_t e = a.max_q * (a.Hq / a.Hkv) <= 16 ? launch(cache_attn_kernel<DH, 1>, grid, dim3(64 * CA_WAVES), st, a, sp)
+                                                : launch(cache_attn_kernel<DH, 2>, grid, dim3(64 * CA_WAVES), st, a, sp);
+  if (e == hipSuccess && sp.n > 1) e = launch(cache_join_kernel<DH>, dim3(a.n_seqs * a.max_q), dim3(256), st, a, sp);
+  return e;
+}
+
+}  // namespace
+
+size_t cache_attention_workspace(const CacheAttn& a, int dh) {
+  if (!few_rows(a)) return 0;
+  const Split sp = split_of(a);
+  return sp.n > 1 ? (size_t)sp.n * a.n_rows * a.Hq * (dh + 2) * sizeof(float) : 0;
+}
 
 hipError_t launch_cache_attention(hipStream_t st, const CacheAttn& a, int dh) {
-  return launch(cache_attn_simple_kernel, dim3(a.n_seqs * a.max_q, a.Hq), dim3(64), st, a, dh);
+  return dh == 32 ? attention<32>(st, a) : dh == 64 ? attention<64>(st, a) : attention<128>(st, a);
 }
 
 }  // namespace april
