@@ -347,8 +347,8 @@ int april_cache_append(const april_cache_append_args* args);
  * 0 .. lens[b] - c + i.  (One row: a decode iteration.  As many rows as tokens: a whole prompt.)
  * n_q_heads / n_kv_heads (at most 16) consecutive query heads share a KV head.
  * A row that sees no token is 0 and its lse -infinity.  Rows of no sequence are left as they were.  A NaN in the
- * cache reaches the rows that see it; a page id outside the pool that a sequence's length covers makes its rows NaN,
- * and so does a length outside 0 .. max_len (or beyond the block table). */
+ * cache reaches the rows that see it.  A page id outside the pool makes the rows that see a token on it NaN (and
+ * may others of their sequence); a length outside 0 .. max_len, or beyond the block table, all rows of its sequence. */
 typedef struct {
   int32_t n_q_heads, n_kv_heads, head_dim;
   int32_t n_pages, n_seqs;

@@ -280,54 +280,6 @@ hipError_t launch_cache_append(hipStream_t st, const CacheAppend& a, bool f32) {
 }
 
 // ---------------------------------------------------------------------------
-// Attention, simple form: a wavefront per (row, query head), a token per trip, online softmax.
-// ---------------------------------------------------------------------------
-namespace {
-
-__device__ inline float cache_value(const unsigned char* page, int dh, int value, int tok, int d) {
-  const unsigned byte = page[cache_code_off(dh, value, d / 32, tok) + (d % 32) / 2];
-  const unsigned e = page[cache_scale_off(dh, value, d / 32, tok)];
-  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(byte, __uint_as_float(e << 23), 0);
-  return (float)p[d & 1];
-}
-
-__global__ __launch_bounds__(64) void cache_attn_simple_kernel(CacheAttn a, int dh) {
-  const int b = blockIdx.x / a.max_q, i = blockIdx.x % a.max_q, h = blockIdx.y, lane = threadIdx.x;
-  const int first = a.q_start != nullptr ? a.q_start[b] : b, c = a.q_start != nullptr ? a.q_start[b + 1] - first : 1, r = first + i;
-  if (first < 0 || i >= c || r >= a.n_rows) return;
-  const int len = a.lens[b];
-  bool bad = len < 0 || len > a.max_len;
-  const int seen = bad ? 0 : min(len, len - c + i + 1), kvh = h / (a.Hq / a.Hkv);
-  const bf16_t* q = a.q + r * a.q_row + h * a.q_head;
-  const bool has0 = lane < dh, has1 = lane + 64 < dh;
-  const float q0 = has0 ? (float)q[lane] : 0.f, q1 = has1 ? (float)q[lane + 64] : 0.f;
-  float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
-  if (!bad)
-    for (int p = 0; p * CACHE_PAGE < len; ++p) bad |= (unsigned)a.block_table[(size_t)b * a.table_stride + p] >= (unsigned)a.n_pages;
-  if (!bad)
-    for (int t = 0; t < seen; ++t) {
-      const unsigned char* page = a.pool + ((size_t)a.block_table[(size_t)b * a.table_stride + t / CACHE_PAGE] * a.Hkv + kvh) * cache_block_bytes(dh);
-      float part = 0.f;
-      if (has0) part += q0 * cache_value(page, dh, 0, t % CACHE_PAGE, lane);
-      if (has1) part += q1 * cache_value(page, dh, 0, t % CACHE_PAGE, lane + 64);
-      for (int d = 32; d; d >>= 1) part += __shfl_xor(part, d, 64);
-      const float s = part * a.c2, m_new = fmaxf(m, s);
-      const float corr = m == -INFINITY ? 0.f : exp2f(m - m_new), w = exp2f(s - m_new);
-      l = l * corr + w;
-      o0 = o0 * corr + w * (has0 ? cache_value(page, dh, 1, t % CACHE_PAGE, lane) : 0.f);
-      o1 = o1 * corr + w * (has1 ? cache_value(page, dh, 1, t % CACHE_PAGE, lane + 64) : 0.f);
-      m = m_new;
-    }
-  const float inv = bad ? NAN : (l == 0.f ? 0.f : 1.0f / l);
-  bf16_t* out = a.out + r * a.out_row + h * a.out_head;
-  if (has0) out[lane] = (bf16_t)(o0 * inv);
-  if (has1) out[lane + 64] = (bf16_t)(o1 * inv);
-  if (a.lse != nullptr && lane == 0) a.lse[(size_t)r * a.Hq + h] = bad ? NAN : (l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f);
-}
-
-}  // namespace
-
-// ---------------------------------------------------------------------------
 // Attention of few rows: one workgroup (4 wavefronts) per (sequence, KV head, split of the context), up to 16 CT columns
 // (row of the sequence, query head of the KV head).  The wavefronts take the split's tiles of 32 tokens in turn, each with an online
 // softmax in registers; they meet in LDS, the splits of a context in a second small kernel, both in a fixed order.
@@ -397,7 +349,6 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
   const int len = bad ? 0 : len_raw;
   const int t_begin = split * sp.chunk;
   if (split > 0 && t_begin >= len) return;
-  const int n_splits = max(1, (len + sp.chunk - 1) / sp.chunk);
   const int t_end = min(len, t_begin + sp.chunk), n_tiles = (t_end - t_begin + 31) >> 5, n_pages = (t_end - t_begin + 15) >> 4;
 
   // page ids of the split, one per lane and register; ids outside the pool are noticed and not followed
@@ -632,12 +583,13 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
       lsum += wgt[w] * p[CT * 16 + col];
     }
     const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;
-    if (qi >= nq) continue;
+    if (qi >= nq || (split > 0 && vis[ct] <= t_begin)) continue;
+    const bool whole = vis[ct] <= sp.chunk;            // the row's tokens are all in the first split
     for (int d = wave; d < DT; d += CA_WAVES) {
       f32x4 o = f32x4{};
 #pragma unroll
       for (int w = 0; w < CA_WAVES; ++w) o += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds[w]) + CT * 32 + col * OS + d * 16 + 4 * g) * wgt[w];
-      if (n_splits == 1) {
+      if (whole) {
         bf16x4 ob;
 #pragma unroll
         for (int e = 0; e < 4; ++e) ob[e] = (bf16_t)(o[e] * inv);
@@ -647,20 +599,20 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
       }
     }
     if (wave == 0 && g == 0) {
-      if (n_splits > 1) *reinterpret_cast<float2*>(part_ml(a, split, r, h)) = float2{M, lsum};
+      if (!whole) *reinterpret_cast<float2*>(part_ml(a, split, r, h)) = float2{M, lsum};
       else if (a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = lsum == 0.f ? -INFINITY : (M + log2f(lsum)) * 0.6931471805599453f;
     }
   }
 }
 
-// Joins the splits of the contexts that have several, in their order: a workgroup per row, 4 dimensions per thread.
+// Joins the splits of the rows that see tokens of several, in their order: a workgroup per row, 4 dimensions per thread.
 template <int DH>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttn a, Split sp) {
   const int b = blockIdx.x / a.max_q, i = blockIdx.x % a.max_q;
   const int first = a.q_start != nullptr ? a.q_start[b] : b, count = a.q_start != nullptr ? a.q_start[b + 1] - first : 1, r = first + i;
   const int len = a.lens[b];
-  if (first < 0 || i >= count || r >= a.n_rows || len < 0 || len > a.max_len || len <= sp.chunk) return;
-  const int n_splits = (len + sp.chunk - 1) / sp.chunk;
+  if (first < 0 || i >= count || r >= a.n_rows || len < 0 || len > a.max_len || len - count + i + 1 <= sp.chunk) return;
+  const int n_splits = (len - count + i + sp.chunk) / sp.chunk;
   for (int e = threadIdx.x; e < a.Hq * (DH / 4); e += 256) {
     const int h = e / (DH / 4), d = 4 * (e % (DH / 4));
     float M = -INFINITY, lsum = 0.f;
@@ -682,25 +634,281 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttn a, Split sp) 
   }
 }
 
-// Splits of the longest context: enough workgroups to fill the chip, a wavefront at least two tiles.
+// ---------------------------------------------------------------------------
+// Attention of many rows: a workgroup (4 wavefronts) owns 256 columns (row, query head) of one (sequence, KV head) and walks over
+// the tokens that they see in stages of 64: each block of 32 codes is opened to bf16 once per workgroup, into LDS, and serves all
+// of its columns.  A wavefront takes 64 columns, two tiles of v_mfma_f32_32x32x16_bf16, transposed products as above:
+//   S^T[token, column] = K . Q^T,  O^T[dim, column] = V^T . P^T;
+// the accumulators of the first, rounded to bf16 in place, are the operand of the second, whose V fragment is read transposed.
+// Two stage buffers: while one is worked on, the codes of the next are opened into the other and those of the one behind it
+// requested.  Rows of LDS are not padded; their 16-byte units are permuted by row so that neither the
+// writes (16 tokens of one unit) nor the reads (16 tokens of a unit; 4 tokens of 4 units) meet on a bank.
+// ---------------------------------------------------------------------------
+constexpr int RA_STAGE = 64, RA_COLS = 256;
+
+template <int DH> __device__ inline int k_unit(int row, int u) { return u ^ ((row / (128 / DH)) & (DH / 8 - 1)); }
+template <int DH> __device__ inline int v_unit(int row, int u) { return u ^ (4 * ((row / (128 / DH)) & (DH / 32 - 1))) ^ ((row >> 2) & 3); }
+
+template <int DH>
+__global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Split sp, int n_qt) {
+  constexpr int KC = DH / 16, DT = DH / 32, CT = 2, NB = DH / 32, NV = DH == 128 ? 2 : 1;
+  constexpr float RESCALE = 8.0f;
+  __shared__ bf16x8 lds[2][2][RA_STAGE * DH / 8];            // [buffer][keys | values][token][16-byte unit]
+  __shared__ unsigned long long s_nan[2][4];                 // blocks of NaN among the values, one bit per block that a wavefront opens
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cl = lane & 31, hf = lane >> 5, hh = lane & 15, g = lane >> 4;
+  const int G = a.Hq / a.Hkv;
+  // KV heads first (different XCDs), the tiles with the most tokens before the others, splits last
+  const int kvh = (int)(blockIdx.x % a.Hkv);
+  int rest = (int)(blockIdx.x / a.Hkv);
+  const int b = rest % a.n_seqs;
+  rest /= a.n_seqs;
+  const int qt = n_qt - 1 - rest % n_qt, split = rest / n_qt;
+  const int first = a.q_start != nullptr ? a.q_start[b] : b, count = a.q_start != nullptr ? a.q_start[b + 1] - first : 1;
+  const int len_raw = a.lens[b];
+  if (first < 0 || count <= 0 || first >= a.n_rows) return;
+  const int nq = min(min(count, a.max_q), a.n_rows - first), n_cols = nq * G, col0 = qt * RA_COLS;
+  if (col0 >= n_cols) return;
+  bool bad = len_raw < 0 || len_raw > a.max_len;
+  const int len = bad ? 0 : len_raw;
+  const int t_begin = split * sp.chunk;
+  const int seen = max(0, len - count + min(n_cols - 1, col0 + RA_COLS - 1) / G + 1);       // by the workgroup's last column
+  if (split > 0 && t_begin >= seen) return;
+  const int t_end = min(seen, t_begin + sp.chunk), n_stages = max(0, t_end - t_begin + RA_STAGE - 1) / RA_STAGE;
+  const int last_page = max(0, t_end - 1) / CACHE_PAGE - t_begin / CACHE_PAGE;
+  const int* bt = a.block_table + (size_t)b * a.table_stride + t_begin / CACHE_PAGE;
+
+  // what this thread opens of a stage
+  const int my_pg = DH == 128 ? wave : DH == 64 ? 2 * (wave & 1) + (g >> 1) : g, my_blk = DH == 128 ? g : DH == 64 ? g & 1 : 0;
+  const int my_row = my_pg * CACHE_PAGE + hh;
+  const bool opens = DH > 32 || wave < 2;
+  int my_page = 0;                                   // page ids of 16 stages, one per lane
+  uint4 code[NV];
+  unsigned scale = 127;                              // (dh 128: of the key and, above it, of the value)
+  auto request = [&](int st) {
+    if ((st & 15) == 0) {
+      const int i = st * 4 + lane;
+      my_page = bt[i < last_page ? i : last_page];
+      const bool out = (unsigned)my_page >= (unsigned)a.n_pages;
+      bad |= __any(out);
+      if (out) my_page = 0;
+    }
+    const int i = st * 4 + my_pg;
+    const int page = __shfl(my_page, (i < last_page ? i : last_page) & 63, 64);
+    if (!opens) return;
+    const unsigned char* blk = a.pool + ((size_t)page * a.Hkv + kvh) * cache_block_bytes(DH);
+    if constexpr (DH == 128) {
+#pragma unroll
+      for (int p = 0; p < NV; ++p) code[p] = *reinterpret_cast<const uint4*>(blk + cache_code_off(DH, p, my_blk, hh));
+      scale = *reinterpret_cast<const unsigned short*>(blk + cache_scale_off(DH, 0, my_blk, hh));
+    } else {
+      const int value = DH == 64 ? wave >> 1 : wave;
+      code[0] = *reinterpret_cast<const uint4*>(blk + cache_code_off(DH, value, my_blk, hh));
+      scale = blk[cache_scale_off(DH, value, my_blk, hh)];
+    }
+  };
+  auto open = [&](int st) {
+    const int buf = st & 1;
+#pragma unroll
+    for (int p = 0; p < NV; ++p) {
+      const int value = DH == 128 ? p : DH == 64 ? wave >> 1 : wave;
+      uint4 c = code[p];
+      unsigned e = DH == 128 ? (p ? scale >> 8 : scale & 255) : scale;
+      if (value == 1) {
+        // zeros behind the context's end, where anything may lie, and for blocks of NaN: the columns that see them are marked
+        if (t_begin + st * RA_STAGE + my_row >= len) { c = uint4{0, 0, 0, 0}; e = 127; }
+        const unsigned long long nan = __ballot(opens && e == 255);
+        if (e == 255) { c = uint4{0, 0, 0, 0}; e = 127; }
+        if (lane == 0) s_nan[buf][wave] = nan;
+      }
+      if (!opens) continue;
+      bf16x8* to = &lds[buf][value][my_row * (DH / 8)];
+      const unsigned w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int u = my_blk * 4 + j;
+        to[value ? v_unit<DH>(my_row, u) : k_unit<DH>(my_row, u)] = cache_open(w[j], e);
+      }
+    }
+  };
+  if (n_stages > 0) request(0);
+
+  // queries: column cl of tile ct; lane half hf holds dims 16 c + 8 hf .. + 7
+  bf16x8 qf[CT][KC];
+  int vis[CT], vis_first[CT], row[CT], head[CT];
+  bool used[CT];
+  int wave_seen = 0;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int c0 = col0 + wave * 64 + ct * 32, col = c0 + cl, i = col / G;
+    used[ct] = col < n_cols;
+    row[ct] = first + (used[ct] ? i : 0);
+    head[ct] = kvh * G + (col - i * G);
+    vis[ct] = used[ct] ? len - count + i + 1 : 0;
+    vis_first[ct] = len - count + c0 / G + 1;
+    if (c0 < n_cols) wave_seen = max(wave_seen, len - count + min(n_cols - 1, c0 + 31) / G + 1);
+    const bf16_t* q = a.q + row[ct] * a.q_row + head[ct] * a.q_head + 8 * hf;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      const bf16x8 v = *reinterpret_cast<const bf16x8*>(q + 16 * c);
+      qf[ct][c] = used[ct] ? v : bf16x8{};
+    }
+  }
+  float m_run[CT], l_run[CT];
+  unsigned poison[CT];
+  f32x16 oacc[CT][DT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    m_run[ct] = -INFINITY; l_run[ct] = 0.f; poison[ct] = 0;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) oacc[ct][d] = f32x16{};
+  }
+  if (n_stages > 0) open(0);
+  if (n_stages > 1) request(1);
+  __syncthreads();
+
+  for (int st = 0; st < n_stages; ++st) {
+    if (st + 1 < n_stages) open(st + 1);
+    if (st + 2 < n_stages) request(st + 2);
+    const int buf = st & 1, ts = t_begin + st * RA_STAGE;
+#pragma unroll
+    for (int half = 0; half < RA_STAGE / 32; ++half) {
+      const int t0 = ts + half * 32;
+      if (t0 >= wave_seen) continue;
+      f32x16 sacc[CT];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) sacc[ct] = f32x16{};
+      const bf16x8* kl = &lds[buf][0][(half * 32 + cl) * (DH / 8)];
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        const bf16x8 kf = kl[k_unit<DH>(half * 32 + cl, 2 * c + hf)];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) sacc[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ct][c], sacc[ct], 0, 0, 0);
+      }
+      bf16x8 pf[CT][2];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        if (t0 + 32 > vis_first[ct]) {               // some column of the tile does not see all 32 tokens
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (t0 + 8 * (i >> 2) + 4 * hf + (i & 3) >= vis[ct]) sacc[ct][i] = -INFINITY;
+        }
+        float mx = sacc[ct][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sacc[ct][i]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.c2;
+        const bool grow = mx > m_run[ct] + RESCALE;
+        if (__any(grow)) {
+          const float corr = grow ? __builtin_amdgcn_exp2f(m_run[ct] - mx) : 1.0f;
+          m_run[ct] = grow ? mx : m_run[ct];
+          l_run[ct] *= corr;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) oacc[ct][d] *= corr;
+        }
+        const float m = m_run[ct] == -INFINITY ? 0.f : m_run[ct];
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float pe = __builtin_amdgcn_exp2f(__fmaf_rn(sacc[ct][i], a.c2, -m));
+          sum[i & 1] += pe;
+          pf[ct][i >> 3][i & 7] = (bf16_t)pe;
+        }
+        l_run[ct] += sum[0] + sum[1];
+      }
+      const bf16_t* vl = reinterpret_cast<const bf16_t*>(&lds[buf][1][0]);
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          union { bf16x4 h[2]; bf16x8 v; } vf;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int r = half * 32 + k * 16 + j * 8 + 4 * hf + (hh >> 2);
+            vf.h[j] = read_transposed(vl + r * DH + v_unit<DH>(r, d * 4 + 2 * (g & 1) + ((hh & 3) >> 1)) * 8 + 4 * (hh & 1));
+          }
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) oacc[ct][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[ct][k], oacc[ct][d], 0, 0, 0);
+        }
+    }
+    unsigned long long nan = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) nan |= (DH == 32 && w != 1) || (DH == 64 && w < 2) ? 0 : s_nan[buf][w];
+    if (__builtin_amdgcn_readfirstlane((int)(nan | nan >> 32))) {
+      int half4 = 4 * hf;
+      asm volatile("" : "+v"(half4));
+#pragma clang loop unroll(disable)
+      for (int j = 0; j < 32; ++j) {                 // this lane's tokens of the stage
+        const int tok = 8 * (j >> 2) + half4 + (j & 3), pg = tok >> 4;
+        const unsigned long long m = DH == 128 ? s_nan[buf][pg] : DH == 64 ? s_nan[buf][2 + (pg >> 1)] >> (32 * (pg & 1)) : s_nan[buf][1] >> (16 * pg);
+#pragma clang loop unroll(disable)
+        for (int blk = 0; blk < NB; ++blk)
+          if (m >> (16 * blk + (tok & 15)) & 1) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+              if (ts + tok < vis[ct]) poison[ct] |= 1u << blk;
+          }
+      }
+    }
+    __syncthreads();
+  }
+
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    unsigned p = poison[ct] | (unsigned)__shfl_xor((int)poison[ct], 32, 64);
+    float l = l_run[ct] + __shfl_xor(l_run[ct], 32, 64);
+    if (bad) { l = NAN; p = 15; }
+    if (!used[ct] || (split > 0 && vis[ct] <= t_begin)) continue;
+    const bool whole = vis[ct] <= sp.chunk;
+    const int r = row[ct], h = head[ct];
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int dim = d * 32 + 8 * q + 4 * hf;
+        f32x4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = p >> d & 1 ? NAN : oacc[ct][d][4 * q + e];
+        if (whole) {
+          bf16x4 ob;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) ob[e] = (bf16_t)(o[e] * inv);
+          *reinterpret_cast<bf16x4*>(a.out + r * a.out_row + h * a.out_head + dim) = ob;
+        } else {
+          *reinterpret_cast<f32x4*>(part_o<DH>(a, sp.n, split, r, h) + dim) = o;
+        }
+      }
+    if (hf == 0) {
+      if (!whole) *reinterpret_cast<float2*>(part_ml(a, split, r, h)) = float2{m_run[ct], l};
+      else if (a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = l == 0.f ? -INFINITY : (m_run[ct] + log2f(l)) * 0.6931471805599453f;
+    }
+  }
+}
+
+bool few_rows(const CacheAttn& a) { return (long long)a.max_q * (a.Hq / a.Hkv) <= 32; }
+int row_tiles(const CacheAttn& a) { return (int)(((long long)a.max_q * (a.Hq / a.Hkv) + RA_COLS - 1) / RA_COLS); }
+
+// Splits of the longest context: enough workgroups to fill the chip; of few rows a wavefront has at least two tiles, of
+// many rows a workgroup 8 stages.
 Split split_of(const CacheAttn& a) {
-  const long long groups = (long long)a.n_seqs * a.Hkv;
-  long long n = std::max<long long>((1024 + groups - 1) / std::max<long long>(groups, 1), (a.max_len + CA_MOST - 1) / CA_MOST);
-  n = std::max<long long>(1, std::min<long long>(n, (a.max_len + 255) / 256));
+  const bool few = few_rows(a);
+  const long long groups = std::max<long long>(1, (long long)a.n_seqs * a.Hkv * (few ? 1 : row_tiles(a)));
+  long long n = ((few ? 1024 : 256) + groups - 1) / groups;
+  if (few) n = std::max<long long>(n, (a.max_len + CA_MOST - 1) / CA_MOST);
+  n = std::max<long long>(1, std::min<long long>(n, (a.max_len + (few ? 255 : 511)) / (few ? 256 : 512)));
   Split s;
-  s.chunk = (int)(((a.max_len + n - 1) / n + 127) / 128 * 128);
-  s.chunk = std::max(128, std::min(s.chunk, CA_MOST));
+  s.chunk = (int)std::max<long long>(128, ((a.max_len + n - 1) / n + 127) / 128 * 128);
+  if (few) s.chunk = std::min(s.chunk, CA_MOST);
   s.n = std::max(1, (a.max_len + s.chunk - 1) / s.chunk);
   return s;
 }
-bool few_rows(const CacheAttn& a) { return (long long)a.max_q * (a.Hq / a.Hkv) <= 32; }
 
 template <int DH> hipError_t attention(hipStream_t st, const CacheAttn& a) {
-  if (!few_rows(a)) return launch(cache_attn_simple_kernel, dim3(a.n_seqs * a.max_q, a.Hq), dim3(64), st, a, DH);
   const Split sp = split_of(a);
-  const dim3 grid((unsigned)a.Hkv * a.n_seqs * sp.n);
-  hipError_t e = a.max_q * (a.Hq / a.Hkv) <= 16 ? launch(cache_attn_kernel<DH, 1>, grid, dim3(64 * CA_WAVES), st, a, sp)
-                                                : launch(cache_attn_kernel<DH, 2>, grid, dim3(64 * CA_WAVES), st, a, sp);
+  const int n_qt = row_tiles(a);
+  const dim3 grid((unsigned)a.Hkv * a.n_seqs * sp.n * (few_rows(a) ? 1 : n_qt));
+  hipError_t e = !few_rows(a) ? launch(cache_attn_rows_kernel<DH>, grid, dim3(256), st, a, sp, n_qt)
+                 : a.max_q * (a.Hq / a.Hkv) <= 16 ? launch(cache_attn_kernel<DH, 1>, grid, dim3(64 * CA_WAVES), st, a, sp)
+                                                  : launch(cache_attn_kernel<DH, 2>, grid, dim3(64 * CA_WAVES), st, a, sp);
   if (e == hipSuccess && sp.n > 1) e = launch(cache_join_kernel<DH>, dim3(a.n_seqs * a.max_q), dim3(256), st, a, sp);
   return e;
 }
@@ -708,7 +916,6 @@ template <int DH> hipError_t attention(hipStream_t st, const CacheAttn& a) {
 }  // namespace
 
 size_t cache_attention_workspace(const CacheAttn& a, int dh) {
-  if (!few_rows(a)) return 0;
   const Split sp = split_of(a);
   return sp.n > 1 ? (size_t)sp.n * a.n_rows * a.Hq * (dh + 2) * sizeof(float) : 0;
 }
