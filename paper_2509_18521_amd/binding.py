@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass, field
 from typing import Dict, List, NamedTuple, Optional, Sequence
 
@@ -112,7 +113,23 @@ class april_cache_attention_args(C.Structure):
         ("workspace_bytes", C.c_int64), ("stream", C.c_void_p)]
 
 
+# The same structs as bytes: packing them is a third of the time of filling a ctypes structure.
+_PACK_EXTEND = struct.Struct("4iq12Q").pack
+_PACK_APPEND = struct.Struct("6i4q7Q").pack
+_PACK_ATTENTION = struct.Struct("9if5q8QqQ").pack
+
 _lib = None
+_calls = {}
+
+
+def _call(name):
+    """A library function that takes its struct as bytes."""
+    f = _calls.get(name)
+    if f is None:
+        f = load_library()[name]
+        f.argtypes, f.restype = [C.c_char_p], C.c_int64 if name.endswith("workspace") else C.c_int
+        _calls[name] = f
+    return f
 
 
 def load_library():
@@ -401,8 +418,7 @@ def april_get_info(ctx) -> dict:
 
 
 # ---------------------------------------------------------------------------
-# Operators of the 4-bit KV cache, on torch tensors of one GPU (any object with their data_ptr, stride, shape, dtype and
-# device would do).  They are enqueued on torch's current stream of the tensors' device and return at once; what they
+# Operators of the 4-bit KV cache, on torch tensors of one GPU.  They are enqueued on torch's current stream of the tensors' device and return at once; what they
 # allocate (results that were not handed in, attention's workspace) comes from torch on that stream, so they may be
 # captured into a graph.
 # ---------------------------------------------------------------------------
@@ -416,57 +432,89 @@ class CacheTables(NamedTuple):
     status: object
 
 
+_torch = None               # imported by the first of these calls (the engine's calls need none)
+
+
+def _need_torch():
+    global _torch
+    import torch
+    _torch = torch
+
+
 def _refuse(text, *args):
     raise AprilError(APRIL_EINVAL, text % args if args else text)
 
 
-def _want(name, t, dtype, shape, device, strided=False):
-    """t's data pointer, or a refusal: another type, shape (None: any) or device, or not contiguous where it has to be."""
-    if str(t.dtype) != dtype:
+def _refuse_tensor(name, t, dtype, shape, dev, contiguous):
+    if t.dtype is not dtype:
         _refuse("%s: %s wanted, not %s", name, dtype, t.dtype)
-    if len(t.shape) != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
-        _refuse("%s: shape %s wanted, not %s", name, shape, tuple(t.shape))
-    if t.device != device:
-        _refuse("%s is on %s, not on %s", name, t.device, device)
-    if not strided and not t.is_contiguous():
-        _refuse("%s has to be contiguous", name)
+    if t.shape != shape:
+        _refuse("%s: shape %s wanted, not %s", name, tuple(shape), tuple(t.shape))
+    if t.get_device() != dev:
+        _refuse("%s is on %s, not on GPU %d", name, t.device, dev)
+    _refuse("%s has to be contiguous" if contiguous else "%s: the dimensions of a head have to be adjacent", name)
+
+
+def _ptr(name, t, dtype, shape, dev):
+    """Pointer of a contiguous tensor of that type and shape on GPU `dev`, or a refusal.  (One test: a call is a few microseconds.)"""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _refuse_tensor(name, t, dtype, shape, dev, True)
     return t.data_ptr()
 
 
-def _table(t, device):
-    """(pointer, rows, columns, stride) of a block table; its rows may lie apart."""
-    p = _want("block_table", t, "torch.int32", (None, None), device, True)
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+def _rows(name, t, dtype, shape, dev):
+    """(pointer, strides of rows and heads) of a tensor [rows][heads][head_dim] whose heads may lie apart."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        _refuse_tensor(name, t, dtype, shape, dev, False)
+    row, head, dim = t.stride()
+    if dim != 1:
+        _refuse_tensor(name, t, dtype, shape, dev, False)
+    return t.data_ptr(), row, head
+
+
+def _table(t, rows, dev):
+    """(pointer, columns, stride) of a block table; its rows may lie apart."""
+    if len(t.shape) != 2 or t.shape[0] != rows:
+        _refuse("block_table: %d rows wanted, not %s", rows, tuple(t.shape))
+    cols, stride = t.shape[1], t.stride()
+    if stride[1] != 1 and cols > 1:
         _refuse("block_table: the pages of a sequence have to be adjacent")
-    return p, rows, cols, max(t.stride(0), cols) if rows == 1 else t.stride(0)
+    if t.dtype is not _torch.int32 or t.get_device() != dev:
+        _refuse_tensor("block_table", t, _torch.int32, t.shape, dev, True)
+    return t.data_ptr(), cols, max(stride[0], cols) if rows == 1 else stride[0]
+
+
+def _gpu(name, t):
+    dev = t.get_device()
+    if dev < 0:
+        _refuse("%s is on %s, not on a GPU", name, t.device)
+    return dev
 
 
 def _pool(pool):
-    if pool.device.type != "cuda":
-        _refuse("the pool is on %s, not on a GPU", pool.device)
-    p = _want("pool", pool, "torch.uint8", (None, None, None), pool.device)
-    if pool.shape[2] not in (544, 1088, 2176):
-        _refuse("pool: blocks of %d bytes, not 17 * head_dim for a head_dim of 32, 64 or 128", pool.shape[2])
-    return p, pool.shape[0], pool.shape[1], pool.shape[2] // 17, pool.device
+    """(pointer, pages, KV heads, head_dim, GPU)."""
+    if _torch is None:
+        _need_torch()
+    if len(pool.shape) != 3 or pool.shape[2] not in (544, 1088, 2176):
+        _refuse("pool: [pages][KV heads][17 * head_dim] wanted for a head_dim of 32, 64 or 128, not %s", tuple(pool.shape))
+    dev = _gpu("pool", pool)
+    pages, heads, size = pool.shape
+    return _ptr("pool", pool, _torch.uint8, pool.shape, dev), pages, heads, size // 17, dev
 
 
-def _strided(name, t):
-    """Strides of rows and heads; the dimensions of a head have to be adjacent."""
-    if t.stride(2) != 1 and t.shape[2] > 1:
-        _refuse("%s: the dimensions of a head have to be adjacent", name)
-    return t.stride(0), t.stride(1)
+def _bytes(pack, *fields):
+    try:
+        return pack(*fields)
+    except struct.error as e:
+        _refuse("an argument is outside its type's range: %s", e)
 
 
-def _enqueue(call, args, device):
-    """Call with the stream that torch works on for `device`, the device being the current one meanwhile."""
-    import torch
-    if torch.cuda.current_device() == device.index:
-        args.stream = torch.cuda.current_stream().cuda_stream
-        return _check(None, call(C.byref(args)))
-    with torch.cuda.device(device):
-        args.stream = torch.cuda.current_stream().cuda_stream
-        return _check(None, call(C.byref(args)))
+def _enqueue(call, dev, pack, *fields):
+    """Call with the fields' struct, the stream that torch works on for GPU `dev` last; that GPU is the current one meanwhile."""
+    if _torch.cuda.current_device() == dev:
+        return _check(None, call(_bytes(pack, *fields, _torch._C._cuda_getCurrentRawStream(dev))))
+    with _torch.cuda.device(dev):
+        return _check(None, call(_bytes(pack, *fields, _torch._C._cuda_getCurrentRawStream(dev))))
 
 
 def april_cache_block_bytes(head_dim: int) -> int:
@@ -475,8 +523,9 @@ def april_cache_block_bytes(head_dim: int) -> int:
 
 def make_cache_pool(n_pages: int, n_kv_heads: int, head_dim: int, device="cuda"):
     """A pool of n_pages pages of 16 tokens, uninitialised: nothing reads what has not been stored."""
-    import torch
-    return torch.empty((n_pages, n_kv_heads, april_cache_block_bytes(head_dim)), dtype=torch.uint8, device=device)
+    if _torch is None:
+        _need_torch()
+    return _torch.empty((n_pages, n_kv_heads, april_cache_block_bytes(head_dim)), dtype=_torch.uint8, device=device)
 
 
 def april_cache_extend(lens, new_lens, block_table, free_pages, free_top, n_rows: int, out: Optional[Sequence] = None) -> CacheTables:
@@ -486,25 +535,23 @@ def april_cache_extend(lens, new_lens, block_table, free_pages, free_top, n_rows
     free_pages.  out: an earlier call's result (or six tensors in its order) to write into; its lens and free_top may be
     the arguments themselves.
     """
-    import torch
-    dev = lens.device
-    if dev.type != "cuda":
-        _refuse("lens is on %s, not on a GPU", dev)
-    n = lens.shape[0] if lens.dim() == 1 else _refuse("lens: one dimension wanted")
-    table, rows, cols, stride = _table(block_table, dev)
-    if rows != n:
-        _refuse("block_table: %d rows for %d sequences", rows, n)
+    if _torch is None:
+        _need_torch()
+    i32 = _torch.int32
+    dev = _gpu("lens", lens)
+    if len(lens.shape) != 1 or len(free_pages.shape) != 1:
+        _refuse("lens and free_pages: one dimension wanted")
+    n, n_pages = lens.shape[0], free_pages.shape[0]
+    table, cols, stride = _table(block_table, n, dev)
     if out is None:
-        e = lambda *s, t=torch.int32: torch.empty(s, dtype=t, device=dev)  # noqa: E731
-        out = CacheTables(e(n), e(1), e(n + 1), e(n_rows, t=torch.int64), e(n_rows), e(1))
-    i32, o = "torch.int32", out
-    args = april_cache_extend_args(
-        n, cols, free_pages.shape[0], n_rows, stride, _want("lens", lens, i32, (n,), dev), _want("new_lens", new_lens, i32, (n,), dev),
-        _want("free_top", free_top, i32, (1,), dev), table, _want("free_pages", free_pages, i32, (None,), dev),
-        _want("out.lens", o[0], i32, (n,), dev), _want("out.free_top", o[1], i32, (1,), dev), _want("out.q_start", o[2], i32, (n + 1,), dev),
-        _want("out.slot_map", o[3], "torch.int64", (n_rows,), dev), _want("out.positions", o[4], i32, (n_rows,), dev),
-        _want("out.status", o[5], i32, (1,), dev))
-    _enqueue(load_library().april_cache_extend, args, dev)
+        e = lambda size, t=i32: _torch.empty(size, dtype=t, device=lens.device)  # noqa: E731
+        out = CacheTables(e(n), e(1), e(n + 1), e(n_rows, _torch.int64), e(n_rows), e(1))
+    o_lens, o_top, q_start, slots, positions, status = out
+    _enqueue(_call("april_cache_extend"), dev, _PACK_EXTEND, n, cols, n_pages, n_rows, stride, _ptr("lens", lens, i32, (n,), dev),
+             _ptr("new_lens", new_lens, i32, (n,), dev), _ptr("free_top", free_top, i32, (1,), dev), table,
+             _ptr("free_pages", free_pages, i32, (n_pages,), dev), _ptr("out.lens", o_lens, i32, (n,), dev), _ptr("out.free_top", o_top, i32, (1,), dev),
+             _ptr("out.q_start", q_start, i32, (n + 1,), dev), _ptr("out.slot_map", slots, _torch.int64, (n_rows,), dev),
+             _ptr("out.positions", positions, i32, (n_rows,), dev), _ptr("out.status", status, i32, (1,), dev))
     return out if isinstance(out, CacheTables) else CacheTables(*out)
 
 
@@ -512,48 +559,47 @@ def april_cache_append(pool, k, v, slot_map, k_values=None, v_values=None) -> No
     """Store k and v [n_rows, n_kv_heads, head_dim] (bf16 or fp32) in the pool at slot_map [n_rows] (int64); rows whose slot lies
     outside the pool are left out.  k_values, v_values: contiguous, of k's type: what the cache now stands for."""
     p, pages, heads, dh, dev = _pool(pool)
-    t = str(k.dtype)
-    if t not in ("torch.bfloat16", "torch.float32"):
+    t = k.dtype
+    if t is not _torch.bfloat16 and t is not _torch.float32:
         _refuse("k: bfloat16 or float32 wanted, not %s", t)
-    shape = (slot_map.shape[0], heads, dh)
-    args = april_cache_append_args(
-        pages, heads, dh, shape[0], APRIL_DTYPE_BF16 if t == "torch.bfloat16" else APRIL_DTYPE_FP32, 0, *_strided("k", k), *_strided("v", v),
-        _want("k", k, t, shape, dev, True), _want("v", v, t, shape, dev, True),
-        None if k_values is None else _want("k_values", k_values, t, shape, dev),
-        None if v_values is None else _want("v_values", v_values, t, shape, dev), _want("slot_map", slot_map, "torch.int64", (None,), dev), p)
-    _enqueue(load_library().april_cache_append, args, dev)
+    if len(slot_map.shape) != 1:
+        _refuse("slot_map: one dimension wanted")
+    n = slot_map.shape[0]
+    shape = (n, heads, dh)
+    kp, k_row, k_head = _rows("k", k, t, shape, dev)
+    vp, v_row, v_head = _rows("v", v, t, shape, dev)
+    _enqueue(_call("april_cache_append"), dev, _PACK_APPEND, pages, heads, dh, n, APRIL_DTYPE_BF16 if t is _torch.bfloat16 else APRIL_DTYPE_FP32, 0,
+             k_row, k_head, v_row, v_head, kp, vp, 0 if k_values is None else _ptr("k_values", k_values, t, shape, dev),
+             0 if v_values is None else _ptr("v_values", v_values, t, shape, dev), _ptr("slot_map", slot_map, _torch.int64, (n,), dev), p)
 
 
 def april_cache_attention(q, pool, block_table, lens, max_len: int, *, q_start=None, max_q: int = 1, scale: float = 0.0, out=None, lse=None,
                           workspace=None):
     """Causal attention of q [n_rows, n_q_heads, head_dim] (bf16) over the cache: rows q_start[b] .. q_start[b + 1] - 1 are the last tokens
     of sequence b (q_start None: row b).  lens [n_seqs]: tokens in the cache, those of the rows included; max_len, max_q: bounds on
-    lens and on a sequence's rows.  lse: fp32 [n_rows, n_q_heads], written if given.  Returns out (empty rows behind the
-    last sequence are left as they were; in a new `out` they are undefined)."""
-    import torch
+    lens and on a sequence's rows.  lse: fp32 [n_rows, n_q_heads], written if given.  Returns out (rows of no sequence are left as
+    they were; in a new `out` they are undefined)."""
     p, pages, heads, dh, dev = _pool(pool)
-    if q.dim() != 3:
-        _refuse("q: [rows, heads, head_dim] wanted")
-    shape, n = tuple(q.shape), lens.shape[0]
-    qp = _want("q", q, "torch.bfloat16", (None, None, dh), dev, True)
-    table, rows, cols, stride = _table(block_table, dev)
-    if rows != n:
-        _refuse("block_table: %d rows for %d sequences", rows, n)
+    bf16, i32 = _torch.bfloat16, _torch.int32
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != dh or len(lens.shape) != 1:
+        _refuse("q: [rows][heads][%d] wanted, not %s, and lens of one dimension", dh, tuple(shape))
+    n, (rows, q_heads, _) = lens.shape[0], shape
+    qp, q_row, q_head = _rows("q", q, bf16, shape, dev)
+    table, cols, stride = _table(block_table, n, dev)
     if out is None:
-        out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
-    args = april_cache_attention_args(
-        shape[1], heads, dh, pages, n, cols, shape[0], max_q, max_len, scale, stride, *_strided("q", q), *_strided("out", out),
-        qp, p, table, _want("lens", lens, "torch.int32", (n,), dev),
-        None if q_start is None else _want("q_start", q_start, "torch.int32", (n + 1,), dev), _want("out", out, "torch.bfloat16", shape, dev, True),
-        None if lse is None else _want("lse", lse, "torch.float32", shape[:2], dev))
-    lib = load_library()
-    need = _check(None, lib.april_cache_attention_workspace(C.byref(args)))
-    if need and workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    if workspace is not None:
-        args.workspace = _want("workspace", workspace, "torch.uint8", (None,), dev)
-        args.workspace_bytes = workspace.shape[0]
-    _enqueue(lib.april_cache_attention, args, dev)
+        out = _torch.empty(shape, dtype=bf16, device=q.device)
+    op, o_row, o_head = _rows("out", out, bf16, shape, dev)
+    fields = (q_heads, heads, dh, pages, n, cols, rows, max_q, max_len, scale, stride, q_row, q_head, o_row, o_head, qp, p, table,
+              _ptr("lens", lens, i32, (n,), dev), 0 if q_start is None else _ptr("q_start", q_start, i32, (n + 1,), dev), op,
+              0 if lse is None else _ptr("lse", lse, _torch.float32, (rows, q_heads), dev))
+    need = _check(None, _call("april_cache_attention_workspace")(_bytes(_PACK_ATTENTION, *fields, 0, 0, 0)))
+    if workspace is None:
+        workspace = _torch.empty(need, dtype=_torch.uint8, device=q.device) if need else None
+    elif len(workspace.shape) != 1:
+        _refuse("workspace: one dimension wanted")
+    size = 0 if workspace is None else workspace.shape[0]
+    _enqueue(_call("april_cache_attention"), dev, _PACK_ATTENTION, *fields, _ptr("workspace", workspace, _torch.uint8, (size,), dev) if size else 0, size)
     return out
 
 

@@ -95,13 +95,16 @@ int april_cache_attention(const april_cache_attention_args* a) {
   if (a->n_seqs == 0 || a->n_rows == 0) return APRIL_OK;
   if (!a->q || !a->pool || !a->block_table || !a->lens || !a->out) REFUSE("april_cache_attention: null array");
   if (!a->q_start && a->n_rows < a->n_seqs) REFUSE("april_cache_attention: fewer rows than sequences, and no q_start");
-  if (!aligned(a->q, 16) || a->q_row % 8 || a->q_head % 8 || !aligned(a->pool, 16)) REFUSE("april_cache_attention: q's heads and the pool must be 16-byte aligned");
-  if (!aligned(a->out, 8) || a->out_row % 4 || a->out_head % 4) REFUSE("april_cache_attention: out's heads must be 8-byte aligned");
+  // (a stride over a single row or head is not used)
+  const int64_t q_row = a->n_rows > 1 ? a->q_row : 0, q_head = a->n_q_heads > 1 ? a->q_head : 0, out_row = a->n_rows > 1 ? a->out_row : 0,
+                out_head = a->n_q_heads > 1 ? a->out_head : 0;
+  if (!aligned(a->q, 16) || q_row % 8 || q_head % 8 || !aligned(a->pool, 16)) REFUSE("april_cache_attention: q's heads and the pool must be 16-byte aligned");
+  if (!aligned(a->out, 8) || out_row % 4 || out_head % 4) REFUSE("april_cache_attention: out's heads must be 8-byte aligned");
   if (a->table_stride < a->max_pages && a->n_seqs > 1) REFUSE("april_cache_attention: rows of the block table overlap");
   const size_t need = cache_attention_workspace(k, a->head_dim);
   if (need > 0 && (!a->workspace || a->workspace_bytes < (int64_t)need || !aligned(a->workspace, 16)))
     REFUSE("april_cache_attention: needs %zu bytes of 16-byte aligned workspace (april_cache_attention_workspace)", need);
-  k.table_stride = a->table_stride; k.q_row = a->q_row; k.q_head = a->q_head; k.out_row = a->out_row; k.out_head = a->out_head;
+  k.table_stride = a->table_stride; k.q_row = q_row; k.q_head = q_head; k.out_row = out_row; k.out_head = out_head;
   k.q = (const bf16_t*)a->q; k.pool = (const unsigned char*)a->pool; k.block_table = a->block_table; k.lens = a->lens; k.q_start = a->q_start;
   k.out = (bf16_t*)a->out; k.lse = a->lse; k.ws = (float*)a->workspace;
   return launched("april_cache_attention", launch_cache_attention((hipStream_t)a->stream, k, a->head_dim));

@@ -99,18 +99,32 @@ def test_the_binding_refuses_tensors_that_are_not_on_a_gpu_or_of_another_kind():
         ap.april_cache_append(t(2, 2, 544, d=torch.uint8), t(3, 2, 32, d=torch.float32), t(3, 2, 32, d=torch.float32), t(3, d=torch.int64))
     with pytest.raises(ap.AprilError, match="not on a GPU"):
         ap.april_cache_attention(t(3, 2, 32, d=torch.bfloat16), t(2, 2, 544, d=torch.uint8), t(3, 4), t(3), 60)
-    cpu = torch.device("cpu")
-    with pytest.raises(ap.AprilError, match="torch.int32 wanted"):
-        binding._want("x", t(3, d=torch.int64), "torch.int32", (3,), cpu)
-    with pytest.raises(ap.AprilError, match="shape"):
-        binding._want("x", t(3), "torch.int32", (4,), cpu)
-    with pytest.raises(ap.AprilError, match="contiguous"):
-        binding._want("x", t(6)[::2], "torch.int32", (3,), cpu)
+    binding._need_torch()
+    i32 = torch.int32
+    for bad, match in ((t(3, d=torch.int64), "torch.int32 wanted"), (t(4), "shape"), (t(6)[::2], "contiguous")):
+        with pytest.raises(ap.AprilError, match=match):
+            binding._ptr("x", bad, i32, (3,), -1)               # (-1: what a tensor on the CPU calls its GPU)
+    assert binding._ptr("x", t(3), i32, (3,), -1)
+    with pytest.raises(ap.AprilError, match="on GPU 0"):
+        binding._ptr("x", t(3), i32, (3,), 0)
     with pytest.raises(ap.AprilError, match="adjacent"):
-        binding._table(t(4, 3).t(), cpu)
+        binding._table(t(4, 3).t(), 3, -1)
+    with pytest.raises(ap.AprilError, match="rows"):
+        binding._table(t(4, 3), 3, -1)
     with pytest.raises(ap.AprilError, match="adjacent"):
-        binding._strided("x", t(3, 32, 2).transpose(1, 2))
+        binding._rows("x", t(3, 32, 2).transpose(1, 2), i32, (3, 2, 32), -1)
+    assert binding._rows("x", t(3, 2, 40)[..., :32], i32, (3, 2, 32), -1)[1:] == (80, 40)
+
+
+def test_numbers_beyond_their_type_are_refused():
+    with pytest.raises(ap.AprilError, match="range"):
+        binding._bytes(binding._PACK_EXTEND, 1 << 31, *range(16))
 
 
 def test_struct_layouts():
-    assert (C.sizeof(ap.april_cache_extend_args), C.sizeof(ap.april_cache_append_args), C.sizeof(ap.april_cache_attention_args)) == (120, 112, 160)
+    import struct
+    for cls, pack, n in ((ap.april_cache_extend_args, "4iq12Q", 17), (ap.april_cache_append_args, "6i4q7Q", 17), (ap.april_cache_attention_args, "9if5q8QqQ", 25)):
+        assert C.sizeof(cls) == struct.calcsize(pack) and len(cls._fields_) == n
+        values = list(range(3, 3 + n))                          # the packed bytes are the structure's, field by field
+        got = cls.from_buffer_copy(struct.pack(pack, *values))
+        assert [getattr(got, f) for f, _ in cls._fields_] == values
