@@ -21,6 +21,7 @@ import numpy as np
 
 DTYPE_FP32 = 0
 DTYPE_BF16 = 1
+DTYPE_BF16_KV4 = 2      # bf16 with the KV cache in 4 bits
 
 SAMPLER_GREEDY = 0
 SAMPLER_TOPK = 1
@@ -164,7 +165,7 @@ def weight_tensor(s: ModelShape, name: str, shape: Tuple[int, ...], kind: str, s
     else:
         a = rng.standard_normal(shape, dtype=np.float32)
         a *= np.float32(1.0 / np.sqrt(shape[-1]))
-    if s.dtype == DTYPE_BF16:
+    if s.dtype != DTYPE_FP32:
         a = bf16_bits_to_fp32(fp32_to_bf16_bits(a)).reshape(shape)
     return a
 

@@ -41,6 +41,8 @@ extern "C" {
 
 #define APRIL_DTYPE_FP32 0
 #define APRIL_DTYPE_BF16 1
+#define APRIL_DTYPE_BF16_KV4 2   /* bf16, but the KV cache in 4 bits (the blocks of the 4-bit cache operators below): 3.8 times
+                                    the tokens in the same memory, and keys and values rounded to MXFP4         */
 #define APRIL_MEM_KV      1   /* memory tags of april_memory_pause / april_memory_resume */
 #define APRIL_MEM_WEIGHTS 2
 #define APRIL_SAMPLER_GREEDY 0
@@ -61,7 +63,7 @@ typedef struct april_buffer april_buffer;  /* opaque handle: a continuation buff
 typedef struct {
   int32_t n_layers, d_model, n_q_heads, n_kv_heads, head_dim, d_ffn, vocab;
   int32_t n_experts, experts_per_tok, d_expert_ffn;  /* 0,0,0 => dense MLP                */
-  int32_t dtype;             /* APRIL_DTYPE_*: type of weights, KV cache, GEMM operands   */
+  int32_t dtype;             /* APRIL_DTYPE_*: type of weights, KV cache, GEMM operands (BF16_KV4: cache apart) */
   float   rope_theta, rms_eps;
   int32_t kv_block_tokens;   /* tokens per KV page; must be 16                            */
   int64_t kv_pool_bytes;     /* 0 => sized for max_inflight sequences of max_ctx tokens,
@@ -97,7 +99,7 @@ typedef struct {
 /* One named weight tensor.  `data` is host or device memory (on_device says which),
  * borrowed for the duration of april_init only: the library keeps its own copy in
  * the layout its kernels want.  Element type: float for APRIL_DTYPE_FP32, bf16 bit
- * patterns (uint16) for APRIL_DTYPE_BF16; norm gains are always float.
+ * patterns (uint16) for APRIL_DTYPE_BF16 and APRIL_DTYPE_BF16_KV4; norm gains are always float.
  * Names (l = layer index): tok_emb [vocab,d]; attn_norm.l [d]; wq.l [Hq*dh,d];
  * wk.l, wv.l [Hkv*dh,d]; wo.l [d,Hq*dh]; mlp_norm.l [d]; w_gate.l, w_up.l [F,d];
  * w_down.l [d,F]; final_norm [d]; lm_head [vocab,d]; for experts: router.l [E,d],

@@ -40,8 +40,16 @@ def open_block(codes, biased):
 def rounded(x):
     """Values that the cache stands for once x [..., head_dim] is stored."""
     x = np.asarray(x, dtype=np.float64)
-    flat = x.reshape(-1, 32)
-    return np.stack([open_block(*round_block(b)) for b in flat]).reshape(x.shape) if len(flat) else x.copy()
+    b = x.reshape(-1, 32)
+    fine = np.all(np.isfinite(b), axis=1)
+    frac, power = np.frexp(np.max(np.abs(np.where(fine[:, None], b, 0.0)), axis=1))
+    e = np.clip(np.where(frac >= 0.875, power, power - 1) - 2, -125, 125)
+    e = np.where(frac == 0, -125, e)
+    dist = np.abs(np.abs(b)[:, :, None] * 2.0 ** -e[:, None, None].astype(np.float64) - STEPS)
+    even, odd = dist[:, :, 0::2], dist[:, :, 1::2]
+    code = np.where(even.min(-1) <= odd.min(-1), 2 * even.argmin(-1), 2 * odd.argmin(-1) + 1)
+    y = np.copysign(STEPS[code] * 2.0 ** e[:, None].astype(np.float64), b)
+    return np.where(fine[:, None], y, np.nan).reshape(x.shape)
 
 
 def store(pool, k, v, slots):

@@ -26,6 +26,8 @@ from __future__ import annotations
 
 import numpy as np
 
+from . import kv_cache
+
 F64 = np.float64
 
 
@@ -109,6 +111,8 @@ class Decoder:
         vocab, n_experts, experts_per_tok, rope_theta, rms_eps.  weights: name -> array."""
         self.s = shape
         self.w = {k: np.asarray(v, dtype=F64) for k, v in weights.items()}
+        # what a cache of fewer bits makes of keys / values [..., head_dim] (shape.dtype 2: 4 bits)
+        self.kv_round = kv_cache.rounded if getattr(shape, "dtype", None) == 2 else None
         self.route_margins = None     # set to a list to collect (position, layer, margin) of routed layers
 
     def new_cache(self, capacity=0):
@@ -134,8 +138,8 @@ class Decoder:
             v = (h @ w[f"wv.{l}"].T).reshape(T, s.n_kv_heads, s.head_dim)
             q = rope(q, pos[:, None], s.rope_theta)
             k = rope(k, pos[:, None], s.rope_theta)
-            cache.k[l][p0:p0 + T] = k
-            cache.v[l][p0:p0 + T] = v
+            cache.k[l][p0:p0 + T] = k if self.kv_round is None else self.kv_round(k)
+            cache.v[l][p0:p0 + T] = v if self.kv_round is None else self.kv_round(v)
             K = cache.k[l][:p0 + T]                                # [C, H_kv, d_h]
             V = cache.v[l][:p0 + T]
             # key j is visible to the query at position p iff j <= p

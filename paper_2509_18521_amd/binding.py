@@ -17,7 +17,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libapril.so")
 
 APRIL_OK, APRIL_EINVAL, APRIL_ENOMEM, APRIL_ESTARVED, APRIL_EHANDLE, APRIL_EDEVICE = 0, -1, -2, -3, -4, -5
-APRIL_DTYPE_FP32, APRIL_DTYPE_BF16 = 0, 1
+APRIL_DTYPE_FP32, APRIL_DTYPE_BF16, APRIL_DTYPE_BF16_KV4 = 0, 1, 2
 APRIL_SAMPLER_GREEDY, APRIL_SAMPLER_TOPK, APRIL_SAMPLER_CATEGORICAL = 0, 1, 2
 APRIL_MEM_KV, APRIL_MEM_WEIGHTS = 1, 2
 APRIL_KERNEL_CLASSES = 24
@@ -624,7 +624,7 @@ def pack_weights(shape, weights_fp32: Dict[str, np.ndarray]) -> Dict[str, np.nda
     out = {}
     for name, a in weights_fp32.items():
         is_gain = name.startswith(("attn_norm", "mlp_norm", "final_norm"))
-        if shape.dtype == APRIL_DTYPE_BF16 and not is_gain:
+        if shape.dtype != APRIL_DTYPE_FP32 and not is_gain:
             bits = np.ascontiguousarray(a, dtype=np.float32).view(np.uint32)
             if np.any(bits & np.uint32(0xFFFF)):
                 raise ValueError(f"{name}: values are not exactly representable in bf16")

@@ -19,6 +19,10 @@ struct CacheExtend {
   int *block_table, *free_pages, *lens_out, *free_top_out, *q_start;
   long long* slot_map;
   int *positions, *status;
+  // the engine's admission: sequence b is row row_of[b] of the table, holds nothing yet (lens null), and its pages are counted
+  // in held_of[row]; no rows, lengths or first rows are wanted (null)
+  const int* row_of;
+  int* held_of;
 };
 hipError_t launch_cache_extend(hipStream_t st, const CacheExtend& a);
 
@@ -43,6 +47,26 @@ struct CacheAttn {
   float* lse;
   float* ws;
 };
+// The engine's rows (decode: items = the scheduler's work list; prefill: tiles of q_tile positions).
+struct CacheRows {
+  const int4* items;
+  const int2* ctl;
+  const int* row_pos;
+  int q_tile;
+};
+void launch_cache_decode(hipStream_t st, const CacheAttn& a, int dh, const CacheRows& er, int rows, int chunk, int max_splits, int grid_splits);
+void launch_cache_prefill(hipStream_t st, const CacheAttn& a, int dh, const CacheRows& er, int n_items);
+// Queries rotated to bf16 rows [row][Hq][dh] (Hq 0: none); keys and values (kv_src: a row's keys, then its values) into the rows' pages if `store`.
+struct CacheRope {
+  const float *q_src, *kv_src;     // partial p of row r: src + p * partial_stride + r * ld
+  int q_ld, kv_ld, n_partials;
+  size_t partial_stride;
+  const float *rope_cos, *rope_sin;
+  bf16_t* q;
+  unsigned char* pool;             // the layer's pages
+  int Hq, store;
+};
+void launch_cache_rope(hipStream_t st, RowCtx rc, Slots s, const CacheRope& f, int dh, int Hkv);
 size_t cache_attention_workspace(const CacheAttn& a, int dh);
 hipError_t launch_cache_attention(hipStream_t st, const CacheAttn& a, int dh);
 

@@ -58,7 +58,7 @@ int april_cache_extend(const april_cache_extend_args* a) {
     REFUSE("april_cache_extend: null array");
   if (!aligned(a->slot_map, 8)) REFUSE("april_cache_extend: slot_map must be 8-byte aligned");
   const CacheExtend k{a->n_seqs, a->max_pages, a->n_pages, a->n_rows, (size_t)a->table_stride, a->lens, a->new_lens, a->free_top, a->block_table,
-                      a->free_pages, a->lens_out, a->free_top_out, a->q_start, reinterpret_cast<long long*>(a->slot_map), a->positions, a->status};
+                      a->free_pages, a->lens_out, a->free_top_out, a->q_start, reinterpret_cast<long long*>(a->slot_map), a->positions, a->status, nullptr, nullptr};
   return launched("april_cache_extend", launch_cache_extend((hipStream_t)a->stream, k));
 }
 

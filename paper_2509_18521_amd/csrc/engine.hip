@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "../../include/april.h"
+#include "cache.h"
 #include "kernels.h"
 
 using namespace april;
@@ -122,6 +123,7 @@ struct april_ctx {
   bool own_stream = false;
   std::string err;
   bool bf16 = false, use_mfma = false;
+  bool kv4 = false;              // the KV cache holds 4 bits (APRIL_DTYPE_BF16_KV4)
   size_t esz = 4;
 
   // weights
@@ -140,6 +142,7 @@ struct april_ctx {
   KVLayout kvl;
   int n_pages = 0;
   int64_t kv_pool_bytes = 0, kv_bytes_per_token = 0;
+  size_t kv4_layer_bytes = 0;    // 4-bit cache: a layer's pages
   int free_pages_host = 0;
 
   // scheduler state
@@ -586,7 +589,7 @@ void forward(april_ctx* c, RowCtx rows, RowCtx srows, const int* gather, double 
   hipStream_t st = c->stream;
   const int d = m.d_model, dh = m.head_dim, Hq = m.n_q_heads, Hkv = m.n_kv_heads, F = m.d_ffn, V = m.vocab;
   const int nq = Hq * dh, nkv = Hkv * dh, nqkv = nq + 2 * nkv;
-  const double e = (double)c->esz;
+  const double e = (double)c->esz, ekv = c->kv4 ? 17.0 / 32 : e;       // bytes of a weight or activation, of a cached element
   if (c->f32_dot && gather == nullptr && forward_f32_pays(rows.max_rows, c->step_max_ctx, nq)) {
     const SamplerCfg sc = sampler_cfg(c);
     const bool greedy = (sc.kind == APRIL_SAMPLER_GREEDY || (sc.kind == APRIL_SAMPLER_TOPK && sc.top_k <= 1)) && !c->cfg.debug_logits;
@@ -646,7 +649,30 @@ void forward(april_ctx* c, RowCtx rows, RowCtx srows, const int* gather, double 
     bf16_t* q16 = reinterpret_cast<bf16_t*>(c->q_rot);
     const bool pf_attn = c->attn_mfma && gather != nullptr && c->prefill_tiled;
     bool roped = false;
-    if (tile && pf_attn && l + 1 == m.n_layers && last_layer_cut_pays(c, rows.max_rows, srows.max_rows)) {
+    // 4-bit cache: the projection leaves fp32 rows (decode: their partial sums), which a kernel of its own rotates and stores
+    unsigned char* pool4 = static_cast<unsigned char*>(c->kv_pool) + (size_t)l * c->kv4_layer_bytes;
+    auto rope4 = [&](RowCtx rc, const float* q_src, int q_ld, const float* kv_src, int kv_ld, int n_part, int n_heads, bool store, double n) {
+      ProfScope p(c, KC_ROPE, n * (nqkv * 4.0 + nq * e + 2 * nkv * ekv), 0);
+      launch_cache_rope(st, rc, c->ds, CacheRope{q_src, kv_src, q_ld, kv_ld, n_part, c->qkv_stride, c->rope_cos, c->rope_sin, q16, pool4, n_heads, store ? 1 : 0}, dh, Hkv);
+    };
+    if (c->kv4 && tile && l + 1 == m.n_layers && last_layer_cut_pays(c, rows.max_rows, srows.max_rows)) {
+      // (as below: behind the last layer's keys and values only the sampling rows go on)
+      bf16_t* hl = (bf16_t*)c->hf;
+      norm(srows, 0, L.attn_norm, hl, gather, srows.max_rows, false, nullptr, c->proj);
+      gemm(KC_GEMM_QKV, rows, c->h_act, nullptr, L.wqkv_s + (size_t)nq * d, c->qkv, 2 * nkv, d, 1, 0, B);
+      rope4(rows, c->qkv, 0, c->qkv, 2 * nkv, 1, 0, true, B);
+      gemm(KC_GEMM_QKV, srows, hl, nullptr, L.wqkv_s, c->qkv, nq, d, 1, 0, srows.max_rows);
+      rope4(srows, c->qkv, nq, c->qkv, 0, 1, Hq, false, srows.max_rows);
+      roped = true;
+      x_res = c->proj;
+      rows = srows;
+      B = srows.max_rows;
+      gather_final = nullptr;
+    } else if (c->kv4) {
+      gemm(KC_GEMM_QKV, rows, c->h_act, nullptr, L.wqkv_s, c->qkv, nqkv, d, sq, c->qkv_stride, B, normed_by_down ? c->ssq : nullptr);
+      rope4(rows, c->qkv, nqkv, c->qkv + nq, nqkv, sq, Hq, true, B);
+      roped = true;
+    } else if (tile && pf_attn && l + 1 == m.n_layers && last_layer_cut_pays(c, rows.max_rows, srows.max_rows)) {
       // Behind the last layer's keys and values only the sampling rows go on: their queries, then everything, on rows
       // packed together.  (proj, which no prefill product writes, takes their residual stream; hf their normed rows until the final norm.)
       bf16_t* hl = (bf16_t*)c->hf;
@@ -676,7 +702,22 @@ void forward(april_ctx* c, RowCtx rows, RowCtx srows, const int* gather, double 
       if (c->bf16) launch_rope_append<bf16_t>(st, rows, c->ds, c->qkv, sq, c->qkv_stride, c->rope_cos, c->rope_sin, c->q_rot, (bf16_t*)c->kv_pool, c->kvl, l, Hq, pf_attn ? q16 : nullptr);
       else launch_rope_append<float>(st, rows, c->ds, c->qkv, sq, c->qkv_stride, c->rope_cos, c->rope_sin, c->q_rot, (float*)c->kv_pool, c->kvl, l, Hq);
     }
-    if (pf_attn) {
+    if (c->kv4) {
+      CacheAttn ca{};
+      ca.Hq = Hq; ca.Hkv = Hkv; ca.n_pages = c->n_pages; ca.max_pages = c->max_blocks; ca.n_rows = c->attn_ws_rows; ca.max_q = 1; ca.max_len = c->max_ctx;
+      ca.c2 = 1.4426950408889634f / sqrtf((float)dh);
+      ca.table_stride = c->max_blocks; ca.q_row = nq; ca.q_head = dh; ca.q = q16; ca.pool = pool4; ca.block_table = c->ds.block_table;
+      ca.out = (bf16_t*)c->attn_out; ca.ws = c->attn_ws;
+      ProfScope p(c, KC_ATTN, C * 2.0 * nkv * ekv + B * nq * 2 * e, 4.0 * C * nq);
+      if (gather != nullptr) {
+        const bool cut = rows.row_slot == srows.row_slot;
+        launch_cache_prefill(st, ca, dh, CacheRows{cut ? c->pf_last_items : c->pf_items, nullptr, nullptr, attn_prefill_tile(Hq / Hkv)},
+                             cut ? srows.max_rows : c->pf_n_items);
+      } else {
+        const int gs = std::min(c->attn_max_splits, std::max(1, ceil_div(c->step_max_ctx, c->attn_chunk)));
+        launch_cache_decode(st, ca, dh, CacheRows{c->d_att_items, rows.ctl, rows.row_pos, 0}, rows.max_rows, c->attn_chunk, c->attn_max_splits, gs);
+      }
+    } else if (pf_attn) {
       // prefill: one workgroup per tile of query positions, the keys / values of a prompt are
       // streamed once per tile instead of once per row
       ProfScope p(c, KC_ATTN, C * 2.0 * nkv * e + B * nq * (4.0 + e), 4.0 * C * nq);
@@ -906,7 +947,8 @@ int april_init(const april_model_cfg* cfg, const april_tensor* weights, int32_t 
   if (hipGetDeviceCount(&ndev) != hipSuccess || ndev <= 0) return fail(nullptr, APRIL_EDEVICE, "no HIP device");
   const april_model_cfg& g = *cfg;
   const bool moe = g.n_experts != 0;
-  if (moe && (g.dtype != APRIL_DTYPE_BF16 || g.n_experts < 1 || g.n_experts > 256 || g.experts_per_tok < 1 ||
+  const bool any_bf16 = g.dtype == APRIL_DTYPE_BF16 || g.dtype == APRIL_DTYPE_BF16_KV4;
+  if (moe && (!any_bf16 || g.n_experts < 1 || g.n_experts > 256 || g.experts_per_tok < 1 ||
               g.experts_per_tok > 8 || g.experts_per_tok > g.n_experts || g.d_expert_ffn <= 0 ||
               g.d_expert_ffn % 32 || g.d_model % 64 || g.n_experts % 32))
     return fail(nullptr, APRIL_EINVAL, "routed experts need bf16, 32 | n_experts <= 256, experts_per_tok <= 8, 32 | d_expert_ffn, 64 | d_model");
@@ -917,7 +959,7 @@ int april_init(const april_model_cfg* cfg, const april_tensor* weights, int32_t 
   if (g.n_q_heads / g.n_kv_heads > 16) return fail(nullptr, APRIL_EINVAL, "at most 16 query heads per KV head");
   if (g.head_dim != 32 && g.head_dim != 64 && g.head_dim != 128) return fail(nullptr, APRIL_EINVAL, "head_dim must be 32, 64 or 128");
   if (g.d_model % 8 || g.d_model > 8192) return fail(nullptr, APRIL_EINVAL, "d_model must be a multiple of 8, at most 8192");
-  if (g.dtype != APRIL_DTYPE_FP32 && g.dtype != APRIL_DTYPE_BF16) return fail(nullptr, APRIL_EINVAL, "bad dtype");
+  if (g.dtype != APRIL_DTYPE_FP32 && !any_bf16) return fail(nullptr, APRIL_EINVAL, "bad dtype");
   if (g.max_inflight <= 0 || g.max_inflight > 2048) return fail(nullptr, APRIL_EINVAL, "max_inflight must be in 1..2048");
   if (g.max_ctx <= 1 || g.max_ctx > 32768) return fail(nullptr, APRIL_EINVAL, "max_ctx must be in 2..32768");
   if (g.sampler != APRIL_SAMPLER_GREEDY && g.sampler != APRIL_SAMPLER_TOPK && g.sampler != APRIL_SAMPLER_CATEGORICAL)
@@ -931,21 +973,26 @@ int april_init(const april_model_cfg* cfg, const april_tensor* weights, int32_t 
     return fail(nullptr, APRIL_EINVAL, "n_samples_per_prompt must be in 0..max_inflight");
   const int nq = g.n_q_heads * g.head_dim, nkv = g.n_kv_heads * g.head_dim, nqkv = nq + 2 * nkv;
   const int d = g.d_model, F = g.d_ffn, V = g.vocab;
-  if (g.dtype == APRIL_DTYPE_BF16 && (d % 32 || (!moe && F % 32) || V % 32 || nq % 32 || nqkv % 32))
+  if (any_bf16 && (d % 32 || (!moe && F % 32) || V % 32 || nq % 32 || nqkv % 32))
     return fail(nullptr, APRIL_EINVAL, "bf16 path needs d_model, d_ffn, vocab, head widths multiple of 32");
+
+  if (g.dtype == APRIL_DTYPE_BF16_KV4 && nkv > 8192)
+    return fail(nullptr, APRIL_EINVAL, "the 4-bit KV cache needs n_kv_heads * head_dim of at most 8192");
 
   april_ctx* c = new april_ctx();
   c->cfg = g;
   c->dm = ModelDims{g.n_layers, d, g.n_q_heads, g.n_kv_heads, g.head_dim, F, V, g.n_experts, g.experts_per_tok,
                     g.d_expert_ffn, g.rope_theta, g.rms_eps, 16};
   c->moe = moe; c->n_experts = g.n_experts; c->top_k_experts = g.experts_per_tok; c->d_expert = g.d_expert_ffn;
-  c->bf16 = g.dtype == APRIL_DTYPE_BF16;
+  c->bf16 = any_bf16;
+  c->kv4 = g.dtype == APRIL_DTYPE_BF16_KV4;
   c->esz = c->bf16 ? 2 : 4;
   const char* gm = getenv("APRIL_GEMM");
   c->use_mfma = c->bf16 && !(gm && !strcmp(gm, "ref"));
   c->f32_dot = !c->bf16 && forward_f32_takes(d, F, nq, nqkv, V);
   const char* am = getenv("APRIL_ATTN");
   c->attn_mfma = c->bf16 && !(am && !strcmp(am, "ref"));
+  if (c->kv4 && !(c->use_mfma && c->attn_mfma)) { delete c; return fail(nullptr, APRIL_EINVAL, "the 4-bit KV cache runs on the MFMA path only"); }
   if (moe && !(c->use_mfma && c->attn_mfma)) { delete c; return fail(nullptr, APRIL_EINVAL, "routed experts run on the MFMA path only"); }
   const char* fr = getenv("APRIL_FUSE_ROPE");
   c->fuse_rope = !(fr && !strcmp(fr, "0"));
@@ -972,7 +1019,7 @@ int april_init(const april_model_cfg* cfg, const april_tensor* weights, int32_t 
   }
   if (const char* gi = getenv("APRIL_GRAPH_ITERS")) c->graph_iters = std::max(1, std::min(16, atoi(gi)));
   const char* pa = getenv("APRIL_PREFILL_ATTN");
-  c->prefill_tiled = !(pa && !strcmp(pa, "rows"));
+  c->prefill_tiled = c->kv4 || !(pa && !strcmp(pa, "rows"));
   const char* tg = getenv("APRIL_TILE_GEMM");
   c->tile_gemm = !(tg && !strcmp(tg, "0"));
   const char* gr = getenv("APRIL_GRAPH");
@@ -1048,7 +1095,7 @@ int april_init(const april_model_cfg* cfg, const april_tensor* weights, int32_t 
   TRY(dev_alloc(c, &c->d_list_a, 2048)); TRY(dev_alloc(c, &c->d_list_b, 2048));
 
   // ---- KV pool --------------------------------------------------------------------
-  c->kv_bytes_per_token = (int64_t)2 * g.n_layers * nkv * e;
+  c->kv_bytes_per_token = c->kv4 ? (int64_t)g.n_layers * g.n_kv_heads * cache_block_bytes(g.head_dim) / 16 : (int64_t)2 * g.n_layers * nkv * e;
   const int64_t page_bytes = c->kv_bytes_per_token * 16;
   int64_t pool = g.kv_pool_bytes;
   if (pool <= 0) {
@@ -1071,6 +1118,7 @@ int april_init(const april_model_cfg* cfg, const april_tensor* weights, int32_t 
   c->kvl.mode = c->attn_mfma ? 1 : 0;
   c->kvl.kv_stride = (size_t)c->n_pages * nkv * 16;
   c->kvl.layer_stride = 2 * c->kvl.kv_stride;
+  c->kv4_layer_bytes = (size_t)c->n_pages * g.n_kv_heads * cache_block_bytes(g.head_dim);
   TRY(dev_alloc(c, &c->d_free_stack, c->n_pages, false));
   launch_init_free_stack(c->stream, c->d_free_stack, c->n_pages);
   c->free_pages_host = c->n_pages;
@@ -1091,7 +1139,7 @@ int april_init(const april_model_cfg* cfg, const april_tensor* weights, int32_t 
   c->prefill_cap = std::max(g.max_ctx, 16384);
   if (lean) {
     const size_t tk = moe ? g.experts_per_tok : 0;
-    const size_t row_bytes = (size_t)d * 7 + (size_t)nq * 6 + (size_t)F * 2 + (moe ? (size_t)g.n_experts * 4 + tk * (2 * (size_t)g.d_expert_ffn + 4 * (size_t)d + 16) : 0);
+    const size_t row_bytes = (size_t)d * 7 + (size_t)nq * 6 + (c->kv4 ? (size_t)nqkv * 4 : 0) + (size_t)F * 2 + (moe ? (size_t)g.n_experts * 4 + tk * (2 * (size_t)g.d_expert_ffn + 4 * (size_t)d + 16) : 0);
     const size_t rows = std::min<size_t>({((size_t)4 << 30) / row_bytes, 65536, (size_t)S * g.max_ctx});
     c->prefill_cap = std::max(c->prefill_cap, (int)rows);
   }
@@ -1102,7 +1150,7 @@ int april_init(const april_model_cfg* cfg, const april_tensor* weights, int32_t 
   c->proj_stride = PR * d;
   TRY(dev_alloc(c, &c->x_res, M * d));
   if (c->use_mfma) TRY(dev_alloc(c, &c->ssq, (size_t)(d / 32) * M));
-  TRY(dev_alloc(c, &c->qkv, (size_t)c->s_qkv * c->qkv_stride));
+  TRY(dev_alloc(c, &c->qkv, std::max((size_t)c->s_qkv * c->qkv_stride, c->kv4 ? M * nqkv : 0)));      // (4-bit cache: prefill rows too)
   TRY(dev_alloc(c, &c->q_rot, M * nq));
   TRY(dev_alloc(c, &c->proj, (size_t)std::max(c->s_o, c->s_down) * c->proj_stride));
   if (!c->use_mfma) TRY(dev_alloc(c, &c->gu, M * 2 * F));
@@ -1147,7 +1195,7 @@ int april_init(const april_model_cfg* cfg, const april_tensor* weights, int32_t 
     c->attn_ws_rows = std::min<int>(c->m_cap, std::max({512, (S + 31) / 32 * 32, by_bytes}));
     TRY(dev_alloc(c, &c->attn_ws, (size_t)c->attn_ws_rows * g.n_kv_heads * c->attn_max_splits * rec, false));
     const char* al = getenv("APRIL_ATTN_LIST");
-    c->att_list = c->fuse_rope && !(al && !strcmp(al, "0"));
+    c->att_list = c->kv4 || (c->fuse_rope && !(al && !strcmp(al, "0")));
     if (c->att_list) {
       c->att_items_cap = S * c->attn_max_splits;
       TRY(dev_alloc(c, &c->d_att_items, (size_t)c->att_items_cap + 1));
@@ -1868,15 +1916,21 @@ int april_rollout_step(april_ctx* c, const april_request* new_reqs, int32_t n_ne
     // pages of every rollout that is (re-)prefilled this step, in admission order, before
     // the first scheduler pass hands out decode pages
     if (!prefill_slots.empty()) {
-      int* h_list = c->h_stage; int* h_need = c->h_stage + c->n_slots;
+      int* h_list = c->h_stage; int* h_len = c->h_stage + c->n_slots;
       for (size_t i = 0; i < prefill_slots.size(); ++i) {
         const SlotH& sh = c->slots[prefill_slots[i]];
         h_list[i] = prefill_slots[i];
-        h_need[i] = ceil_div(sh.prompt_len + sh.gen, blk);
+        h_len[i] = sh.prompt_len + sh.gen;
       }
       HIPCHK(c, hipMemcpyAsync(c->d_list_a, h_list, prefill_slots.size() * sizeof(int), hipMemcpyHostToDevice, st));
-      HIPCHK(c, hipMemcpyAsync(c->d_list_b, h_need, prefill_slots.size() * sizeof(int), hipMemcpyHostToDevice, st));
-      launch_alloc_prefill(st, c->d_ctrl, c->ds, c->d_list_a, c->d_list_b, (int)prefill_slots.size(), c->d_free_stack);
+      HIPCHK(c, hipMemcpyAsync(c->d_list_b, h_len, prefill_slots.size() * sizeof(int), hipMemcpyHostToDevice, st));
+      CacheExtend ext{};
+      ext.n_seqs = (int)prefill_slots.size(); ext.max_pages = c->max_blocks; ext.n_pages = c->n_pages; ext.table_stride = c->max_blocks;
+      ext.new_lens = c->d_list_b; ext.row_of = c->d_list_a; ext.held_of = c->ds.n_blocks;
+      ext.block_table = c->ds.block_table; ext.free_pages = c->d_free_stack;
+      ext.free_top = ext.free_top_out = &c->d_ctrl->free_top;
+      ext.status = &c->d_ctrl->error;
+      HIPCHK(c, launch_cache_extend(st, ext));
       // the prefill must not run on block tables that were not filled: look at the error flag now
       HIPCHK(c, hipMemcpyAsync(c->h_ctrl, c->d_ctrl, sizeof(Ctrl), hipMemcpyDeviceToHost, st));
       HIPCHK(c, hipStreamSynchronize(st));

@@ -219,8 +219,6 @@ __device__ inline void finish_row(const Slots& s, Ctrl* ctrl, const RowState& q,
 void launch_sched(hipStream_t st, Ctrl* ctrl, Slots s, int* row_slot, int* row_pos,
                   int* free_stack, int blk, int check_only, int row_cap, int ctx_cap,
                   int4* att_items = nullptr, int att_split = 0, int att_cap = 0);
-void launch_alloc_prefill(hipStream_t st, Ctrl* ctrl, Slots s, const int* slot_list,
-                          const int* n_blocks_needed, int n, int* free_stack);
 void launch_free_slots(hipStream_t st, Ctrl* ctrl, Slots s, const int* slot_list, int n,
                        int* free_stack);
 void launch_init_free_stack(hipStream_t st, int* free_stack, int n_blocks);

@@ -199,35 +199,6 @@ void launch_sched(hipStream_t st, Ctrl* ctrl, Slots s, int* row_slot, int* row_p
                      check_only, row_cap, ctx_cap, att_items, att_split, att_cap);
 }
 
-// Pages for freshly admitted rollouts (prefill): slot_list[i] gets need[i] pages.
-__global__ __launch_bounds__(256) void alloc_prefill_kernel(Ctrl* c, Slots s, const int* slot_list,
-                                                            const int* need, int n, int* free_stack) {
-  __shared__ int s_off[2049];
-  const int free_top = c->free_top;
-  if (threadIdx.x == 0) {
-    int acc = 0;
-    for (int i = 0; i < n; ++i) { s_off[i] = acc; acc += need[i]; }
-    s_off[n] = acc;
-  }
-  __syncthreads();
-  const int total = s_off[n];
-  if (total > free_top) { if (threadIdx.x == 0) c->error = 1; return; }
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    const int slot = slot_list[i], nb = need[i];
-    if (nb > s.max_blocks) { c->error = 1; continue; }
-    for (int j = 0; j < nb; ++j)
-      s.block_table[(size_t)slot * s.max_blocks + j] = free_stack[free_top - 1 - (s_off[i] + j)];
-    s.n_blocks[slot] = nb;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) c->free_top = free_top - total;
-}
-void launch_alloc_prefill(hipStream_t st, Ctrl* ctrl, Slots s, const int* slot_list, const int* need, int n,
-                          int* free_stack) {
-  if (n <= 0) return;
-  hipLaunchKernelGGL(alloc_prefill_kernel, dim3(1), dim3(256), 0, st, ctrl, s, slot_list, need, n, free_stack);
-}
-
 // Return every page of the listed slots to the stack.
 __global__ __launch_bounds__(256) void free_slots_kernel(Ctrl* c, Slots s, const int* slot_list, int n,
                                                          int* free_stack) {

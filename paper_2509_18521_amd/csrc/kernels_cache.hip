@@ -79,7 +79,7 @@ __global__ __launch_bounds__(EXT_THREADS) void cache_extend_kernel(CacheExtend a
   bool bad;
   auto scan = [&](int chunk) {
     const int b = chunk * EXT_THREADS + tid;
-    len = b < a.n_seqs ? a.lens[b] : 0;
+    len = b < a.n_seqs && a.lens != nullptr ? a.lens[b] : 0;
     add = b < a.n_seqs ? a.new_lens[b] : 0;
     bad = len < 0 || len > cap || (add > 0 && (long long)len + add > cap);
     const int held = bad ? 0 : (len + CACHE_PAGE - 1) / CACHE_PAGE;
@@ -99,22 +99,22 @@ __global__ __launch_bounds__(EXT_THREADS) void cache_extend_kernel(CacheExtend a
   }
   const long long have = (long long)top + all_rel;
   int status = 0;
-  if (any_bad || all_row > a.n_rows || top < 0 || have > a.n_pages) status = 2;
+  if (any_bad || (a.row_of == nullptr && all_row > a.n_rows) || top < 0 || have > a.n_pages) status = 2;
   else if (all_lack > have) status = 1;
   if (tid == 0) {
     *a.status = status;
     *a.free_top_out = status ? top : (int)(have - all_lack);
-    a.q_start[0] = 0;
+    if (a.q_start != nullptr) a.q_start[0] = 0;
   }
+  auto table_row = [&](int b) { return a.block_table + (size_t)(a.row_of != nullptr ? a.row_of[b] : b) * a.table_stride; };
   I base = 0;
   for (int c = 0; c < n_chunks; ++c) {              // lengths, first rows, pages given back
     if (n_chunks > 1) scan(c);
-    const int b = c * EXT_THREADS + tid;
     if (status == 0) {
       const int n = min(EXT_THREADS, a.n_seqs - c * EXT_THREADS);
       for (I k = tid; k < t_rel; k += EXT_THREADS) {
         const int s = find_in(s_rel, n, k);
-        a.free_pages[top + base + k] = a.block_table[(size_t)(c * EXT_THREADS + s) * a.table_stride + (size_t)(k - s_rel[s])];
+        a.free_pages[top + base + k] = table_row(c * EXT_THREADS + s)[k - s_rel[s]];
       }
       base += t_rel;
     }
@@ -127,20 +127,21 @@ __global__ __launch_bounds__(EXT_THREADS) void cache_extend_kernel(CacheExtend a
     if (n_chunks > 1) scan(c);
     const int b = c * EXT_THREADS + tid, n = min(EXT_THREADS, a.n_seqs - c * EXT_THREADS);
     if (b < a.n_seqs) {
-      a.lens_out[b] = status ? len : (add < 0 ? 0 : len + add);
-      a.q_start[b + 1] = status ? 0 : (int)(row_base + row + (add < 0 ? 0 : add));
+      const int now = status ? len : (add < 0 ? 0 : len + add);
+      if (a.lens_out != nullptr) a.lens_out[b] = now;
+      if (a.q_start != nullptr) a.q_start[b + 1] = status ? 0 : (int)(row_base + row + (add < 0 ? 0 : add));
+      if (a.held_of != nullptr && status == 0) a.held_of[a.row_of[b]] = (now + CACHE_PAGE - 1) / CACHE_PAGE;
     }
     if (status == 0) {
       for (I k = tid; k < t_lack; k += EXT_THREADS) {
         const int s = find_in(s_lack, n, k);
-        a.block_table[(size_t)(c * EXT_THREADS + s) * a.table_stride + (s_len[s] + CACHE_PAGE - 1) / CACHE_PAGE + (size_t)(k - s_lack[s])] =
-            a.free_pages[have - 1 - (base + k)];
+        table_row(c * EXT_THREADS + s)[(s_len[s] + CACHE_PAGE - 1) / CACHE_PAGE + (int)(k - s_lack[s])] = a.free_pages[have - 1 - (base + k)];
       }
       if (rows) {
         __syncthreads();
         for (I k = tid; k < t_row; k += EXT_THREADS) {
           const int s = find_in(s_row, n, k), pos = s_len[s] + (int)(k - s_row[s]);
-          put_row(a, (int)(row_base + k), a.block_table[(size_t)(c * EXT_THREADS + s) * a.table_stride + pos / CACHE_PAGE], pos);
+          put_row(a, (int)(row_base + k), table_row(c * EXT_THREADS + s)[pos / CACHE_PAGE], pos);
         }
       }
       base += t_lack;
@@ -165,11 +166,11 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(CacheExtend a) {
 }  // namespace
 
 hipError_t launch_cache_extend(hipStream_t st, const CacheExtend& a) {
-  const bool rows = a.n_rows <= 4096;
+  const bool rows = a.n_rows > 0 && a.n_rows <= 4096;
   const bool small = (long long)a.n_seqs * a.max_pages * CACHE_PAGE < (1ll << 30);
   hipError_t e = small ? launch(cache_extend_kernel<int>, dim3(1), dim3(EXT_THREADS), st, a, rows ? 1 : 0)
                        : launch(cache_extend_kernel<long long>, dim3(1), dim3(EXT_THREADS), st, a, rows ? 1 : 0);
-  if (e == hipSuccess && !rows) e = launch(cache_rows_kernel, dim3((a.n_rows + 255) / 256), dim3(256), st, a);
+  if (e == hipSuccess && a.n_rows > 0 && !rows) e = launch(cache_rows_kernel, dim3((a.n_rows + 255) / 256), dim3(256), st, a);
   return e;
 }
 
@@ -312,6 +313,11 @@ __device__ inline bf16x4 read_transposed(const bf16_t* p) {
 
 struct Split { int chunk, n; };                  // tokens of a split, splits of the longest context
 
+// Where a row's head's dimension goes: rows with strides, or (engine) the fragment-tiled layout of the products behind it.
+template <int DH, bool ENGINE> __device__ inline bf16_t* out_at(const CacheAttn& a, int r, int h, int d) {
+  return ENGINE ? a.out + act_index<true>(r, h * DH + d, a.Hq * DH) : a.out + r * a.out_row + h * a.out_head + d;
+}
+
 template <int DH> struct KRaw;
 template <> struct KRaw<32> { typedef unsigned type; };
 template <> struct KRaw<64> { typedef uint2 type; };
@@ -328,8 +334,9 @@ template <int DH> __device__ inline float* part_o(const CacheAttn& a, int n_spli
   return a.ws + (size_t)n_splits * a.n_rows * a.Hq * 2 + (((size_t)split * a.n_rows + r) * a.Hq + h) * DH;
 }
 
-template <int DH, int CT>
-__global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_kernel(CacheAttn a, Split sp) {
+// ENGINE: the work list of a decode iteration, entry 0 = {number}, entry 1 + i = {row, split, slot, position} (see launch_sched).
+template <int DH, int CT, bool ENGINE>
+__global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_kernel(CacheAttn a, Split sp, CacheRows er) {
   constexpr int KC = DH / 32, DT = DH / 16, NV = DH == 128 ? 2 : 1;
   constexpr int VS = DH + 16, OS = DH + 4;            // row strides in LDS: opened values, merged outputs
   constexpr int REC = CT * 16 * (2 + OS);             // floats of a wavefront's result
@@ -340,9 +347,19 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane & 15, g = lane >> 4;
   const int G = a.Hq / a.Hkv;
   // KV heads go round first: the heads of one sequence on different XCDs; splits last: only long contexts have the later ones
-  const int kvh = (int)(blockIdx.x % a.Hkv), rest = (int)(blockIdx.x / a.Hkv), b = rest % a.n_seqs, split = rest / a.n_seqs;
-  const int first = a.q_start != nullptr ? a.q_start[b] : b, count = a.q_start != nullptr ? a.q_start[b + 1] - first : 1;
-  const int len_raw = a.lens[b];
+  const int kvh = (int)(blockIdx.x % a.Hkv), rest = (int)(blockIdx.x / a.Hkv);
+  int b, split, first, count = 1, len_raw;
+  if (ENGINE) {
+    const int4 head = er.items[0], it = er.items[1 + rest];
+    if (er.ctl->y || rest >= head.x) return;
+    first = it.x; split = it.y; b = it.z; len_raw = it.w + 1;
+  } else {
+    b = rest % a.n_seqs;
+    split = rest / a.n_seqs;
+    first = a.q_start != nullptr ? a.q_start[b] : b;
+    if (a.q_start != nullptr) count = a.q_start[b + 1] - first;
+    len_raw = a.lens[b];
+  }
   if (first < 0 || count <= 0 || first >= a.n_rows) return;
   const int nq = min(min(count, a.max_q), a.n_rows - first);
   bool bad = len_raw < 0 || len_raw > a.max_len;
@@ -593,7 +610,7 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
         bf16x4 ob;
 #pragma unroll
         for (int e = 0; e < 4; ++e) ob[e] = (bf16_t)(o[e] * inv);
-        *reinterpret_cast<bf16x4*>(a.out + r * a.out_row + h * a.out_head + d * 16 + 4 * g) = ob;
+        *reinterpret_cast<bf16x4*>(out_at<DH, ENGINE>(a, r, h, d * 16 + 4 * g)) = ob;
       } else {
         *reinterpret_cast<f32x4*>(part_o<DH>(a, sp.n, split, r, h) + d * 16 + 4 * g) = o;
       }
@@ -606,11 +623,12 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
 }
 
 // Joins the splits of the rows that see tokens of several, in their order: a workgroup per row, 4 dimensions per thread.
-template <int DH>
-__global__ __launch_bounds__(256) void cache_join_kernel(CacheAttn a, Split sp) {
-  const int b = blockIdx.x / a.max_q, i = blockIdx.x % a.max_q;
-  const int first = a.q_start != nullptr ? a.q_start[b] : b, count = a.q_start != nullptr ? a.q_start[b + 1] - first : 1, r = first + i;
-  const int len = a.lens[b];
+template <int DH, bool ENGINE>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheAttn a, Split sp, CacheRows er) {
+  const int b = ENGINE ? (int)blockIdx.x : (int)blockIdx.x / a.max_q, i = ENGINE ? 0 : (int)blockIdx.x % a.max_q;
+  if (ENGINE && (er.ctl->y || b >= er.ctl->x)) return;
+  const int first = !ENGINE && a.q_start != nullptr ? a.q_start[b] : b, count = !ENGINE && a.q_start != nullptr ? a.q_start[b + 1] - first : 1, r = first + i;
+  const int len = ENGINE ? er.row_pos[b] + 1 : a.lens[b];
   if (first < 0 || i >= count || r >= a.n_rows || len < 0 || len > a.max_len || len - count + i + 1 <= sp.chunk) return;
   const int n_splits = (len - count + i + sp.chunk) / sp.chunk;
   for (int e = threadIdx.x; e < a.Hq * (DH / 4); e += 256) {
@@ -629,7 +647,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttn a, Split sp) 
     bf16x4 ob;
 #pragma unroll
     for (int q = 0; q < 4; ++q) ob[q] = (bf16_t)(o[q] * inv);
-    *reinterpret_cast<bf16x4*>(a.out + r * a.out_row + h * a.out_head + d) = ob;
+    *reinterpret_cast<bf16x4*>(out_at<DH, ENGINE>(a, r, h, d)) = ob;
     if (d == 0 && a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = lsum == 0.f ? -INFINITY : (M + log2f(lsum)) * 0.6931471805599453f;
   }
 }
@@ -649,8 +667,9 @@ constexpr int RA_STAGE = 64, RA_COLS = 256;
 template <int DH> __device__ inline int k_unit(int row, int u) { return u ^ ((row / (128 / DH)) & (DH / 8 - 1)); }
 template <int DH> __device__ inline int v_unit(int row, int u) { return u ^ (4 * ((row / (128 / DH)) & (DH / 32 - 1))) ^ ((row >> 2) & 3); }
 
-template <int DH>
-__global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Split sp, int n_qt) {
+// ENGINE: items {slot, first row of the sequence, its tokens, first position of the tile} of er.q_tile positions (see launch_attn_prefill).
+template <int DH, bool ENGINE>
+__global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Split sp, int n_qt, CacheRows er) {
   constexpr int KC = DH / 16, DT = DH / 32, CT = 2, NB = DH / 32, NV = DH == 128 ? 2 : 1;
   constexpr float RESCALE = 8.0f;
   __shared__ bf16x8 lds[2][2][RA_STAGE * DH / 8];            // [buffer][keys | values][token][16-byte unit]
@@ -660,13 +679,23 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
   // KV heads first (different XCDs), the tiles with the most tokens before the others, splits last
   const int kvh = (int)(blockIdx.x % a.Hkv);
   int rest = (int)(blockIdx.x / a.Hkv);
-  const int b = rest % a.n_seqs;
-  rest /= a.n_seqs;
-  const int qt = n_qt - 1 - rest % n_qt, split = rest / n_qt;
-  const int first = a.q_start != nullptr ? a.q_start[b] : b, count = a.q_start != nullptr ? a.q_start[b + 1] - first : 1;
-  const int len_raw = a.lens[b];
-  if (first < 0 || count <= 0 || first >= a.n_rows) return;
-  const int nq = min(min(count, a.max_q), a.n_rows - first), n_cols = nq * G, col0 = qt * RA_COLS;
+  int b, split = 0, first, count = 1, len_raw, n_cols, col0;
+  if (ENGINE) {
+    const int4 it = er.items[rest];
+    b = it.x; first = it.y; count = len_raw = it.z;
+    col0 = it.w * G;
+    n_cols = min(count, it.w + er.q_tile) * G;
+  } else {
+    b = rest % a.n_seqs;
+    rest /= a.n_seqs;
+    split = rest / n_qt;
+    first = a.q_start != nullptr ? a.q_start[b] : b;
+    if (a.q_start != nullptr) count = a.q_start[b + 1] - first;
+    len_raw = a.lens[b];
+    if (first < 0 || count <= 0 || first >= a.n_rows) return;
+    col0 = (n_qt - 1 - rest % n_qt) * RA_COLS;
+    n_cols = min(min(count, a.max_q), a.n_rows - first) * G;
+  }
   if (col0 >= n_cols) return;
   bool bad = len_raw < 0 || len_raw > a.max_len;
   const int len = bad ? 0 : len_raw;
@@ -741,7 +770,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
   for (int ct = 0; ct < CT; ++ct) {
     const int c0 = col0 + wave * 64 + ct * 32, col = c0 + cl, i = col / G;
     used[ct] = col < n_cols;
-    row[ct] = first + (used[ct] ? i : 0);
+    row[ct] = first + (used[ct] ? i : col0 / G);
     head[ct] = kvh * G + (col - i * G);
     vis[ct] = used[ct] ? len - count + i + 1 : 0;
     vis_first[ct] = len - count + c0 / G + 1;
@@ -872,7 +901,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
           bf16x4 ob;
 #pragma unroll
           for (int e = 0; e < 4; ++e) ob[e] = (bf16_t)(o[e] * inv);
-          *reinterpret_cast<bf16x4*>(a.out + r * a.out_row + h * a.out_head + dim) = ob;
+          *reinterpret_cast<bf16x4*>(out_at<DH, ENGINE>(a, r, h, dim)) = ob;
         } else {
           *reinterpret_cast<f32x4*>(part_o<DH>(a, sp.n, split, r, h) + dim) = o;
         }
@@ -906,10 +935,10 @@ template <int DH> hipError_t attention(hipStream_t st, const CacheAttn& a) {
   const Split sp = split_of(a);
   const int n_qt = row_tiles(a);
   const dim3 grid((unsigned)a.Hkv * a.n_seqs * sp.n * (few_rows(a) ? 1 : n_qt));
-  hipError_t e = !few_rows(a) ? launch(cache_attn_rows_kernel<DH>, grid, dim3(256), st, a, sp, n_qt)
-                 : a.max_q * (a.Hq / a.Hkv) <= 16 ? launch(cache_attn_kernel<DH, 1>, grid, dim3(64 * CA_WAVES), st, a, sp)
-                                                  : launch(cache_attn_kernel<DH, 2>, grid, dim3(64 * CA_WAVES), st, a, sp);
-  if (e == hipSuccess && sp.n > 1) e = launch(cache_join_kernel<DH>, dim3(a.n_seqs * a.max_q), dim3(256), st, a, sp);
+  hipError_t e = !few_rows(a) ? launch(cache_attn_rows_kernel<DH, false>, grid, dim3(256), st, a, sp, n_qt, CacheRows{})
+                 : a.max_q * (a.Hq / a.Hkv) <= 16 ? launch(cache_attn_kernel<DH, 1, false>, grid, dim3(64 * CA_WAVES), st, a, sp, CacheRows{})
+                                                  : launch(cache_attn_kernel<DH, 2, false>, grid, dim3(64 * CA_WAVES), st, a, sp, CacheRows{});
+  if (e == hipSuccess && sp.n > 1) e = launch(cache_join_kernel<DH, false>, dim3(a.n_seqs * a.max_q), dim3(256), st, a, sp, CacheRows{});
   return e;
 }
 
@@ -918,6 +947,90 @@ template <int DH> hipError_t attention(hipStream_t st, const CacheAttn& a) {
 size_t cache_attention_workspace(const CacheAttn& a, int dh) {
   const Split sp = split_of(a);
   return sp.n > 1 ? (size_t)sp.n * a.n_rows * a.Hq * (dh + 2) * sizeof(float) : 0;
+}
+
+// The engine's passes: decode iterations over the scheduler's work list, prefill over its tiles of query positions.  Splits have the
+// engine's length, whatever the batch, so that a rollout's sums depend on its own length alone.
+void launch_cache_decode(hipStream_t st, const CacheAttn& a, int dh, const CacheRows& er, int rows, int chunk, int max_splits, int grid_splits) {
+  const Split sp{chunk, max_splits};
+  const dim3 grid((unsigned)rows * grid_splits * a.Hkv);
+#define CACHE_DECODE(DH)                                                                        \
+  launch(cache_attn_kernel<DH, 1, true>, grid, dim3(64 * CA_WAVES), st, a, sp, er);               \
+  if (grid_splits > 1) launch(cache_join_kernel<DH, true>, dim3(rows), dim3(256), st, a, sp, er)
+  switch (dh) {
+    case 32: CACHE_DECODE(32); break;
+    case 64: CACHE_DECODE(64); break;
+    default: CACHE_DECODE(128); break;
+  }
+#undef CACHE_DECODE
+}
+void launch_cache_prefill(hipStream_t st, const CacheAttn& a, int dh, const CacheRows& er, int n_items) {
+  if (n_items <= 0) return;
+  const Split sp{0x7fffff80, 1};
+  const dim3 grid((unsigned)n_items * a.Hkv);
+  switch (dh) {
+    case 32: launch(cache_attn_rows_kernel<32, true>, grid, dim3(256), st, a, sp, 1, er); break;
+    case 64: launch(cache_attn_rows_kernel<64, true>, grid, dim3(256), st, a, sp, 1, er); break;
+    default: launch(cache_attn_rows_kernel<128, true>, grid, dim3(256), st, a, sp, 1, er); break;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The engine's rotary embedding and store: a workgroup per row.  Sums the projection's partials, rotates the queries (bf16 rows) and
+// the key, and stores key and value in the row's page; they meet in LDS, where a block's 32 dimensions lie together.
+// ---------------------------------------------------------------------------
+namespace {
+
+__global__ __launch_bounds__(256) void cache_rope_kernel(RowCtx rc, Slots s, CacheRope f, int dh, int Hkv) {
+  extern __shared__ float s_kv[];                     // [key | value][Hkv * dh]
+  const int r = blockIdx.x;
+  ROW_GUARD(rc, r);
+  const int slot = rc.row_slot[r], pos = rc.row_pos[r], half = dh >> 1, nkv = Hkv * dh;
+  const float* cs = f.rope_cos + (size_t)pos * half;
+  const float* sn = f.rope_sin + (size_t)pos * half;
+  auto value = [&](const float* src, int col) {
+    float x = src[col];
+    for (int p = 1; p < f.n_partials; ++p) x += src[p * f.partial_stride + col];        // in the order p = 0, 1, ...
+    return x;
+  };
+  const float* q = f.q_src + (size_t)r * f.q_ld;
+  const float* kv = f.kv_src + (size_t)r * f.kv_ld;
+  for (int e = threadIdx.x; e < (f.Hq + (f.store ? Hkv : 0)) * half; e += 256) {
+    const int hd = e / half, i = e - hd * half;
+    const float* src = hd < f.Hq ? q + hd * dh : kv + (hd - f.Hq) * dh;
+    const float a = value(src, i), b = value(src, i + half), ra = rope_first(a, b, cs[i], sn[i]), rb = rope_second(a, b, cs[i], sn[i]);
+    if (hd < f.Hq) {
+      bf16_t* to = f.q + ((size_t)r * f.Hq + hd) * dh + i;
+      to[0] = (bf16_t)ra;
+      to[half] = (bf16_t)rb;
+    } else {
+      s_kv[(hd - f.Hq) * dh + i] = ra;
+      s_kv[(hd - f.Hq) * dh + i + half] = rb;
+    }
+  }
+  if (!f.store) return;
+  for (int e = threadIdx.x; e < nkv; e += 256) s_kv[nkv + e] = value(kv, nkv + e);
+  __syncthreads();
+  const int page = s.block_table[(size_t)slot * s.max_blocks + pos / CACHE_PAGE], tok = pos % CACHE_PAGE;
+  unsigned char* base = f.pool + (size_t)page * Hkv * cache_block_bytes(dh);
+  // (2 nkv / 8 pieces, a multiple of 4: a block's four lanes take every trip together)
+  for (int e = threadIdx.x; e < nkv / 4; e += 256) {
+    const int at = e * 8, val = at >= nkv, d = at - val * nkv, head = d / dh, blk = d % dh / 32, part = d % 32 / 8;
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = s_kv[at + i];
+    unsigned ex;
+    const unsigned c = cache_codes(x, ex);
+    unsigned char* to = base + (size_t)head * cache_block_bytes(dh);
+    *reinterpret_cast<unsigned*>(to + cache_code_off(dh, val, blk, tok) + part * 4) = c;
+    if (part == 0) to[cache_scale_off(dh, val, blk, tok)] = (unsigned char)ex;
+  }
+}
+
+}  // namespace
+
+void launch_cache_rope(hipStream_t st, RowCtx rc, Slots s, const CacheRope& f, int dh, int Hkv) {
+  hipLaunchKernelGGL(cache_rope_kernel, dim3(rc.max_rows), dim3(256), f.store ? 2 * Hkv * dh * sizeof(float) : 0, st, rc, s, f, dh, Hkv);
 }
 
 hipError_t launch_cache_attention(hipStream_t st, const CacheAttn& a, int dh) {

@@ -37,6 +37,16 @@ def test_ties_go_to_the_even_code_and_rounded_values_stay():
     assert np.all(np.isnan(kc.rounded(x)))
 
 
+def test_rounding_of_many_blocks_is_that_of_each():
+    rng = np.random.default_rng(7)
+    x = rng.standard_normal((9, 2, 64)) * np.exp2(rng.integers(-140, 128, size=(9, 2, 1)).astype(np.float64))
+    x[0, 0, :32] = 0
+    x[1, 1, 40] = np.nan
+    x[2, 0, :32] = rng.integers(-24, 25, size=32) * 0.25
+    each = np.stack([kc.open_block(*kc.round_block(b)) for b in x.reshape(-1, 32)]).reshape(x.shape)
+    assert np.array_equal(kc.rounded(x), each, equal_nan=True)
+
+
 def test_store_and_read():
     rng = np.random.default_rng(1)
     pool = rng.integers(0, 256, size=(5, 2, 17 * 64), dtype=np.uint8)
