@@ -293,7 +293,7 @@ hipError_t launch_cache_append(hipStream_t st, const CacheAppend& a, bool f32) {
 // terms, was tried: its sums keep about 17 bits, 4.5e-6 of a score against 8e-9 here, and a short row's lse showed it.)
 // V: a fragment wants 8 tokens of one dimension, the store 32 dimensions of one token (so that a token is appended without
 // touching its neighbours): lanes open the blocks that they loaded into a tile of LDS, [token][dim], and
-// read it back transposed (ds_read_b64_tr_b16).  Rows of dh + 16 elements put the 8 rows of a read on different banks.
+// read it back transposed (ds_read_b64_tr_b16).  Rows of dh + 16 elements put the rows of a read on different banks.
 // ---------------------------------------------------------------------------
 namespace {
 
@@ -368,13 +368,14 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
   if (split > 0 && t_begin >= len) return;
   const int t_end = min(len, t_begin + sp.chunk), n_tiles = (t_end - t_begin + 31) >> 5, n_pages = (t_end - t_begin + 15) >> 4;
 
-  // page ids of the split, one per lane and register; ids outside the pool are noticed and not followed
+  // page ids of the split, one per lane and register (loading them as the tiles come to them, in a branch, had every wait in the loop be
+  // for all loads: 245 against 238 us); ids outside the pool are noticed and not followed
   const int* bt = a.block_table + (size_t)b * a.table_stride + (t_begin >> 4);
   int my_page[CA_MOST / 1024];
 #pragma unroll
   for (int q = 0; q < CA_MOST / 1024; ++q) {
     const int i = q * 64 + lane;
-    my_page[q] = n_pages > 0 && (q == 0 || q * 64 < n_pages) ? bt[i < n_pages ? i : n_pages - 1] : 0;
+    my_page[q] = n_pages > q * 64 ? bt[i < n_pages ? i : n_pages - 1] : 0;
     const bool out = (unsigned)my_page[q] >= (unsigned)a.n_pages;
     bad |= __any(out);
     if (out) my_page[q] = 0;
@@ -479,11 +480,11 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
             }
       }
       if (DH > 32 || g < 2) {
-        bf16_t* to = vl + row * VS + vblk * 32;
-        *reinterpret_cast<bf16x8*>(to) = cache_open(c.x, e);
-        *reinterpret_cast<bf16x8*>(to + 8) = cache_open(c.y, e);
-        *reinterpret_cast<bf16x8*>(to + 16) = cache_open(c.z, e);
-        *reinterpret_cast<bf16x8*>(to + 24) = cache_open(c.w, e);
+        bf16x8* to = reinterpret_cast<bf16x8*>(vl + row * VS + vblk * 32);
+        to[0] = cache_open(c.x, e);
+        to[1] = cache_open(c.y, e);
+        to[2] = cache_open(c.z, e);
+        to[3] = cache_open(c.w, e);
       }
     }
     f32x4 sacc[CT][2];
@@ -622,7 +623,9 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
   }
 }
 
-// Joins the splits of the rows that see tokens of several, in their order: a workgroup per row, 4 dimensions per thread.
+// Joins the splits of the rows that see tokens of several, in their order: 4 dimensions of a head per thread, 1024 elements of a row per
+// workgroup.  The loads of 4 splits go out together.  (A workgroup per row, a split at a time: 34 us of the 71 of 7 rows of 32 heads over
+// up to 19 splits.)
 template <int DH, bool ENGINE>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttn a, Split sp, CacheRows er) {
   const int b = ENGINE ? (int)blockIdx.x : (int)blockIdx.x / a.max_q, i = ENGINE ? 0 : (int)blockIdx.x % a.max_q;
@@ -631,26 +634,48 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttn a, Split sp, 
   const int len = ENGINE ? er.row_pos[b] + 1 : a.lens[b];
   if (first < 0 || i >= count || r >= a.n_rows || len < 0 || len > a.max_len || len - count + i + 1 <= sp.chunk) return;
   const int n_splits = (len - count + i + sp.chunk) / sp.chunk;
-  for (int e = threadIdx.x; e < a.Hq * (DH / 4); e += 256) {
-    const int h = e / (DH / 4), d = 4 * (e % (DH / 4));
-    float M = -INFINITY, lsum = 0.f;
-    for (int s = 0; s < n_splits; ++s) M = fmaxf(M, part_ml(a, s, r, h)[0]);
-    const float Mu = M == -INFINITY ? 0.f : M;
-    f32x4 o = f32x4{};
-    for (int s = 0; s < n_splits; ++s) {
-      const float2 ml = *reinterpret_cast<const float2*>(part_ml(a, s, r, h));
-      const float w = __builtin_amdgcn_exp2f(ml.x - Mu);
-      lsum += w * ml.y;
-      o += *reinterpret_cast<const f32x4*>(part_o<DH>(a, sp.n, s, r, h) + d) * w;
-    }
-    const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;
-    bf16x4 ob;
+  const int e = blockIdx.y * 256 + threadIdx.x, h = e / (DH / 4), d = 4 * (e % (DH / 4));
+  if (h >= a.Hq) return;
+  const float* ml = part_ml(a, 0, r, h);
+  const float* po = part_o<DH>(a, sp.n, 0, r, h) + d;
+  const size_t ml_step = (size_t)a.n_rows * a.Hq * 2, o_step = (size_t)a.n_rows * a.Hq * DH;
+  constexpr int U = 4;
+  float M = -INFINITY;
+  for (int s = 0; s < n_splits; s += 2 * U) {
+    float v[2 * U];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) ob[q] = (bf16_t)(o[q] * inv);
-    *reinterpret_cast<bf16x4*>(out_at<DH, ENGINE>(a, r, h, d)) = ob;
-    if (d == 0 && a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = lsum == 0.f ? -INFINITY : (M + log2f(lsum)) * 0.6931471805599453f;
+    for (int u = 0; u < 2 * U; ++u) v[u] = ml[min(s + u, n_splits - 1) * ml_step];
+#pragma unroll
+    for (int u = 0; u < 2 * U; ++u) M = fmaxf(M, v[u]);
   }
+  const float Mu = M == -INFINITY ? 0.f : M;
+  float lsum = 0.f;
+  f32x4 o = f32x4{};
+  for (int s = 0; s < n_splits; s += U) {
+    float2 v[U];
+    f32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = min(s + u, n_splits - 1);
+      v[u] = *reinterpret_cast<const float2*>(ml + at * ml_step);
+      x[u] = *reinterpret_cast<const f32x4*>(po + at * o_step);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (s + u < n_splits) {
+        const float w = __builtin_amdgcn_exp2f(v[u].x - Mu);
+        lsum += w * v[u].y;
+        o += x[u] * w;
+      }
+  }
+  const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;
+  bf16x4 ob;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) ob[q] = (bf16_t)(o[q] * inv);
+  *reinterpret_cast<bf16x4*>(out_at<DH, ENGINE>(a, r, h, d)) = ob;
+  if (!ENGINE && d == 0 && a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = lsum == 0.f ? -INFINITY : (M + log2f(lsum)) * 0.6931471805599453f;
 }
+template <int DH> dim3 join_grid(const CacheAttn& a, int rows) { return dim3(rows, (a.Hq * (DH / 4) + 255) / 256); }
 
 // ---------------------------------------------------------------------------
 // Attention of many rows: a workgroup (4 wavefronts) owns 256 columns (row, query head) of one (sequence, KV head) and walks over
@@ -916,14 +941,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
 bool few_rows(const CacheAttn& a) { return (long long)a.max_q * (a.Hq / a.Hkv) <= 32; }
 int row_tiles(const CacheAttn& a) { return (int)(((long long)a.max_q * (a.Hq / a.Hkv) + RA_COLS - 1) / RA_COLS); }
 
-// Splits of the longest context: enough workgroups to fill the chip; of few rows a wavefront has at least two tiles, of
-// many rows a workgroup 8 stages.
+// Splits of the longest context: enough workgroups to fill the chip, 3 a compute unit of few rows, but no shorter than what pays for the launch
+// that joins them.
 Split split_of(const CacheAttn& a) {
   const bool few = few_rows(a);
+  const int least = few ? 512 : 512;
   const long long groups = std::max<long long>(1, (long long)a.n_seqs * a.Hkv * (few ? 1 : row_tiles(a)));
-  long long n = ((few ? 1024 : 256) + groups - 1) / groups;
+  long long n = std::max<long long>(1, std::min<long long>(((few ? 768 : 256) + groups - 1) / groups, (a.max_len + least - 1) / least));
   if (few) n = std::max<long long>(n, (a.max_len + CA_MOST - 1) / CA_MOST);
-  n = std::max<long long>(1, std::min<long long>(n, (a.max_len + (few ? 255 : 511)) / (few ? 256 : 512)));
   Split s;
   s.chunk = (int)std::max<long long>(128, ((a.max_len + n - 1) / n + 127) / 128 * 128);
   if (few) s.chunk = std::min(s.chunk, CA_MOST);
@@ -938,7 +963,7 @@ template <int DH> hipError_t attention(hipStream_t st, const CacheAttn& a) {
   hipError_t e = !few_rows(a) ? launch(cache_attn_rows_kernel<DH, false>, grid, dim3(256), st, a, sp, n_qt, CacheRows{})
                  : a.max_q * (a.Hq / a.Hkv) <= 16 ? launch(cache_attn_kernel<DH, 1, false>, grid, dim3(64 * CA_WAVES), st, a, sp, CacheRows{})
                                                   : launch(cache_attn_kernel<DH, 2, false>, grid, dim3(64 * CA_WAVES), st, a, sp, CacheRows{});
-  if (e == hipSuccess && sp.n > 1) e = launch(cache_join_kernel<DH, false>, dim3(a.n_seqs * a.max_q), dim3(256), st, a, sp, CacheRows{});
+  if (e == hipSuccess && sp.n > 1) e = launch(cache_join_kernel<DH, false>, join_grid<DH>(a, a.n_seqs * a.max_q), dim3(256), st, a, sp, CacheRows{});
   return e;
 }
 
@@ -956,7 +981,7 @@ void launch_cache_decode(hipStream_t st, const CacheAttn& a, int dh, const Cache
   const dim3 grid((unsigned)rows * grid_splits * a.Hkv);
 #define CACHE_DECODE(DH)                                                                        \
   launch(cache_attn_kernel<DH, 1, true>, grid, dim3(64 * CA_WAVES), st, a, sp, er);               \
-  if (grid_splits > 1) launch(cache_join_kernel<DH, true>, dim3(rows), dim3(256), st, a, sp, er)
+  if (grid_splits > 1) launch(cache_join_kernel<DH, true>, join_grid<DH>(a, rows), dim3(256), st, a, sp, er)
   switch (dh) {
     case 32: CACHE_DECODE(32); break;
     case 64: CACHE_DECODE(64); break;
