@@ -1,5 +1,6 @@
 // Kernels of the 4-bit KV cache (gfx950): tables from request lengths, the store, the attention that reads it.
 #include <algorithm>
+#include <cmath>
 #include <tuple>
 
 #include "cache.h"
@@ -450,11 +451,12 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
     for (int d = 0; d < DT; ++d) oacc[ct][d] = f32x4{};
   }
   bf16_t* vl = reinterpret_cast<bf16_t*>(lds[wave]);
+  bool nan_seen = false;
 
   auto compute = [&](int u, int i) {
     const int t0 = t_begin + (wave + i * CA_WAVES) * 32;
     // values into LDS: zeros behind the context's end (what lies there is anything) and for blocks of NaN, which would reach
-    // columns that do not see them; the columns that do are marked
+    // columns that do not see them; the columns that do are marked behind the loop
 #pragma unroll
     for (int p = 0; p < NV; ++p) {
       __builtin_amdgcn_sched_barrier(0);
@@ -462,22 +464,9 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
       uint4 c = vr[u][p];
       unsigned e = DH == 128 ? ks[u][p] >> 8 : vs[u][p];
       if (t0 + 32 > len && t0 + row >= len) { c = uint4{0, 0, 0, 0}; e = 127; }
-      const unsigned long long nan = __ballot(e == 255);
-      if (nan) {
+      if (__any(e == 255)) {
+        nan_seen = true;
         if (e == 255) { c = uint4{0, 0, 0, 0}; e = 127; }
-        int g4 = 4 * g;
-        asm volatile("" : "+v"(g4));                   // (nothing of this is to be computed ahead, in registers of the loop)
-#pragma clang loop unroll(disable)
-        for (int j = 0; j < 4; ++j)
-#pragma clang loop unroll(disable)
-          for (int pg = DH == 128 ? p : 0; pg < (DH == 128 ? p + 1 : 2); ++pg)
-#pragma clang loop unroll(disable)
-            for (int blk = 0; blk < KC; ++blk) {
-              const int at = g4 + j + 16 * (DH == 128 ? blk : pg * KC + blk), t = t0 + pg * 16 + g4 + j;
-#pragma unroll
-              for (int ct = 0; ct < CT; ++ct)
-                if ((nan >> at & 1) && t < vis[ct]) poison[ct] |= 1u << blk;
-            }
       }
       if (DH > 32 || g < 2) {
         bf16x8* to = reinterpret_cast<bf16x8*>(vl + row * VS + vblk * 32);
@@ -550,21 +539,40 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
     }
     asm volatile("" ::: "memory");
   };
-  int i = 0;
-  for (; i + 2 * R <= cnt; i += R) {
+  // A slot is requested again as soon as its tile is done; behind the last tile that is the last tile once more, so that no load is in a
+  // branch (a wait behind one would be for all loads).  Two copies of the loop's body: every compute unit has to fetch the code of a
+  // launch (with steady state and tail apart, five copies, 61 sequences of 100-2003 tokens took 20.7 us and not 17.4; the loop has 124 registers then, not 168: 192 of
+  // 576-4608 tokens, 32 + 8 heads of 128, 131 and 121).
+  for (int i = 0; i < cnt; i += R) {
 #pragma unroll
     for (int u = 0; u < R; ++u) {
-      compute(u, i + u);
+      if (u == 0 || i + u < cnt) compute(u, i + u);
       __builtin_amdgcn_sched_barrier(0);
-      request(u, i + R + u);
+      request(u, i + u + R);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
+  if (nan_seen)                                      // some block of this wavefront's values is NaN: mark the columns that see it
+#pragma clang loop unroll(disable)
+    for (int i = 0; i < cnt; ++i) {
+      const int tile = wave + i * CA_WAVES, t0 = t_begin + tile * 32;
+#pragma clang loop unroll(disable)
+      for (int p = 0; p < NV; ++p) {
+        const int pl = min(2 * tile + (DH == 128 ? p : vpage), n_pages - 1), page = bt[pl];
+        const unsigned char e = (unsigned)page < (unsigned)a.n_pages ? a.pool[((size_t)page * a.Hkv + kvh) * cache_block_bytes(DH) + off_vs] : 0;
+        const unsigned long long nan = __ballot(e == 255 && t0 + (DH == 128 ? p : vpage) * 16 + hh < len);
+#pragma clang loop unroll(disable)
+        for (int j = 0; j < 4; ++j)
+#pragma clang loop unroll(disable)
+          for (int pg = DH == 128 ? p : 0; pg < (DH == 128 ? p + 1 : 2); ++pg)
+#pragma clang loop unroll(disable)
+            for (int blk = 0; blk < KC; ++blk) {
+              const int at = 4 * g + j + 16 * (DH == 128 ? blk : pg * KC + blk), t = t0 + pg * 16 + 4 * g + j;
 #pragma unroll
-  for (int q = 0; q < 2 * R - 1; ++q)
-    if (i + q < cnt) {
-      compute(q % R, i + q);
-      if (q < R - 1 && i + q + R < cnt) request(q % R, i + q + R);
+              for (int ct = 0; ct < CT; ++ct)
+                if ((nan >> at & 1) && t < vis[ct]) poison[ct] |= 1u << blk;
+            }
+      }
     }
 
   // the wavefronts meet: each publishes (m, l, O), then merges its share of the columns' outputs
@@ -941,12 +949,17 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
 bool few_rows(const CacheAttn& a) { return (long long)a.max_q * (a.Hq / a.Hkv) <= 32; }
 int row_tiles(const CacheAttn& a) { return (int)(((long long)a.max_q * (a.Hq / a.Hkv) + RA_COLS - 1) / RA_COLS); }
 
-// Splits of the longest context: enough workgroups to fill the chip, 3 a compute unit of few rows, but no shorter than what pays for the launch
-// that joins them.
+// Splits of the longest context.  Few rows: a split costs its tiles (0.6 to 0.75 us for each 128 tokens of a workgroup that has a compute unit to
+// itself) and 0.1 us of the join, which takes 2.5 us besides: together least for about 8 sqrt(length) tokens.  us for one sequence of 32 + 8 heads of
+// 128 in splits of 256 | 512 | 1024 | 2048 | 4096: 1000 tokens 9.2 | 10.4 | 10.9 (whole), 331 7.5 | 5.5 (whole),
+// 2000 10.0 | 10.8 | 13.7 | 17.2, 4000 12.1 | 11.5 | 14.0 | 20.0 | 30.2,
+// 16000 28 | 19.3 | 18.0 | 22.2 | 34.8.  Up to 3 workgroups a compute unit that helps (8 sequences of 4000 19.7 | 16.8 | 16.1 | 21.8 | 31.8); where the
+// sequences alone fill the chip (192 of them and their KV heads, 3/4 of the compute units) it does not (32 of 1000 17.0 | 15.7 | 12.7, of 2000 25 | 21.8 | 20.5 | 19.8, of 16000 163 | 134 | 118 | 115 | 115), and
+// splits are for ragged batches.
 Split split_of(const CacheAttn& a) {
   const bool few = few_rows(a);
-  const int least = few ? 512 : 512;
   const long long groups = std::max<long long>(1, (long long)a.n_seqs * a.Hkv * (few ? 1 : row_tiles(a)));
+  const int least = !few ? 512 : groups >= 192 ? 2048 : a.max_len <= 768 ? 768 : ((int)(8 * std::sqrt((double)a.max_len)) + 127) / 128 * 128;
   long long n = std::max<long long>(1, std::min<long long>(((few ? 768 : 256) + groups - 1) / groups, (a.max_len + least - 1) / least));
   if (few) n = std::max<long long>(n, (a.max_len + CA_MOST - 1) / CA_MOST);
   Split s;
