@@ -46,6 +46,7 @@ struct CacheAttn {
   bf16_t* out;
   float* lse;
   float* ws;
+  int ws_rows;                     // rows that the workspace holds (at most n_rows)
 };
 // The engine's rows (decode: items = the scheduler's work list; prefill: tiles of q_tile positions).
 struct CacheRows {

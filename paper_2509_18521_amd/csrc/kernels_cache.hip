@@ -282,7 +282,7 @@ hipError_t launch_cache_append(hipStream_t st, const CacheAppend& a, bool f32) {
 }
 
 // ---------------------------------------------------------------------------
-// Attention of few rows: one workgroup (4 wavefronts) per (sequence, KV head, split of the context), up to 16 CT columns
+// Attention of few rows: one workgroup (4 wavefronts) per (sequence, KV head, split of the context), up to 16 CT columns, CT 1, 2 or 4
 // (row of the sequence, query head of the KV head).  The wavefronts take the split's tiles of 32 tokens in turn, each with an online
 // softmax in registers; they meet in LDS, the splits of a context in a second small kernel, both in a fixed order.
 //
@@ -329,15 +329,32 @@ template <int DH> __device__ inline unsigned k_word(const typename KRaw<DH>::typ
   else return c == 0 ? r.x : c == 1 ? r.y : c == 2 ? r.z : r.w;
 }
 
-// Partial results of a split: per (row, head) maximum and sum, then the unnormalised output.
-__device__ inline float* part_ml(const CacheAttn& a, int split, int r, int h) { return a.ws + (((size_t)split * a.n_rows + r) * a.Hq + h) * 2; }
-template <int DH> __device__ inline float* part_o(const CacheAttn& a, int n_splits, int split, int r, int h) {
-  return a.ws + (size_t)n_splits * a.n_rows * a.Hq * 2 + (((size_t)split * a.n_rows + r) * a.Hq + h) * DH;
+// Blocks of NaN among the values that a column with `vis` visible tokens sees on the page whose first token is t0 (a bit each; every
+// lane of the wavefront calls, each with its own column).
+template <int DH> __device__ inline unsigned nan_blocks(const CacheAttn& a, int page, int kvh, int t0, int len, int vis) {
+  const int lane = threadIdx.x & 63, blk = lane >> 4, tok = lane & 15;
+  bool nan = false;
+  if ((unsigned)page < (unsigned)a.n_pages && blk < DH / 32 && t0 + tok < len)
+    nan = a.pool[((size_t)page * a.Hkv + kvh) * cache_block_bytes(DH) + cache_scale_off(DH, 1, blk, tok)] == 255;
+  const unsigned long long m = __ballot(nan);
+  const unsigned seen = vis > t0 ? 0xffffu >> (16 - min(16, vis - t0)) : 0u;
+  unsigned bits = 0;
+#pragma unroll
+  for (int q = 0; q < DH / 32; ++q) bits |= ((unsigned)(m >> (16 * q)) & seen) ? 1u << q : 0u;
+  return bits;
+}
+
+// Partial results of a split: per (row, head) maximum and sum, then the unnormalised output.  Rows are counted by sequence where that makes
+// fewer than n_rows (a padded batch).
+__device__ inline int part_row(const CacheAttn& a, int r, int b, int i) { return a.ws_rows < a.n_rows ? b * a.max_q + i : r; }
+__device__ inline float* part_ml(const CacheAttn& a, int split, int pr, int h) { return a.ws + (((size_t)split * a.ws_rows + pr) * a.Hq + h) * 2; }
+template <int DH> __device__ inline float* part_o(const CacheAttn& a, int n_splits, int split, int pr, int h) {
+  return a.ws + (size_t)n_splits * a.ws_rows * a.Hq * 2 + (((size_t)split * a.ws_rows + pr) * a.Hq + h) * DH;
 }
 
 // ENGINE: the work list of a decode iteration, entry 0 = {number}, entry 1 + i = {row, split, slot, position} (see launch_sched).
 template <int DH, int CT, bool ENGINE>
-__global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_kernel(CacheAttn a, Split sp, CacheRows er) {
+__global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_attn_kernel(CacheAttn a, Split sp, CacheRows er) {
   constexpr int KC = DH / 32, DT = DH / 16, NV = DH == 128 ? 2 : 1;
   constexpr int VS = DH + 16, OS = DH + 4;            // row strides in LDS: opened values, merged outputs
   constexpr int REC = CT * 16 * (2 + OS);             // floats of a wavefront's result
@@ -554,25 +571,11 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
   }
   if (nan_seen)                                      // some block of this wavefront's values is NaN: mark the columns that see it
 #pragma clang loop unroll(disable)
-    for (int i = 0; i < cnt; ++i) {
-      const int tile = wave + i * CA_WAVES, t0 = t_begin + tile * 32;
-#pragma clang loop unroll(disable)
-      for (int p = 0; p < NV; ++p) {
-        const int pl = min(2 * tile + (DH == 128 ? p : vpage), n_pages - 1), page = bt[pl];
-        const unsigned char e = (unsigned)page < (unsigned)a.n_pages ? a.pool[((size_t)page * a.Hkv + kvh) * cache_block_bytes(DH) + off_vs] : 0;
-        const unsigned long long nan = __ballot(e == 255 && t0 + (DH == 128 ? p : vpage) * 16 + hh < len);
-#pragma clang loop unroll(disable)
-        for (int j = 0; j < 4; ++j)
-#pragma clang loop unroll(disable)
-          for (int pg = DH == 128 ? p : 0; pg < (DH == 128 ? p + 1 : 2); ++pg)
-#pragma clang loop unroll(disable)
-            for (int blk = 0; blk < KC; ++blk) {
-              const int at = 4 * g + j + 16 * (DH == 128 ? blk : pg * KC + blk), t = t0 + pg * 16 + 4 * g + j;
+    for (int i = 0; i < 2 * cnt; ++i) {
+      const int pg = 2 * (wave + (i >> 1) * CA_WAVES) + (i & 1);
+      if (pg >= n_pages) continue;
 #pragma unroll
-              for (int ct = 0; ct < CT; ++ct)
-                if ((nan >> at & 1) && t < vis[ct]) poison[ct] |= 1u << blk;
-            }
-      }
+      for (int ct = 0; ct < CT; ++ct) poison[ct] |= nan_blocks<DH>(a, bt[pg], kvh, t_begin + pg * CACHE_PAGE, len, vis[ct]);
     }
 
   // the wavefronts meet: each publishes (m, l, O), then merges its share of the columns' outputs
@@ -611,6 +614,7 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
     const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;
     if (qi >= nq || (split > 0 && vis[ct] <= t_begin)) continue;
     const bool whole = vis[ct] <= sp.chunk;            // the row's tokens are all in the first split
+    const int pr = part_row(a, r, b, qi);
     for (int d = wave; d < DT; d += CA_WAVES) {
       f32x4 o = f32x4{};
 #pragma unroll
@@ -621,11 +625,11 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 3 : 2) void cache_attn_ker
         for (int e = 0; e < 4; ++e) ob[e] = (bf16_t)(o[e] * inv);
         *reinterpret_cast<bf16x4*>(out_at<DH, ENGINE>(a, r, h, d * 16 + 4 * g)) = ob;
       } else {
-        *reinterpret_cast<f32x4*>(part_o<DH>(a, sp.n, split, r, h) + d * 16 + 4 * g) = o;
+        *reinterpret_cast<f32x4*>(part_o<DH>(a, sp.n, split, pr, h) + d * 16 + 4 * g) = o;
       }
     }
     if (wave == 0 && g == 0) {
-      if (!whole) *reinterpret_cast<float2*>(part_ml(a, split, r, h)) = float2{M, lsum};
+      if (!whole) *reinterpret_cast<float2*>(part_ml(a, split, pr, h)) = float2{M, lsum};
       else if (a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = lsum == 0.f ? -INFINITY : (M + log2f(lsum)) * 0.6931471805599453f;
     }
   }
@@ -644,9 +648,10 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttn a, Split sp, 
   const int n_splits = (len - count + i + sp.chunk) / sp.chunk;
   const int e = blockIdx.y * 256 + threadIdx.x, h = e / (DH / 4), d = 4 * (e % (DH / 4));
   if (h >= a.Hq) return;
-  const float* ml = part_ml(a, 0, r, h);
-  const float* po = part_o<DH>(a, sp.n, 0, r, h) + d;
-  const size_t ml_step = (size_t)a.n_rows * a.Hq * 2, o_step = (size_t)a.n_rows * a.Hq * DH;
+  const int pr = part_row(a, r, b, i);
+  const float* ml = part_ml(a, 0, pr, h);
+  const float* po = part_o<DH>(a, sp.n, 0, pr, h) + d;
+  const size_t ml_step = (size_t)a.ws_rows * a.Hq * 2, o_step = (size_t)a.ws_rows * a.Hq * DH;
   constexpr int U = 4;
   float M = -INFINITY;
   for (int s = 0; s < n_splits; s += 2 * U) {
@@ -692,21 +697,20 @@ template <int DH> dim3 join_grid(const CacheAttn& a, int rows) { return dim3(row
 //   S^T[token, column] = K . Q^T,  O^T[dim, column] = V^T . P^T;
 // the accumulators of the first, rounded to bf16 in place, are the operand of the second, whose V fragment is read transposed.
 // Two stage buffers: while one is worked on, the codes of the next are opened into the other and those of the one behind it
-// requested.  Rows of LDS are not padded; their 16-byte units are permuted by row so that neither the
-// writes (16 tokens of one unit) nor the reads (16 tokens of a unit; 4 tokens of 4 units) meet on a bank.
+// requested.  Rows of LDS are 8 (keys) and 16 (values) elements apart beyond their length, which puts the rows of a read on different
+// banks.  (Units permuted by row instead need an address register for each: with them, and the columns' rows and heads kept
+// through the loop, 48 registers were spilled inside it: 542 and not 354 us for 21 prompts of 1-1999 tokens.)
 // ---------------------------------------------------------------------------
 constexpr int RA_STAGE = 64, RA_COLS = 256;
-
-template <int DH> __device__ inline int k_unit(int row, int u) { return u ^ ((row / (128 / DH)) & (DH / 8 - 1)); }
-template <int DH> __device__ inline int v_unit(int row, int u) { return u ^ (4 * ((row / (128 / DH)) & (DH / 32 - 1))) ^ ((row >> 2) & 3); }
 
 // ENGINE: items {slot, first row of the sequence, its tokens, first position of the tile} of er.q_tile positions (see launch_attn_prefill).
 template <int DH, bool ENGINE>
 __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Split sp, int n_qt, CacheRows er) {
-  constexpr int KC = DH / 16, DT = DH / 32, CT = 2, NB = DH / 32, NV = DH == 128 ? 2 : 1;
+  constexpr int KC = DH / 16, DT = DH / 32, CT = 2, NV = DH == 128 ? 2 : 1;
+  constexpr int KS = DH + 8, VS = DH + 16;                   // row strides in LDS
   constexpr float RESCALE = 8.0f;
-  __shared__ bf16x8 lds[2][2][RA_STAGE * DH / 8];            // [buffer][keys | values][token][16-byte unit]
-  __shared__ unsigned long long s_nan[2][4];                 // blocks of NaN among the values, one bit per block that a wavefront opens
+  __shared__ __align__(16) bf16_t s_k[2][RA_STAGE * KS], s_v[2][RA_STAGE * VS];       // [buffer][token][dim]
+  __shared__ int s_nan;                                      // some block of the values is NaN
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cl = lane & 31, hf = lane >> 5, hh = lane & 15, g = lane >> 4;
   const int G = a.Hq / a.Hkv;
   // KV heads first (different XCDs), the tiles with the most tokens before the others, splits last
@@ -778,41 +782,35 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
       if (value == 1) {
         // zeros behind the context's end, where anything may lie, and for blocks of NaN: the columns that see them are marked
         if (t_begin + st * RA_STAGE + my_row >= len) { c = uint4{0, 0, 0, 0}; e = 127; }
-        const unsigned long long nan = __ballot(opens && e == 255);
-        if (e == 255) { c = uint4{0, 0, 0, 0}; e = 127; }
-        if (lane == 0) s_nan[buf][wave] = nan;
+        if (e == 255) { c = uint4{0, 0, 0, 0}; e = 127; if (opens) s_nan = 1; }
       }
       if (!opens) continue;
-      bf16x8* to = &lds[buf][value][my_row * (DH / 8)];
-      const unsigned w[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int u = my_blk * 4 + j;
-        to[value ? v_unit<DH>(my_row, u) : k_unit<DH>(my_row, u)] = cache_open(w[j], e);
-      }
+      bf16x8* to = reinterpret_cast<bf16x8*>(value ? &s_v[buf][my_row * VS + my_blk * 32] : &s_k[buf][my_row * KS + my_blk * 32]);
+      to[0] = cache_open(c.x, e);
+      to[1] = cache_open(c.y, e);
+      to[2] = cache_open(c.z, e);
+      to[3] = cache_open(c.w, e);
     }
   };
+  if (threadIdx.x == 0) s_nan = 0;
   if (n_stages > 0) request(0);
 
   // queries: column cl of tile ct; lane half hf holds dims 16 c + 8 hf .. + 7
   bf16x8 qf[CT][KC];
-  int vis[CT], vis_first[CT], row[CT], head[CT];
-  bool used[CT];
+  int vis[CT], vis_first[CT];
   int wave_seen = 0;
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
     const int c0 = col0 + wave * 64 + ct * 32, col = c0 + cl, i = col / G;
-    used[ct] = col < n_cols;
-    row[ct] = first + (used[ct] ? i : col0 / G);
-    head[ct] = kvh * G + (col - i * G);
-    vis[ct] = used[ct] ? len - count + i + 1 : 0;
+    const bool used = col < n_cols;
+    vis[ct] = used ? len - count + i + 1 : 0;
     vis_first[ct] = len - count + c0 / G + 1;
     if (c0 < n_cols) wave_seen = max(wave_seen, len - count + min(n_cols - 1, c0 + 31) / G + 1);
-    const bf16_t* q = a.q + row[ct] * a.q_row + head[ct] * a.q_head + 8 * hf;
+    const bf16_t* q = a.q + (first + (used ? i : col0 / G)) * a.q_row + (kvh * G + (col - i * G)) * a.q_head + 8 * hf;
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
       const bf16x8 v = *reinterpret_cast<const bf16x8*>(q + 16 * c);
-      qf[ct][c] = used[ct] ? v : bf16x8{};
+      qf[ct][c] = used ? v : bf16x8{};
     }
   }
   float m_run[CT], l_run[CT];
@@ -824,6 +822,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
 #pragma unroll
     for (int d = 0; d < DT; ++d) oacc[ct][d] = f32x16{};
   }
+  __syncthreads();                                   // (the flag is clear)
   if (n_stages > 0) open(0);
   if (n_stages > 1) request(1);
   __syncthreads();
@@ -839,10 +838,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
       f32x16 sacc[CT];
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) sacc[ct] = f32x16{};
-      const bf16x8* kl = &lds[buf][0][(half * 32 + cl) * (DH / 8)];
+      const bf16_t* kl = &s_k[buf][(half * 32 + cl) * KS + 8 * hf];
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        const bf16x8 kf = kl[k_unit<DH>(half * 32 + cl, 2 * c + hf)];
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kl + 16 * c);
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) sacc[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ct][c], sacc[ct], 0, 0, 0);
       }
@@ -876,51 +875,35 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
         }
         l_run[ct] += sum[0] + sum[1];
       }
-      const bf16_t* vl = reinterpret_cast<const bf16_t*>(&lds[buf][1][0]);
+      const bf16_t* vl = &s_v[buf][(half * 32 + 4 * hf + (hh >> 2)) * VS + 16 * (g & 1) + 4 * (hh & 3)];
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           union { bf16x4 h[2]; bf16x8 v; } vf;
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int r = half * 32 + k * 16 + j * 8 + 4 * hf + (hh >> 2);
-            vf.h[j] = read_transposed(vl + r * DH + v_unit<DH>(r, d * 4 + 2 * (g & 1) + ((hh & 3) >> 1)) * 8 + 4 * (hh & 1));
-          }
+          for (int j = 0; j < 2; ++j) vf.h[j] = read_transposed(vl + (k * 16 + j * 8) * VS + d * 32);
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) oacc[ct][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[ct][k], oacc[ct][d], 0, 0, 0);
         }
     }
-    unsigned long long nan = 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) nan |= (DH == 32 && w != 1) || (DH == 64 && w < 2) ? 0 : s_nan[buf][w];
-    if (__builtin_amdgcn_readfirstlane((int)(nan | nan >> 32))) {
-      int half4 = 4 * hf;
-      asm volatile("" : "+v"(half4));
-#pragma clang loop unroll(disable)
-      for (int j = 0; j < 32; ++j) {                 // this lane's tokens of the stage
-        const int tok = 8 * (j >> 2) + half4 + (j & 3), pg = tok >> 4;
-        const unsigned long long m = DH == 128 ? s_nan[buf][pg] : DH == 64 ? s_nan[buf][2 + (pg >> 1)] >> (32 * (pg & 1)) : s_nan[buf][1] >> (16 * pg);
-#pragma clang loop unroll(disable)
-        for (int blk = 0; blk < NB; ++blk)
-          if (m >> (16 * blk + (tok & 15)) & 1) {
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-              if (ts + tok < vis[ct]) poison[ct] |= 1u << blk;
-          }
-      }
-    }
     __syncthreads();
   }
+  if (s_nan)                                         // (rare: which columns see it)
+#pragma clang loop unroll(disable)
+    for (int pg = 0; pg * CACHE_PAGE < t_end - t_begin; ++pg)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) poison[ct] |= nan_blocks<DH>(a, bt[pg], kvh, t_begin + pg * CACHE_PAGE, len, vis[ct]);
 
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
-    unsigned p = poison[ct] | (unsigned)__shfl_xor((int)poison[ct], 32, 64);
+    unsigned p = poison[ct];
     float l = l_run[ct] + __shfl_xor(l_run[ct], 32, 64);
     if (bad) { l = NAN; p = 15; }
-    if (!used[ct] || (split > 0 && vis[ct] <= t_begin)) continue;
+    const int col = col0 + wave * 64 + ct * 32 + cl, i = col / G;
+    if (col >= n_cols || (split > 0 && vis[ct] <= t_begin)) continue;
     const bool whole = vis[ct] <= sp.chunk;
-    const int r = row[ct], h = head[ct];
+    const int r = first + i, h = kvh * G + (col - i * G), pr = part_row(a, r, b, i);
     const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -936,17 +919,20 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
           for (int e = 0; e < 4; ++e) ob[e] = (bf16_t)(o[e] * inv);
           *reinterpret_cast<bf16x4*>(out_at<DH, ENGINE>(a, r, h, dim)) = ob;
         } else {
-          *reinterpret_cast<f32x4*>(part_o<DH>(a, sp.n, split, r, h) + dim) = o;
+          *reinterpret_cast<f32x4*>(part_o<DH>(a, sp.n, split, pr, h) + dim) = o;
         }
       }
     if (hf == 0) {
-      if (!whole) *reinterpret_cast<float2*>(part_ml(a, split, r, h)) = float2{m_run[ct], l};
+      if (!whole) *reinterpret_cast<float2*>(part_ml(a, split, pr, h)) = float2{m_run[ct], l};
       else if (a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = l == 0.f ? -INFINITY : (m_run[ct] + log2f(l)) * 0.6931471805599453f;
     }
   }
 }
 
-bool few_rows(const CacheAttn& a) { return (long long)a.max_q * (a.Hq / a.Hkv) <= 32; }
+// Up to 64 columns go to the kernel of few rows, whose wavefronts share out the tokens: with all four on the same 64 columns the other one
+// would leave three idle.
+int ws_rows(const CacheAttn& a) { return (int)std::min<long long>(a.n_rows, (long long)a.n_seqs * a.max_q); }
+bool few_rows(const CacheAttn& a) { return (long long)a.max_q * (a.Hq / a.Hkv) <= 64; }
 int row_tiles(const CacheAttn& a) { return (int)(((long long)a.max_q * (a.Hq / a.Hkv) + RA_COLS - 1) / RA_COLS); }
 
 // Splits of the longest context.  Few rows: a split costs its tiles (0.6 to 0.75 us for each 128 tokens of a workgroup that has a compute unit to
@@ -956,11 +942,17 @@ int row_tiles(const CacheAttn& a) { return (int)(((long long)a.max_q * (a.Hq / a
 // 16000 28 | 19.3 | 18.0 | 22.2 | 34.8.  Up to 3 workgroups a compute unit that helps (8 sequences of 4000 19.7 | 16.8 | 16.1 | 21.8 | 31.8); where the
 // sequences alone fill the chip (192 of them and their KV heads, 3/4 of the compute units) it does not (32 of 1000 17.0 | 15.7 | 12.7, of 2000 25 | 21.8 | 20.5 | 19.8, of 16000 163 | 134 | 118 | 115 | 115), and
 // splits are for ragged batches.
+//
+// Many rows: as many splits as fill the two workgroups that a compute unit holds, none shorter than 256 tokens; of whole prompts, whose
+// workgroups see half of the tokens on average, half again as many.  us with 256 | 512 | 1024 | 2048 | 4096 | no splits (32 + 8 heads of 128): 3 sequences of
+// 16384 tokens, 300 rows (120 workgroups) 709 | 498 | 383 | 350 | 327 | 858; one of 8000, 100 rows (16) 50 | 51 | 72 | 120 | 222 | 414; whole prompts:
+// one of 1000 (128) 45 | 49 | 61, of 2000 (256) 114 | 96 | 95 | 114, 768: 85, four of 1000 (512) 123 | 93 | 74.
 Split split_of(const CacheAttn& a) {
   const bool few = few_rows(a);
   const long long groups = std::max<long long>(1, (long long)a.n_seqs * a.Hkv * (few ? 1 : row_tiles(a)));
-  const int least = !few ? 512 : groups >= 192 ? 2048 : a.max_len <= 768 ? 768 : ((int)(8 * std::sqrt((double)a.max_len)) + 127) / 128 * 128;
-  long long n = std::max<long long>(1, std::min<long long>(((few ? 768 : 256) + groups - 1) / groups, (a.max_len + least - 1) / least));
+  const int least = !few ? 256 : groups >= 192 ? 2048 : a.max_len <= 768 ? 768 : ((int)(8 * std::sqrt((double)a.max_len)) + 127) / 128 * 128;
+  const long long most = few ? (768 + groups - 1) / groups : std::max<long long>(1, (2ll * a.max_q > a.max_len ? 768 : 512) / groups);
+  long long n = std::max<long long>(1, std::min<long long>(most, few ? (a.max_len + least - 1) / least : a.max_len / least));
   if (few) n = std::max<long long>(n, (a.max_len + CA_MOST - 1) / CA_MOST);
   Split s;
   s.chunk = (int)std::max<long long>(128, ((a.max_len + n - 1) / n + 127) / 128 * 128);
@@ -969,13 +961,15 @@ Split split_of(const CacheAttn& a) {
   return s;
 }
 
-template <int DH> hipError_t attention(hipStream_t st, const CacheAttn& a) {
+template <int DH> hipError_t attention(hipStream_t st, CacheAttn a) {
   const Split sp = split_of(a);
-  const int n_qt = row_tiles(a);
+  const int n_qt = row_tiles(a), cols = a.max_q * (a.Hq / a.Hkv);
+  a.ws_rows = ws_rows(a);
   const dim3 grid((unsigned)a.Hkv * a.n_seqs * sp.n * (few_rows(a) ? 1 : n_qt));
   hipError_t e = !few_rows(a) ? launch(cache_attn_rows_kernel<DH, false>, grid, dim3(256), st, a, sp, n_qt, CacheRows{})
-                 : a.max_q * (a.Hq / a.Hkv) <= 16 ? launch(cache_attn_kernel<DH, 1, false>, grid, dim3(64 * CA_WAVES), st, a, sp, CacheRows{})
-                                                  : launch(cache_attn_kernel<DH, 2, false>, grid, dim3(64 * CA_WAVES), st, a, sp, CacheRows{});
+                 : cols <= 16 ? launch(cache_attn_kernel<DH, 1, false>, grid, dim3(64 * CA_WAVES), st, a, sp, CacheRows{})
+                 : cols <= 32 ? launch(cache_attn_kernel<DH, 2, false>, grid, dim3(64 * CA_WAVES), st, a, sp, CacheRows{})
+                              : launch(cache_attn_kernel<DH, 4, false>, grid, dim3(64 * CA_WAVES), st, a, sp, CacheRows{});
   if (e == hipSuccess && sp.n > 1) e = launch(cache_join_kernel<DH, false>, join_grid<DH>(a, a.n_seqs * a.max_q), dim3(256), st, a, sp, CacheRows{});
   return e;
 }
@@ -984,7 +978,7 @@ template <int DH> hipError_t attention(hipStream_t st, const CacheAttn& a) {
 
 size_t cache_attention_workspace(const CacheAttn& a, int dh) {
   const Split sp = split_of(a);
-  return sp.n > 1 ? (size_t)sp.n * a.n_rows * a.Hq * (dh + 2) * sizeof(float) : 0;
+  return sp.n > 1 ? (size_t)sp.n * ws_rows(a) * a.Hq * (dh + 2) * sizeof(float) : 0;
 }
 
 // The engine's passes: decode iterations over the scheduler's work list, prefill over its tiles of query positions.  Splits have the

@@ -318,6 +318,21 @@ def test_several_rows_a_sequence(hq, hkv, dh, lens, counts):
     assert np.all(out[starts[-1]:] == 5.0) and np.all(lse[starts[-1]:] == 5.0)
 
 
+@pytest.mark.parametrize("hq,hkv,dh,counts", [(12, 3, 32, [12, 16, 1]), (16, 2, 64, [8, 5, 0]), (14, 2, 128, [9, 1, 6]), (3, 1, 64, [21, 20, 2])])
+def test_up_to_64_columns(hq, hkv, dh, counts):
+    """More than two tiles of 16 columns (rows times heads of a KV head), short contexts and ones of several splits, in a padded batch (the splits'
+    results are then counted by sequence)."""
+    rng = np.random.default_rng([hq, dh, counts[0]])
+    lens = [300, 5000, 9]
+    cache = Cache(rng, lens, hkv, dh)
+    starts = np.concatenate([[0], np.cumsum(counts)])
+    for rows in (starts[-1], 300):
+        q, qv = bf16(rng.standard_normal((rows, hq, dh)) * 2)
+        out, lse, _, _ = attend(cache, q, starts)
+        check_attention(out, lse, qv, starts, cache, 1 / np.sqrt(dh))
+        assert np.all(out[starts[-1]:] == 5.0) and np.all(lse[starts[-1]:] == 5.0)
+
+
 @pytest.mark.parametrize("hq,hkv,dh,lens,counts", [(32, 8, 128, [1500, 700], [1500, 300]), (14, 2, 64, [4300], [90]), (4, 4, 32, [2100, 2], [700, 2]),
                                                    (16, 1, 128, [6000], [33])])
 def test_many_rows_over_long_contexts(hq, hkv, dh, lens, counts):
