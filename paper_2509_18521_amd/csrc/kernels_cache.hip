@@ -220,17 +220,22 @@ __device__ inline bf16x8 cache_open(unsigned c, unsigned e) {
   return o.v;
 }
 
+// A lane's 8 of a block's 32 dimensions: what lets the quad's accesses of 16 bytes lie together.  bf16: 8 part .. + 7; fp32: 4 part .. + 3 and
+// 16 + 4 part .. + 3.
+template <typename T> constexpr int SECOND = sizeof(T) == 2 ? 4 : 16;        // first of its second four, from its first
+template <typename T> __device__ inline int first_dim(int part) { return part * (sizeof(T) == 2 ? 8 : 4); }
+
 template <typename T, bool VEC>
 __device__ inline void load8(const T* p, float (&x)[8]) {
   if constexpr (!VEC) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (float)p[i];
+    for (int i = 0; i < 8; ++i) x[i] = (float)p[i < 4 ? i : SECOND<T> + i - 4];
   } else if constexpr (sizeof(T) == 2) {
     const bf16x8 v = *reinterpret_cast<const bf16x8*>(p);
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
   } else {
-    const f32x4 u = *reinterpret_cast<const f32x4*>(p), v = *reinterpret_cast<const f32x4*>(p + 4);
+    const f32x4 u = *reinterpret_cast<const f32x4*>(p), v = *reinterpret_cast<const f32x4*>(p + SECOND<T>);
 #pragma unroll
     for (int i = 0; i < 4; ++i) { x[i] = u[i]; x[4 + i] = v[i]; }
   }
@@ -241,31 +246,39 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheAppend a) {
   const int nb = a.dh / 32;
   const int unit = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (unit >= a.Hkv * nb) return;
-  const int r = blockIdx.x * 16 + (lane >> 2), part = lane & 3, head = unit / nb, blk = unit % nb;
-  if (r >= a.n_rows) return;
+  const int row = blockIdx.x * 16 + (lane >> 2), r = min(row, a.n_rows - 1), part = lane & 3, head = unit / nb, blk = unit % nb;
+  // (the rows' values are requested with their slots, not behind them)
   const long long slot = a.slot_map[r];
-  if (slot < 0 || slot >= (long long)a.n_pages * CACHE_PAGE) return;
+  float x[2][8];
+  load8<T, VEC>(reinterpret_cast<const T*>(a.k) + r * a.k_row + head * a.k_head + blk * 32 + first_dim<T>(part), x[0]);
+  load8<T, VEC>(reinterpret_cast<const T*>(a.v) + r * a.v_row + head * a.v_head + blk * 32 + first_dim<T>(part), x[1]);
+  __builtin_amdgcn_sched_barrier(0);
+  if (row >= a.n_rows || slot < 0 || slot >= (long long)a.n_pages * CACHE_PAGE) return;
   const int tok = (int)(slot % CACHE_PAGE);
   unsigned char* page = a.pool + ((size_t)(slot / CACHE_PAGE) * a.Hkv + head) * cache_block_bytes(a.dh);
-  float x[2][8];
-  load8<T, VEC>(reinterpret_cast<const T*>(a.k) + r * a.k_row + head * a.k_head + blk * 32 + part * 8, x[0]);
-  load8<T, VEC>(reinterpret_cast<const T*>(a.v) + r * a.v_row + head * a.v_head + blk * 32 + part * 8, x[1]);
+  unsigned e[2];
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
-    unsigned e;
-    const unsigned c = cache_codes(x[q], e);
-    *reinterpret_cast<unsigned*>(page + cache_code_off(a.dh, q, blk, tok) + part * 4) = c;
-    if (part == 0) page[cache_scale_off(a.dh, q, blk, tok)] = (unsigned char)e;
+    const unsigned c = cache_codes(x[q], e[q]);
+    unsigned w = c;                                  // the codes of 8 adjacent dimensions
+    int at = part * 4;
+    if constexpr (sizeof(T) == 4) {                  // pairs of lanes trade: the first halves to the even one, the second halves to the odd one
+      const unsigned other = (unsigned)__builtin_amdgcn_update_dpp(0, (int)c, 0xB1, 0xf, 0xf, false);
+      w = part & 1 ? (other >> 16) | (c & 0xffff0000u) : (c & 0xffffu) | (other << 16);
+      at = (part & 1) * 8 + (part >> 1) * 4;
+    }
+    *reinterpret_cast<unsigned*>(page + cache_code_off(a.dh, q, blk, tok) + at) = w;
     void* values = q ? a.v_values : a.k_values;
     if (values == nullptr) continue;
-    const bf16x8 v = cache_open(c, e);
-    T* dst = reinterpret_cast<T*>(values) + ((size_t)r * a.Hkv + head) * a.dh + blk * 32 + part * 8;
+    const bf16x8 v = cache_open(c, e[q]);
+    T* dst = reinterpret_cast<T*>(values) + ((size_t)r * a.Hkv + head) * a.dh + blk * 32 + first_dim<T>(part);
     if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x8*>(dst) = v;
     else {
 #pragma unroll
-      for (int i = 0; i < 8; i += 4) *reinterpret_cast<f32x4*>(dst + i) = f32x4{(float)v[i], (float)v[i + 1], (float)v[i + 2], (float)v[i + 3]};
+      for (int i = 0; i < 8; i += 4) *reinterpret_cast<f32x4*>(dst + (i ? SECOND<T> : 0)) = f32x4{(float)v[i], (float)v[i + 1], (float)v[i + 2], (float)v[i + 3]};
     }
   }
+  if (part == 0) *reinterpret_cast<unsigned short*>(page + cache_scale_off(a.dh, 0, blk, tok)) = (unsigned short)(e[0] | e[1] << 8);
 }
 
 }  // namespace
