@@ -27,28 +27,37 @@ hipError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t st, A
 // ---------------------------------------------------------------------------
 constexpr int EXT_THREADS = 1024;
 
-// exclusive sum over the workgroup; total: of all of it
+// Exclusive sums of three values over the workgroup, and their totals; the three go through the same two barriers.
 template <typename I>
-__device__ I block_scan(I v, I* s_wave, I& total) {
+__device__ void block_scan(I (&v)[3], I (*s_wave)[EXT_THREADS / 64], I (&total)[3]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  I x = v;
+  I x[3] = {v[0], v[1], v[2]};
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const I y = __shfl_up(x, d, 64);
-    if (lane >= d) x += y;
-  }
-  if (lane == 63) s_wave[wave] = x;
-  __syncthreads();
-  I base = 0;
-  total = 0;
+    I y[3];
 #pragma unroll
-  for (int w = 0; w < EXT_THREADS / 64; ++w) {
-    const I s = s_wave[w];
-    if (w < wave) base += s;
-    total += s;
+    for (int k = 0; k < 3; ++k) y[k] = __shfl_up(x[k], d, 64);
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (lane >= d) x[k] += y[k];
   }
+  __syncthreads();                                   // (the last call's sums have been read)
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    if (lane == 63) s_wave[k][wave] = x[k];
   __syncthreads();
-  return base + x - v;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    I base = 0;
+    total[k] = 0;
+#pragma unroll
+    for (int w = 0; w < EXT_THREADS / 64; ++w) {
+      const I s = s_wave[k][w];
+      if (w < wave) base += s;
+      total[k] += s;
+    }
+    v[k] = base + x[k] - v[k];
+  }
 }
 
 // largest i in 0..n-1 with s[i] <= k (s: exclusive sums, s[0] <= k)
@@ -70,88 +79,123 @@ __device__ inline void put_row(const CacheExtend& a, int r, int page, int pos) {
 // I: int where no sum can pass 31 bits, else long long.  rows: the rows' slots too (else cache_rows_kernel).
 template <typename I>
 __global__ __launch_bounds__(EXT_THREADS) void cache_extend_kernel(CacheExtend a, int rows) {
-  __shared__ I s_wave[EXT_THREADS / 64], s_rel[EXT_THREADS], s_lack[EXT_THREADS], s_row[EXT_THREADS];
-  __shared__ int s_len[EXT_THREADS];
-  const int tid = threadIdx.x, n_chunks = (a.n_seqs + EXT_THREADS - 1) / EXT_THREADS;
+  enum { REL, LACK, ROW };                           // pages given back, pages lacked, rows gained
+  __shared__ I s_wave[3][EXT_THREADS / 64], s_sum[3][EXT_THREADS];
+  __shared__ int s_len[EXT_THREADS], s_flags;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_chunks = (a.n_seqs + EXT_THREADS - 1) / EXT_THREADS;
   const int top = *a.free_top;
   const long long cap = (long long)a.max_pages * CACHE_PAGE;
-  I rel, lack, row, t_rel, t_lack, t_row;           // this thread's sequence: sums before it in its chunk; the chunk's totals
+  I sum[3], total[3];                                // this thread's sequence: sums before it in its chunk; the chunk's totals
   int len, add;
-  bool bad;
+  bool bad = false;
+  if (tid == 0) s_flags = 0;
+  auto table_row = [&](int b) { return a.block_table + (size_t)(a.row_of != nullptr ? a.row_of[b] : b) * a.table_stride; };
+  int last_page = 0;                                 // of this thread's sequence, where it is not full
   auto scan = [&](int chunk) {
     const int b = chunk * EXT_THREADS + tid;
     len = b < a.n_seqs && a.lens != nullptr ? a.lens[b] : 0;
     add = b < a.n_seqs ? a.new_lens[b] : 0;
-    bad = len < 0 || len > cap || (add > 0 && (long long)len + add > cap);
-    const int held = bad ? 0 : (len + CACHE_PAGE - 1) / CACHE_PAGE;
-    const int want = bad || add < 0 ? 0 : (int)(((long long)len + add + CACHE_PAGE - 1) / CACHE_PAGE);
-    rel = block_scan<I>(!bad && add < 0 ? held : 0, s_wave, t_rel);
-    lack = block_scan<I>(want > held ? want - held : 0, s_wave, t_lack);
-    row = block_scan<I>(bad || add < 0 ? 0 : add, s_wave, t_row);
-    s_rel[tid] = rel; s_lack[tid] = lack; s_row[tid] = row; s_len[tid] = len;
+    const bool off = len < 0 || len > cap || (add > 0 && (long long)len + add > cap);
+    bad |= off;
+    if (rows && !off && add > 0 && (len & (CACHE_PAGE - 1))) last_page = table_row(b)[len / CACHE_PAGE];
+    const int held = off ? 0 : (len + CACHE_PAGE - 1) / CACHE_PAGE;
+    const int want = off || add < 0 ? 0 : (int)(((long long)len + add + CACHE_PAGE - 1) / CACHE_PAGE);
+    sum[REL] = !off && add < 0 ? held : 0;
+    sum[LACK] = want > held ? want - held : 0;
+    sum[ROW] = off || add < 0 ? 0 : add;
+    block_scan<I>(sum, s_wave, total);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) s_sum[k][tid] = sum[k];
+    s_len[tid] = len;
     __syncthreads();
   };
-  I all_rel = 0, all_lack = 0, all_row = 0;
-  int any_bad = 0;
+  I all[3] = {0, 0, 0};
   for (int c = 0; c < n_chunks; ++c) {
     scan(c);
-    any_bad |= __syncthreads_or(bad);
-    all_rel += t_rel; all_lack += t_lack; all_row += t_row;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) all[k] += total[k];
   }
-  const long long have = (long long)top + all_rel;
+  // Decode iterations: a thread sees to its sequence's few rows itself, without searches (192 sequences 6.1 and not 7.2 us).
+  constexpr int FEW = 4;
+  if (bad) atomicOr(&s_flags, 1);
+  if (n_chunks > 1 || add > FEW) atomicOr(&s_flags, 2);
+  __syncthreads();
+  const long long have = (long long)top + all[REL];
   int status = 0;
-  if (any_bad || (a.row_of == nullptr && all_row > a.n_rows) || top < 0 || have > a.n_pages) status = 2;
-  else if (all_lack > have) status = 1;
+  if ((s_flags & 1) || (a.row_of == nullptr && all[ROW] > a.n_rows) || top < 0 || have > a.n_pages) status = 2;
+  else if (all[LACK] > have) status = 1;
   if (tid == 0) {
     *a.status = status;
-    *a.free_top_out = status ? top : (int)(have - all_lack);
+    *a.free_top_out = status ? top : (int)(have - all[LACK]);
     if (a.q_start != nullptr) a.q_start[0] = 0;
   }
-  auto table_row = [&](int b) { return a.block_table + (size_t)(a.row_of != nullptr ? a.row_of[b] : b) * a.table_stride; };
   I base = 0;
-  for (int c = 0; c < n_chunks; ++c) {              // lengths, first rows, pages given back
-    if (n_chunks > 1) scan(c);
-    if (status == 0) {
+  if (status == 0 && all[REL] > 0) {                 // pages given back
+    for (int c = 0; c < n_chunks; ++c) {
+      if (n_chunks > 1) scan(c);
       const int n = min(EXT_THREADS, a.n_seqs - c * EXT_THREADS);
-      for (I k = tid; k < t_rel; k += EXT_THREADS) {
-        const int s = find_in(s_rel, n, k);
-        a.free_pages[top + base + k] = table_row(c * EXT_THREADS + s)[k - s_rel[s]];
+      for (I k = tid; k < total[REL]; k += EXT_THREADS) {
+        const int s = find_in(s_sum[REL], n, k);
+        a.free_pages[top + base + k] = table_row(c * EXT_THREADS + s)[k - s_sum[REL][s]];
       }
-      base += t_rel;
+      base += total[REL];
+      if (n_chunks > 1) __syncthreads();             // the sums are used up
     }
-    if (n_chunks > 1) __syncthreads();               // the sums are used up
+    __syncthreads();
   }
-  __syncthreads();
   base = 0;
   I row_base = 0;
-  for (int c = 0; c < n_chunks; ++c) {              // pages taken
+  for (int c = 0; c < n_chunks; ++c) {               // lengths, first rows, pages taken, slots
     if (n_chunks > 1) scan(c);
     const int b = c * EXT_THREADS + tid, n = min(EXT_THREADS, a.n_seqs - c * EXT_THREADS);
     if (b < a.n_seqs) {
       const int now = status ? len : (add < 0 ? 0 : len + add);
       if (a.lens_out != nullptr) a.lens_out[b] = now;
-      if (a.q_start != nullptr) a.q_start[b + 1] = status ? 0 : (int)(row_base + row + (add < 0 ? 0 : add));
+      if (a.q_start != nullptr) a.q_start[b + 1] = status ? 0 : (int)(row_base + sum[ROW] + (add < 0 ? 0 : add));
       if (a.held_of != nullptr && status == 0) a.held_of[a.row_of[b]] = (now + CACHE_PAGE - 1) / CACHE_PAGE;
     }
     if (status == 0) {
-      for (I k = tid; k < t_lack; k += EXT_THREADS) {
-        const int s = find_in(s_lack, n, k);
-        table_row(c * EXT_THREADS + s)[(s_len[s] + CACHE_PAGE - 1) / CACHE_PAGE + (int)(k - s_lack[s])] = a.free_pages[have - 1 - (base + k)];
+      const int* taken = a.free_pages + (have - 1 - base);       // page k of the chunk: taken[-k]
+      if (rows && !(s_flags & 2)) {
+        if (add > 0) {
+          const int held = (len + CACHE_PAGE - 1) / CACHE_PAGE;
+          int page = 0;
+          if (len + add > held * CACHE_PAGE) {
+            page = taken[-(long long)sum[LACK]];
+            table_row(b)[held] = page;
+          }
+#pragma unroll
+          for (int i = 0; i < FEW; ++i)
+            if (i < add) put_row(a, (int)sum[ROW] + i, (len + i) / CACHE_PAGE < held ? last_page : page, len + i);
+        }
+        break;                                       // (one chunk)
       }
-      if (rows) {
-        __syncthreads();
-        for (I k = tid; k < t_row; k += EXT_THREADS) {
-          const int s = find_in(s_row, n, k), pos = s_len[s] + (int)(k - s_row[s]);
-          put_row(a, (int)(row_base + k), table_row(c * EXT_THREADS + s)[pos / CACHE_PAGE], pos);
+      if (total[LACK] <= EXT_THREADS) {
+        if (tid < total[LACK]) {
+          const int s = find_in(s_sum[LACK], n, (I)tid);
+          table_row(c * EXT_THREADS + s)[(s_len[s] + CACHE_PAGE - 1) / CACHE_PAGE + (int)(tid - s_sum[LACK][s])] = taken[-tid];
+        }
+      } else {                                       // prompts: a wavefront per sequence, no searches
+        for (int s = wave; s < n; s += EXT_THREADS / 64) {
+          const I first = s_sum[LACK][s], count = (s + 1 < n ? s_sum[LACK][s + 1] : total[LACK]) - first;
+          if (count == 0) continue;
+          int* to = table_row(c * EXT_THREADS + s) + (s_len[s] + CACHE_PAGE - 1) / CACHE_PAGE;
+          for (I k = lane; k < count; k += 64) to[k] = taken[-(long long)(first + k)];
         }
       }
-      base += t_lack;
-      row_base += t_row;
+      if (rows)
+        for (I k = tid; k < total[ROW]; k += EXT_THREADS) {
+          // (a page taken just now comes from the stack: the table's entry is another thread's)
+          const int s = find_in(s_sum[ROW], n, k), pos = s_len[s] + (int)(k - s_sum[ROW][s]), i = pos / CACHE_PAGE - (s_len[s] + CACHE_PAGE - 1) / CACHE_PAGE;
+          put_row(a, (int)(row_base + k), i < 0 ? table_row(c * EXT_THREADS + s)[pos / CACHE_PAGE] : taken[-(long long)(s_sum[LACK][s] + i)], pos);
+        }
+      base += total[LACK];
+      row_base += total[ROW];
     }
     if (n_chunks > 1) __syncthreads();
   }
   if (rows)
-    for (int r = (status ? 0 : (int)all_row) + tid; r < a.n_rows; r += EXT_THREADS) put_row(a, r, -1, 0);
+    for (int r = (status ? 0 : (int)all[ROW]) + tid; r < a.n_rows; r += EXT_THREADS) put_row(a, r, -1, 0);
 }
 
 // The slots of many rows, one thread each, from what the kernel above has left.
