@@ -350,7 +350,8 @@ int april_cache_append(const april_cache_append_args* args);
  * n_q_heads / n_kv_heads (at most 16) consecutive query heads share a KV head.
  * A row that sees no token is 0 and its lse -infinity.  Rows of no sequence are left as they were.  A NaN in the
  * cache reaches the rows that see it.  A page id outside the pool makes the rows that see a token on it NaN (and
- * may others of their sequence); a length outside 0 .. max_len, or beyond the block table, all rows of its sequence. */
+ * may others of their sequence); a length outside 0 .. max_len, beyond the block table or
+ * beyond 2^30, all rows of its sequence. */
 typedef struct {
   int32_t n_q_heads, n_kv_heads, head_dim;
   int32_t n_pages, n_seqs;

@@ -1,4 +1,5 @@
 // C entry points of the 4-bit KV cache's operators: the arguments' checks, then the launch.  They need no context.
+#include <algorithm>
 #include <cmath>
 
 #include "../../include/april.h"
@@ -29,8 +30,8 @@ int attention_sizes(const april_cache_attention_args* a, CacheAttn* o) {
   o->Hq = a->n_q_heads; o->Hkv = a->n_kv_heads; o->n_pages = a->n_pages; o->n_seqs = a->n_seqs; o->max_pages = a->max_pages;
   o->n_rows = a->n_rows;
   o->max_q = a->max_q < a->n_rows ? a->max_q : (a->n_rows > 0 ? a->n_rows : 1);
-  // (the block table bounds a length too)
-  o->max_len = (int)(a->max_len < (long long)a->max_pages * CACHE_PAGE ? a->max_len : (long long)a->max_pages * CACHE_PAGE);
+  // (the block table bounds a length too, and positions are counted in 30 bits)
+  o->max_len = (int)std::min<long long>({a->max_len, (long long)a->max_pages * CACHE_PAGE, 1ll << 30});
   // workgroups are counted in 31 bits: splits of 128 tokens and tiles of 256 columns bound them from above
   if ((double)a->n_seqs * o->max_q >= 2e9 || (double)a->n_seqs * a->n_kv_heads * ((double)o->max_len / 128 + 1) * ((double)o->max_q * 16 / 256 + 1) >= 2e9)
     REFUSE("april_cache_attention: n_seqs, max_q and max_len bound more work than one call takes");
