@@ -339,7 +339,7 @@ hipError_t launch_cache_append(hipStream_t st, const CacheAppend& a, bool f32) {
 }
 
 // ---------------------------------------------------------------------------
-// Attention of few rows: one workgroup (4 wavefronts) per (sequence, KV head, split of the context), up to 16 CT columns, CT 1, 2 or 4
+// Attention of few rows: one workgroup (W wavefronts) per (sequence, KV head, split of the context), up to 16 CT columns, CT 1, 2 or 4
 // (row of the sequence, query head of the KV head).  The wavefronts take the split's tiles of 32 tokens in turn, each with an online
 // softmax in registers; they meet in LDS, the splits of a context in a second small kernel, both in a fixed order.
 //
@@ -355,7 +355,7 @@ hipError_t launch_cache_append(hipStream_t st, const CacheAppend& a, bool f32) {
 // ---------------------------------------------------------------------------
 namespace {
 
-constexpr int CA_WAVES = 4, CA_MOST = 4096;      // tokens of a split, at most: a lane holds 4 page ids
+constexpr int CA_MOST = 4096;                    // tokens of a split, at most: a lane holds 4 page ids
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 // Four rows (tokens) of 16 bf16 columns each; lane i of 16 points at row i / 4, columns 4 (i % 4).. and gets column i, rows 0..3.
@@ -369,7 +369,7 @@ __device__ inline bf16x4 read_transposed(const bf16_t* p) {
   return u.b;
 }
 
-struct Split { int chunk, n; };                  // tokens of a split, splits of the longest context
+struct Split { int chunk, n, waves; };           // tokens of a split, splits of the longest context, wavefronts of a workgroup (few rows)
 
 // Where a row's head's dimension goes: rows with strides, or (engine) the fragment-tiled layout of the products behind it.
 template <int DH, bool ENGINE> __device__ inline bf16_t* out_at(const CacheAttn& a, int r, int h, int d) {
@@ -410,15 +410,15 @@ template <int DH> __device__ inline float* part_o(const CacheAttn& a, int n_spli
 }
 
 // ENGINE: the work list of a decode iteration, entry 0 = {number}, entry 1 + i = {row, split, slot, position} (see launch_sched).
-template <int DH, int CT, bool ENGINE>
-__global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_attn_kernel(CacheAttn a, Split sp, CacheRows er) {
+template <int DH, int CT, int W, bool ENGINE>
+__global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_attn_kernel(CacheAttn a, Split sp, CacheRows er) {
   constexpr int KC = DH / 32, DT = DH / 16, NV = DH == 128 ? 2 : 1;
   constexpr int VS = DH + 16, OS = DH + 4;            // row strides in LDS: opened values, merged outputs
   constexpr int REC = CT * 16 * (2 + OS);             // floats of a wavefront's result
   constexpr int REGION = REC * 4 > 32 * VS * 2 ? REC * 4 : 32 * VS * 2;
   constexpr float RESCALE = 8.0f;
   typedef typename KRaw<DH>::type kraw_t;
-  __shared__ __align__(16) unsigned char lds[CA_WAVES][REGION];
+  __shared__ __align__(16) unsigned char lds[W][REGION];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane & 15, g = lane >> 4;
   const int G = a.Hq / a.Hkv;
   // KV heads go round first: the heads of one sequence on different XCDs; splits last: only long contexts have the later ones
@@ -467,7 +467,7 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 4 : CT == 2 ? 2 : 1) void 
   uint4 vr[R][NV];
   unsigned ks[R][2], vs[R][NV];
   auto request = [&](int u, int i) {
-    const int tile = min(wave + i * CA_WAVES, n_tiles - 1);
+    const int tile = min(wave + i * W, n_tiles - 1);
     const unsigned char* base[2];
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
@@ -494,7 +494,7 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 4 : CT == 2 ? 2 : 1) void 
       vs[u][0] = vb[off_vs];
     }
   };
-  const int cnt = n_tiles > wave ? (n_tiles - wave + CA_WAVES - 1) / CA_WAVES : 0;
+  const int cnt = n_tiles > wave ? (n_tiles - wave + W - 1) / W : 0;
 #pragma unroll
   for (int u = 0; u < R; ++u)
     if (u < cnt) request(u, u);
@@ -528,7 +528,7 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 4 : CT == 2 ? 2 : 1) void 
   bool nan_seen = false;
 
   auto compute = [&](int u, int i) {
-    const int t0 = t_begin + (wave + i * CA_WAVES) * 32;
+    const int t0 = t_begin + (wave + i * W) * 32;
     // values into LDS: zeros behind the context's end (what lies there is anything) and for blocks of NaN, which would reach
     // columns that do not see them; the columns that do are marked behind the loop
 #pragma unroll
@@ -629,7 +629,7 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 4 : CT == 2 ? 2 : 1) void 
   if (nan_seen)                                      // some block of this wavefront's values is NaN: mark the columns that see it
 #pragma clang loop unroll(disable)
     for (int i = 0; i < 2 * cnt; ++i) {
-      const int pg = 2 * (wave + (i >> 1) * CA_WAVES) + (i & 1);
+      const int pg = 2 * (wave + (i >> 1) * W) + (i & 1);
       if (pg >= n_pages) continue;
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) poison[ct] |= nan_blocks<DH>(a, bt[pg], kvh, t_begin + pg * CACHE_PAGE, len, vis[ct]);
@@ -658,12 +658,12 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 4 : CT == 2 ? 2 : 1) void 
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
     const int col = ct * 16 + hh, qi = col / G, h = kvh * G + col - qi * G, r = first + qi;
-    float M = -INFINITY, wgt[CA_WAVES], lsum = 0.f;
+    float M = -INFINITY, wgt[W], lsum = 0.f;
 #pragma unroll
-    for (int w = 0; w < CA_WAVES; ++w) M = fmaxf(M, reinterpret_cast<const float*>(lds[w])[col]);
+    for (int w = 0; w < W; ++w) M = fmaxf(M, reinterpret_cast<const float*>(lds[w])[col]);
     const float Mu = M == -INFINITY ? 0.f : M;
 #pragma unroll
-    for (int w = 0; w < CA_WAVES; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float* p = reinterpret_cast<const float*>(lds[w]);
       wgt[w] = __builtin_amdgcn_exp2f(p[col] - Mu);
       lsum += wgt[w] * p[CT * 16 + col];
@@ -672,10 +672,10 @@ __global__ __launch_bounds__(64 * CA_WAVES, CT == 1 ? 4 : CT == 2 ? 2 : 1) void 
     if (qi >= nq || (split > 0 && vis[ct] <= t_begin)) continue;
     const bool whole = vis[ct] <= sp.chunk;            // the row's tokens are all in the first split
     const int pr = part_row(a, r, b, qi);
-    for (int d = wave; d < DT; d += CA_WAVES) {
+    for (int d = wave; d < DT; d += W) {
       f32x4 o = f32x4{};
 #pragma unroll
-      for (int w = 0; w < CA_WAVES; ++w) o += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds[w]) + CT * 32 + col * OS + d * 16 + 4 * g) * wgt[w];
+      for (int w = 0; w < W; ++w) o += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds[w]) + CT * 32 + col * OS + d * 16 + 4 * g) * wgt[w];
       if (whole) {
         bf16x4 ob;
 #pragma unroll
@@ -992,13 +992,15 @@ int ws_rows(const CacheAttn& a) { return (int)std::min<long long>(a.n_rows, (lon
 bool few_rows(const CacheAttn& a) { return (long long)a.max_q * (a.Hq / a.Hkv) <= 64; }
 int row_tiles(const CacheAttn& a) { return (int)(((long long)a.max_q * (a.Hq / a.Hkv) + RA_COLS - 1) / RA_COLS); }
 
-// Splits of the longest context.  Few rows: a split costs its tiles (0.6 to 0.75 us for each 128 tokens of a workgroup that has a compute unit to
-// itself) and 0.1 us of the join, which takes 2.5 us besides: together least for about 8 sqrt(length) tokens.  us for one sequence of 32 + 8 heads of
-// 128 in splits of 256 | 512 | 1024 | 2048 | 4096: 1000 tokens 9.2 | 10.4 | 10.9 (whole), 331 7.5 | 5.5 (whole),
-// 2000 10.0 | 10.8 | 13.7 | 17.2, 4000 12.1 | 11.5 | 14.0 | 20.0 | 30.2,
-// 16000 28 | 19.3 | 18.0 | 22.2 | 34.8.  Up to 3 workgroups a compute unit that helps (8 sequences of 4000 19.7 | 16.8 | 16.1 | 21.8 | 31.8); where the
-// sequences alone fill the chip (192 of them and their KV heads, 3/4 of the compute units) it does not (32 of 1000 17.0 | 15.7 | 12.7, of 2000 25 | 21.8 | 20.5 | 19.8, of 16000 163 | 134 | 118 | 115 | 115), and
-// splits are for ragged batches.
+// Splits of the longest context, and the wavefronts that share a split's tiles.  Few rows: 8 wavefronts where the sequences and their KV heads
+// leave compute units with one or two workgroups.  A split saves 0.6 to 0.75 us for each of its 128 tokens and 4 wavefronts and costs 0.1 us of
+// the join, which takes 2.5 us besides: least in all for about 10 sqrt(length) tokens, until the workgroups fill the chip; from 128 sequences and heads on
+// it does not pay below what a workgroup can hold.  us, one row of 32 + 8 heads of 128, 4 wavefronts in splits of 512 | 1024 | 4096, 8 in 512 | 1024 | 4096:
+//   1 sequence of 300 tokens 7.1 (whole), 6.4; 1000 10.6 | 11.0, 9.9 | 9.1; 2000 10.9 | 13.7 | 17.4, 10.1 | 11.7 | 13.3; 4000 11.6 | 14.1 | 30.5, 11.0 | 12.3 | 21.8;
+//     16000 19.7 | 18.2 | 35.2, 19.9 | 16.9 | 26.7
+//   8 of 1000 11.5 | 11.4, 10.6 | 9.7; 4000 16.8 | 16.3 | 32.1, 17.4 | 15.5 | 23.8;   20 of 1000 14.6 | 12.1, 15.4 | 11.0; 4000 26 | 24.6 | 33.3, 30.6 | 26.7 | 25.2
+//   40 of 40 6.0, 6.2; 1000 17.8 | 16.0, 20.3 | 16.1; 4000 47 | 44 | 46, 58 | 47 | 49;   192 of 576-4608 138 | 123 | 125, 177 | 148 | 122
+//   (16 wavefronts: 1 of 4000 11.9 | 12.8 | 20.0, 20 of 4000 46 | 37 | 23.5, 40 of 1000 28 | 21.6.)
 //
 // Many rows: as many splits as fill the two workgroups that a compute unit holds, none shorter than 256 tokens; of whole prompts, whose
 // workgroups see half of the tokens on average, half again as many.  us with 256 | 512 | 1024 | 2048 | 4096 | no splits (32 + 8 heads of 128): 3 sequences of
@@ -1007,14 +1009,15 @@ int row_tiles(const CacheAttn& a) { return (int)(((long long)a.max_q * (a.Hq / a
 Split split_of(const CacheAttn& a) {
   const bool few = few_rows(a);
   const long long groups = std::max<long long>(1, (long long)a.n_seqs * a.Hkv * (few ? 1 : row_tiles(a)));
-  const int least = !few ? 256 : groups >= 192 ? 2048 : a.max_len <= 768 ? 768 : ((int)(8 * std::sqrt((double)a.max_len)) + 127) / 128 * 128;
-  const long long most = few ? (768 + groups - 1) / groups : std::max<long long>(1, (2ll * a.max_q > a.max_len ? 768 : 512) / groups);
+  const int least = !few ? 256 : groups >= 128 ? CA_MOST : a.max_len <= 1152 ? 1152 : ((int)(10 * std::sqrt((double)a.max_len)) + 127) / 128 * 128;
+  const long long most = few ? (640 + groups - 1) / groups : std::max<long long>(1, (2ll * a.max_q > a.max_len ? 768 : 512) / groups);
   long long n = std::max<long long>(1, std::min<long long>(most, few ? (a.max_len + least - 1) / least : a.max_len / least));
   if (few) n = std::max<long long>(n, (a.max_len + CA_MOST - 1) / CA_MOST);
   Split s;
   s.chunk = (int)std::max<long long>(128, ((a.max_len + n - 1) / n + 127) / 128 * 128);
   if (few) s.chunk = std::min(s.chunk, CA_MOST);
   s.n = std::max(1, (a.max_len + s.chunk - 1) / s.chunk);
+  s.waves = groups <= 512 && a.max_len > 128 ? 8 : 4;
   return s;
 }
 
@@ -1024,9 +1027,11 @@ template <int DH> hipError_t attention(hipStream_t st, CacheAttn a) {
   a.ws_rows = ws_rows(a);
   const dim3 grid((unsigned)a.Hkv * a.n_seqs * sp.n * (few_rows(a) ? 1 : n_qt));
   hipError_t e = !few_rows(a) ? launch(cache_attn_rows_kernel<DH, false>, grid, dim3(256), st, a, sp, n_qt, CacheRows{})
-                 : cols <= 16 ? launch(cache_attn_kernel<DH, 1, false>, grid, dim3(64 * CA_WAVES), st, a, sp, CacheRows{})
-                 : cols <= 32 ? launch(cache_attn_kernel<DH, 2, false>, grid, dim3(64 * CA_WAVES), st, a, sp, CacheRows{})
-                              : launch(cache_attn_kernel<DH, 4, false>, grid, dim3(64 * CA_WAVES), st, a, sp, CacheRows{});
+                 : cols <= 16 ? (sp.waves == 8 ? launch(cache_attn_kernel<DH, 1, 8, false>, grid, dim3(512), st, a, sp, CacheRows{})
+                                               : launch(cache_attn_kernel<DH, 1, 4, false>, grid, dim3(256), st, a, sp, CacheRows{}))
+                 : cols <= 32 ? (sp.waves == 8 ? launch(cache_attn_kernel<DH, 2, 8, false>, grid, dim3(512), st, a, sp, CacheRows{})
+                                               : launch(cache_attn_kernel<DH, 2, 4, false>, grid, dim3(256), st, a, sp, CacheRows{}))
+                              : launch(cache_attn_kernel<DH, 4, 4, false>, grid, dim3(256), st, a, sp, CacheRows{});
   if (e == hipSuccess && sp.n > 1) e = launch(cache_join_kernel<DH, false>, join_grid<DH>(a, a.n_seqs * a.max_q), dim3(256), st, a, sp, CacheRows{});
   return e;
 }
@@ -1041,10 +1046,10 @@ size_t cache_attention_workspace(const CacheAttn& a, int dh) {
 // The engine's passes: decode iterations over the scheduler's work list, prefill over its tiles of query positions.  Splits have the
 // engine's length, whatever the batch, so that a rollout's sums depend on its own length alone.
 void launch_cache_decode(hipStream_t st, const CacheAttn& a, int dh, const CacheRows& er, int rows, int chunk, int max_splits, int grid_splits) {
-  const Split sp{chunk, max_splits};
+  const Split sp{chunk, max_splits, 4};
   const dim3 grid((unsigned)rows * grid_splits * a.Hkv);
 #define CACHE_DECODE(DH)                                                                        \
-  launch(cache_attn_kernel<DH, 1, true>, grid, dim3(64 * CA_WAVES), st, a, sp, er);               \
+  launch(cache_attn_kernel<DH, 1, 4, true>, grid, dim3(256), st, a, sp, er);                      \
   if (grid_splits > 1) launch(cache_join_kernel<DH, true>, join_grid<DH>(a, rows), dim3(256), st, a, sp, er)
   switch (dh) {
     case 32: CACHE_DECODE(32); break;
@@ -1055,7 +1060,7 @@ void launch_cache_decode(hipStream_t st, const CacheAttn& a, int dh, const Cache
 }
 void launch_cache_prefill(hipStream_t st, const CacheAttn& a, int dh, const CacheRows& er, int n_items) {
   if (n_items <= 0) return;
-  const Split sp{0x7fffff80, 1};
+  const Split sp{0x7fffff80, 1, 4};
   const dim3 grid((unsigned)n_items * a.Hkv);
   switch (dh) {
     case 32: launch(cache_attn_rows_kernel<32, true>, grid, dim3(256), st, a, sp, 1, er); break;
