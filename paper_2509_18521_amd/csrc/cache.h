@@ -55,8 +55,6 @@ struct CacheRows {
   const int* row_pos;
   int q_tile;
 };
-void launch_cache_decode(hipStream_t st, const CacheAttn& a, int dh, const CacheRows& er, int rows, int chunk, int max_splits, int grid_splits);
-void launch_cache_prefill(hipStream_t st, const CacheAttn& a, int dh, const CacheRows& er, int n_items);
 // Queries rotated to bf16 rows [row][Hq][dh] (Hq 0: none); keys and values (kv_src: a row's keys, then its values) into the rows' pages if `store`.
 struct CacheRope {
   const float *q_src, *kv_src;     // partial p of row r: src + p * partial_stride + r * ld
@@ -68,6 +66,9 @@ struct CacheRope {
   int Hq, store;
 };
 void launch_cache_rope(hipStream_t st, RowCtx rc, Slots s, const CacheRope& f, int dh, int Hkv);
+// f: the kernel does launch_cache_rope's work itself (a.q is not read); its rows' keys and values are then the tokens of this iteration.
+void launch_cache_decode(hipStream_t st, const CacheAttn& a, int dh, const CacheRows& er, int rows, int chunk, int max_splits, int grid_splits, const CacheRope* f);
+void launch_cache_prefill(hipStream_t st, const CacheAttn& a, int dh, const CacheRows& er, int n_items);
 size_t cache_attention_workspace(const CacheAttn& a, int dh);
 hipError_t launch_cache_attention(hipStream_t st, const CacheAttn& a, int dh);
 

@@ -649,7 +649,7 @@ void forward(april_ctx* c, RowCtx rows, RowCtx srows, const int* gather, double 
     bf16_t* q16 = reinterpret_cast<bf16_t*>(c->q_rot);
     const bool pf_attn = c->attn_mfma && gather != nullptr && c->prefill_tiled;
     bool roped = false;
-    // 4-bit cache: the projection leaves fp32 rows (decode: their partial sums), which a kernel of its own rotates and stores
+    // 4-bit cache: the projection leaves fp32 rows (decode: their partial sums), which a kernel of its own (decode: the attention) rotates and stores
     unsigned char* pool4 = static_cast<unsigned char*>(c->kv_pool) + (size_t)l * c->kv4_layer_bytes;
     auto rope4 = [&](RowCtx rc, const float* q_src, int q_ld, const float* kv_src, int kv_ld, int n_part, int n_heads, bool store, double n) {
       ProfScope p(c, KC_ROPE, n * (nqkv * 4.0 + nq * e + 2 * nkv * ekv), 0);
@@ -670,7 +670,7 @@ void forward(april_ctx* c, RowCtx rows, RowCtx srows, const int* gather, double 
       gather_final = nullptr;
     } else if (c->kv4) {
       gemm(KC_GEMM_QKV, rows, c->h_act, nullptr, L.wqkv_s, c->qkv, nqkv, d, sq, c->qkv_stride, B, normed_by_down ? c->ssq : nullptr);
-      rope4(rows, c->qkv, nqkv, c->qkv + nq, nqkv, sq, Hq, true, B);
+      if (gather != nullptr || !c->fuse_rope) rope4(rows, c->qkv, nqkv, c->qkv + nq, nqkv, sq, Hq, true, B);
       roped = true;
     } else if (tile && pf_attn && l + 1 == m.n_layers && last_layer_cut_pays(c, rows.max_rows, srows.max_rows)) {
       // Behind the last layer's keys and values only the sampling rows go on: their queries, then everything, on rows
@@ -715,7 +715,9 @@ void forward(april_ctx* c, RowCtx rows, RowCtx srows, const int* gather, double 
                              cut ? srows.max_rows : c->pf_n_items);
       } else {
         const int gs = std::min(c->attn_max_splits, std::max(1, ceil_div(c->step_max_ctx, c->attn_chunk)));
-        launch_cache_decode(st, ca, dh, CacheRows{c->d_att_items, rows.ctl, rows.row_pos, 0}, rows.max_rows, c->attn_chunk, c->attn_max_splits, gs);
+        const CacheRope f{c->qkv, nullptr, nqkv, 0, sq, c->qkv_stride, c->rope_cos, c->rope_sin, nullptr, pool4, Hq, 1};
+        launch_cache_decode(st, ca, dh, CacheRows{c->d_att_items, rows.ctl, rows.row_pos, 0}, rows.max_rows, c->attn_chunk, c->attn_max_splits, gs,
+                            c->fuse_rope ? &f : nullptr);
       }
     } else if (pf_attn) {
       // prefill: one workgroup per tile of query positions, the keys / values of a prompt are

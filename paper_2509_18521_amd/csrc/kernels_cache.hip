@@ -409,9 +409,12 @@ template <int DH> __device__ inline float* part_o(const CacheAttn& a, int n_spli
   return a.ws + (size_t)n_splits * a.ws_rows * a.Hq * 2 + (((size_t)split * a.ws_rows + pr) * a.Hq + h) * DH;
 }
 
+// Whose rows: a caller's (the operator), or the engine's decode iteration, with the queries given or (fused) with the projection's partials.
+enum { CA_ROWS, CA_ENGINE, CA_FUSED };
 // ENGINE: the work list of a decode iteration, entry 0 = {number}, entry 1 + i = {row, split, slot, position} (see launch_sched).
-template <int DH, int CT, int W, bool ENGINE>
-__global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_attn_kernel(CacheAttn a, Split sp, CacheRows er) {
+template <int DH, int CT, int W, int MODE>
+__global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_attn_kernel(CacheAttn a, Split sp, CacheRows er, CacheRope f) {
+  constexpr bool ENGINE = MODE != CA_ROWS, FUSED = MODE == CA_FUSED;
   constexpr int KC = DH / 32, DT = DH / 16, NV = DH == 128 ? 2 : 1;
   constexpr int VS = DH + 16, OS = DH + 4;            // row strides in LDS: opened values, merged outputs
   constexpr int REC = CT * 16 * (2 + OS);             // floats of a wavefront's result
@@ -419,6 +422,8 @@ __global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_a
   constexpr float RESCALE = 8.0f;
   typedef typename KRaw<DH>::type kraw_t;
   __shared__ __align__(16) unsigned char lds[W][REGION];
+  __shared__ __align__(16) uint4 s_new[FUSED ? 2 * (DH / 32) : 1];       // the new token's codes, key and value, and their scales
+  __shared__ unsigned s_new_scale[FUSED ? 2 * (DH / 32) : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane & 15, g = lane >> 4;
   const int G = a.Hq / a.Hkv;
   // KV heads go round first: the heads of one sequence on different XCDs; splits last: only long contexts have the later ones
@@ -495,9 +500,100 @@ __global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_a
     }
   };
   const int cnt = n_tiles > wave ? (n_tiles - wave + W - 1) / W : 0;
+  auto first_tiles = [&]() {
 #pragma unroll
-  for (int u = 0; u < R; ++u)
-    if (u < cnt) request(u, u);
+    for (int u = 0; u < R; ++u)
+      if (u < cnt) request(u, u);
+  };
+  const bool has_new = FUSED && len > 0 && t_end == len;          // the split of the token that this iteration adds
+  bf16_t* s_q = reinterpret_cast<bf16_t*>(lds);        // [head][DH + 8] until the queries are in registers
+  if (FUSED) {
+    // The workgroup sums the projection's partials of its query heads and rotates them, a pair (i, i + DH / 2) per thread, and in the
+    // last split the new token's key (rotated) and value, "heads" G and G + 1; those are rounded by 4 lanes a block, stored in the page
+    // and kept for the tile that holds them.  The partials are requested before the first tiles, so the sums run while those arrive.
+    // (A kernel of its own for this costs a launch a layer: 96 sequences of 1000 tokens, 8 layers: 0.410 against 0.362 ms an iteration.
+    // Four partials of two pairs at a time: 8 have head dim 128 spill and gain nothing.)
+    constexpr int HALF = DH / 2, U = 2, QB = 4, QS = DH + 8;
+    float* s_kv = reinterpret_cast<float*>(s_q + 16 * QS);               // [key | value][DH]
+    const int n_pairs = (has_new ? G + 2 : G) * HALF, np = f.n_partials, pos = max(len - 1, 0);
+    const float* src = f.q_src + (size_t)first * f.q_ld;
+    const float* cs = f.rope_cos + (size_t)pos * HALF;
+    const float* sn = f.rope_sin + (size_t)pos * HALF;
+    auto trip = [&](int p0, auto requests) {
+      const float* col[U];
+      float cv[U], sv[U], x[U], y[U], vx[U][QB], vy[U][QB];
+      int hd[U], ii[U];
+      auto load = [&](int q0) {
+#pragma unroll
+        for (int q = 0; q < QB; ++q)
+          if (q0 + q < np) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const float* c = col[u] + (size_t)(q0 + q) * f.partial_stride;
+              vx[u][q] = c[0]; vy[u][q] = c[HALF];
+            }
+          }
+      };
+      auto add = [&](int q0) {                         // in the order p = 0, 1, ...
+#pragma unroll
+        for (int q = 0; q < QB; ++q)
+          if (q0 + q < np) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) { x[u] = q0 + q ? x[u] + vx[u][q] : vx[u][q]; y[u] = q0 + q ? y[u] + vy[u][q] : vy[u][q]; }
+          }
+      };
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int e = min(p0 + u * 64 * W + (int)threadIdx.x, n_pairs - 1);
+        hd[u] = e / HALF; ii[u] = e % HALF;
+        col[u] = src + (size_t)(hd[u] < G ? kvh * G + hd[u] : a.Hq + (hd[u] - G) * a.Hkv + kvh) * DH + ii[u];
+        cv[u] = cs[ii[u]]; sv[u] = sn[ii[u]];
+        x[u] = y[u] = 0.f;
+      }
+      load(0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (requests) first_tiles();
+      __builtin_amdgcn_sched_barrier(0);
+      add(0);
+      for (int q0 = QB; q0 < np; q0 += QB) { load(q0); add(q0); }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (p0 + u * 64 * W + (int)threadIdx.x >= n_pairs) continue;
+        const int i = ii[u];
+        const float ra = rope_first(x[u], y[u], cv[u], sv[u]), rb = rope_second(x[u], y[u], cv[u], sv[u]);
+        if (hd[u] < G) {
+          s_q[hd[u] * QS + i] = (bf16_t)ra;
+          s_q[hd[u] * QS + i + HALF] = (bf16_t)rb;
+        } else {
+          const bool key = hd[u] == G;
+          float* to = s_kv + (key ? 0 : DH) + i;
+          to[0] = key ? ra : x[u];
+          to[HALF] = key ? rb : y[u];
+        }
+      }
+    };
+    trip(0, std::true_type{});
+    for (int p0 = U * 64 * W; p0 < n_pairs; p0 += U * 64 * W) trip(p0, std::false_type{});
+    __syncthreads();
+    if (has_new && (int)threadIdx.x < 2 * DH / 8) {
+      const int val = threadIdx.x / (DH / 8), blk = threadIdx.x % (DH / 8) / 4, part = threadIdx.x % 4, tok = pos % CACHE_PAGE, new_page = bt[(pos - t_begin) / CACHE_PAGE];
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = s_kv[val * DH + blk * 32 + part * 8 + i];
+      unsigned e;
+      const unsigned c = cache_codes(x, e);
+      reinterpret_cast<unsigned*>(s_new)[(val * (DH / 32) + blk) * 4 + part] = c;
+      unsigned char* to = f.pool + ((size_t)new_page * a.Hkv + kvh) * cache_block_bytes(DH);
+      const bool in_pool = (unsigned)new_page < (unsigned)a.n_pages;
+      if (in_pool) *reinterpret_cast<unsigned*>(to + cache_code_off(DH, val, blk, tok) + part * 4) = c;
+      if (part == 0) {
+        s_new_scale[val * (DH / 32) + blk] = e;
+        if (in_pool) to[cache_scale_off(DH, val, blk, tok)] = (unsigned char)e;
+      }
+    }
+  } else {
+    first_tiles();
+  }
 
   // queries, and the tokens that each column sees
   bf16x8 qf[CT][KC];
@@ -510,10 +606,11 @@ __global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_a
     const bf16_t* q = a.q + (first + (used ? i : 0)) * a.q_row + (kvh * G + h) * a.q_head + g * (DH / 4);
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
-      const bf16x8 v = *reinterpret_cast<const bf16x8*>(q + 8 * c);
+      const bf16x8 v = *reinterpret_cast<const bf16x8*>(FUSED ? s_q + (used ? h : 0) * (DH + 8) + g * (DH / 4) + 8 * c : q + 8 * c);
       qf[ct][c] = used ? v : bf16x8{};
     }
   }
+  if (FUSED) __syncthreads();                          // (the tiles' memory held the queries)
   const int vis_min = len - count + 1;                // what the sequence's first row sees
   float m_run[CT], l_run[CT];
   unsigned poison[CT];                                // bit: this column sees a NaN among the values of that block
@@ -529,6 +626,19 @@ __global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_a
 
   auto compute = [&](int u, int i) {
     const int t0 = t_begin + (wave + i * W) * 32;
+    if (FUSED && has_new && t0 + 32 >= len) {          // the new token, wherever its page's copy may be
+      const int pp = (len - 1 - t0) >> 4, tin = (len - 1) & 15;
+      if (hh == tin) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+          if (p == pp) {
+            kr[u][p] = *reinterpret_cast<const kraw_t*>(reinterpret_cast<const unsigned char*>(s_new) + kblk * 16 + kbyte);
+            ks[u][p] = s_new_scale[kblk];
+            if (DH == 128) { vr[u][p % NV] = s_new[DH / 32 + vblk]; ks[u][p] |= s_new_scale[DH / 32 + vblk] << 8; }
+          }
+        if (DH != 128 && vpage == pp) { vr[u][0] = s_new[DH / 32 + vblk]; vs[u][0] = s_new_scale[DH / 32 + vblk]; }
+      }
+    }
     // values into LDS: zeros behind the context's end (what lies there is anything) and for blocks of NaN, which would reach
     // columns that do not see them; the columns that do are marked behind the loop
 #pragma unroll
@@ -1027,11 +1137,11 @@ template <int DH> hipError_t attention(hipStream_t st, CacheAttn a) {
   a.ws_rows = ws_rows(a);
   const dim3 grid((unsigned)a.Hkv * a.n_seqs * sp.n * (few_rows(a) ? 1 : n_qt));
   hipError_t e = !few_rows(a) ? launch(cache_attn_rows_kernel<DH, false>, grid, dim3(256), st, a, sp, n_qt, CacheRows{})
-                 : cols <= 16 ? (sp.waves == 8 ? launch(cache_attn_kernel<DH, 1, 8, false>, grid, dim3(512), st, a, sp, CacheRows{})
-                                               : launch(cache_attn_kernel<DH, 1, 4, false>, grid, dim3(256), st, a, sp, CacheRows{}))
-                 : cols <= 32 ? (sp.waves == 8 ? launch(cache_attn_kernel<DH, 2, 8, false>, grid, dim3(512), st, a, sp, CacheRows{})
-                                               : launch(cache_attn_kernel<DH, 2, 4, false>, grid, dim3(256), st, a, sp, CacheRows{}))
-                              : launch(cache_attn_kernel<DH, 4, 4, false>, grid, dim3(256), st, a, sp, CacheRows{});
+                 : cols <= 16 ? (sp.waves == 8 ? launch(cache_attn_kernel<DH, 1, 8, CA_ROWS>, grid, dim3(512), st, a, sp, CacheRows{}, CacheRope{})
+                                               : launch(cache_attn_kernel<DH, 1, 4, CA_ROWS>, grid, dim3(256), st, a, sp, CacheRows{}, CacheRope{}))
+                 : cols <= 32 ? (sp.waves == 8 ? launch(cache_attn_kernel<DH, 2, 8, CA_ROWS>, grid, dim3(512), st, a, sp, CacheRows{}, CacheRope{})
+                                               : launch(cache_attn_kernel<DH, 2, 4, CA_ROWS>, grid, dim3(256), st, a, sp, CacheRows{}, CacheRope{}))
+                              : launch(cache_attn_kernel<DH, 4, 4, CA_ROWS>, grid, dim3(256), st, a, sp, CacheRows{}, CacheRope{});
   if (e == hipSuccess && sp.n > 1) e = launch(cache_join_kernel<DH, false>, join_grid<DH>(a, a.n_seqs * a.max_q), dim3(256), st, a, sp, CacheRows{});
   return e;
 }
@@ -1045,11 +1155,12 @@ size_t cache_attention_workspace(const CacheAttn& a, int dh) {
 
 // The engine's passes: decode iterations over the scheduler's work list, prefill over its tiles of query positions.  Splits have the
 // engine's length, whatever the batch, so that a rollout's sums depend on its own length alone.
-void launch_cache_decode(hipStream_t st, const CacheAttn& a, int dh, const CacheRows& er, int rows, int chunk, int max_splits, int grid_splits) {
+void launch_cache_decode(hipStream_t st, const CacheAttn& a, int dh, const CacheRows& er, int rows, int chunk, int max_splits, int grid_splits, const CacheRope* f) {
   const Split sp{chunk, max_splits, 4};
   const dim3 grid((unsigned)rows * grid_splits * a.Hkv);
 #define CACHE_DECODE(DH)                                                                        \
-  launch(cache_attn_kernel<DH, 1, 4, true>, grid, dim3(256), st, a, sp, er);                      \
+  if (f != nullptr) launch(cache_attn_kernel<DH, 1, 4, CA_FUSED>, grid, dim3(256), st, a, sp, er, *f);           \
+  else launch(cache_attn_kernel<DH, 1, 4, CA_ENGINE>, grid, dim3(256), st, a, sp, er, CacheRope{});                \
   if (grid_splits > 1) launch(cache_join_kernel<DH, true>, join_grid<DH>(a, rows), dim3(256), st, a, sp, er)
   switch (dh) {
     case 32: CACHE_DECODE(32); break;
@@ -1070,7 +1181,7 @@ void launch_cache_prefill(hipStream_t st, const CacheAttn& a, int dh, const Cach
 }
 
 // ---------------------------------------------------------------------------
-// The engine's rotary embedding and store: a workgroup per row.  Sums the projection's partials, rotates the queries (bf16 rows) and
+// The engine's rotary embedding and store where the attention does not do them itself (prompts; APRIL_FUSE_ROPE=0): a workgroup per row.  Sums the projection's partials, rotates the queries (bf16 rows) and
 // the key, and stores key and value in the row's page; they meet in LDS, where a block's 32 dimensions lie together.
 // ---------------------------------------------------------------------------
 namespace {

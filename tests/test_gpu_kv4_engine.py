@@ -97,6 +97,30 @@ def test_contexts_of_several_splits(head_dim, prompt_len):
     parity(ai.Workload("kv4_long", shape, 3, prompt_len, 2, 3, 8, 1.6, 0.4, 3, 8, ai.SAMPLER_GREEDY, 0, 2, 77), 2, 5, 12)
 
 
+@pytest.mark.parametrize("n_q,n_kv,dh,d_model,prompt_len", [(14, 2, 64, 896, 70), (8, 2, 128, 256, 1100), (16, 1, 128, 192, 31), (3, 3, 32, 160, 16)])
+def test_rotary_inside_the_attention_or_before_it(n_q, n_kv, dh, d_model, prompt_len, monkeypatch):
+    """Both sum the projection's partials in one order and round alike, so every logit is the same to the bit."""
+    shape = kv4(ai.ModelShape(2, d_model, n_q, n_kv, dh, 256, 512))
+    w = ai.Workload("kv4_rope", shape, 5, prompt_len, 5, 5, 24, 2.0, 0.5, 4, 24, ai.SAMPLER_GREEDY, 0, 1, 15)
+    weights = ai.make_weights(shape, w.seed)
+    reqs = ai.make_requests(w, 5)
+    logits = []
+    for fused in ("1", "0"):
+        monkeypatch.setenv("APRIL_FUSE_ROPE", fused)
+        ctx = make_engine(w, weights, debug=True)
+        try:
+            for r in reqs:
+                ap().april_debug_watch(ctx, r.request_id, 0, w.max_new)
+            got = run_gpu(ctx, reqs, 5, 5, w.max_new, 1)[0]
+            logits.append({(rid, i): ap().april_debug_logits(ctx, rid, i, shape.vocab)[0]
+                           for rid, t in zip(got["ids"], got["tokens"]) for i in range(len(t))})
+        finally:
+            ap().april_destroy(ctx)
+    assert len(logits[0]) >= 20 and logits[0].keys() == logits[1].keys()
+    for at in logits[0]:
+        np.testing.assert_array_equal(logits[0][at], logits[1][at])
+
+
 def test_many_rows_in_flight():
     shape = kv4(ai.ModelShape(2, 128, 4, 2, 32, 256, 512))
     parity(ai.Workload("kv4_rows", shape, 40, 6, 100, 160, 5, 1.2, 0.4, 2, 5, ai.SAMPLER_GREEDY, 0, 1, 5), 1, 160, 300)
