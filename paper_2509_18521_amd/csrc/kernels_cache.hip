@@ -4,6 +4,7 @@
 #include <tuple>
 
 #include "cache.h"
+#include <float.h>
 
 namespace april {
 
@@ -865,10 +866,47 @@ template <int DH> dim3 join_grid(const CacheAttn& a, int rows) { return dim3(row
 // the accumulators of the first, rounded to bf16 in place, are the operand of the second, whose V fragment is read transposed.
 // Two stage buffers: while one is worked on, the codes of the next are opened into the other and those of the one behind it
 // requested.  Rows of LDS are 8 (keys) and 16 (values) elements apart beyond their length, which puts the rows of a read on different
-// banks.  (Units permuted by row instead need an address register for each: with them, and the columns' rows and heads kept
-// through the loop, 48 registers were spilled inside it: 542 and not 354 us for 21 prompts of 1-1999 tokens.)
-// ---------------------------------------------------------------------------
+// banks.
+// At head dim 128 accumulators and queries take 192 of the 256 registers that two wavefronts a SIMD leave; one register too many
+// has the loop wait for its reload and with it for the codes on their way.  So the codes go past the registers (copied into LDS), and what follows
+// from a lane's number is computed where it is used.  A fragment's read from LDS takes as long as four products, so two are in flight
+// (left to itself the compiler reads into the registers just used, and waits), and the exponentials of a half's second 16
+// tokens run beside the products of its first.  21 prompts of 1-1999 tokens, 32 + 8 heads: 358 us; without
+// spills 325, fragments ahead 317, queries and outputs as whole rows 304, exponentials beside products 288 (797 TFLOP/s).  What is left:
+// queries, outputs and the first stage alone take 110 us (2 x 172 MB), opening and barriers 46; priorities for either kind of phase,
+// three fragments in flight and the codes requested later changed nothing.
 constexpr int RA_STAGE = 64, RA_COLS = 256;
+typedef unsigned u32x4_8 __attribute__((ext_vector_type(4), aligned(8)));      // outputs are 8-byte aligned
+
+__device__ inline void copy_to_lds(const void* src_lane, uint4* lds_base) {      // 64 lanes x 16 bytes, past the registers
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_global_load_lds(src_lane, lds_base, 16, 0, 0);
+#else
+  (void)src_lane; (void)lds_base;
+#endif
+}
+__device__ inline void loads_done() {                // vmcnt(0)
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_s_waitcnt(0x0f70);
+#endif
+  asm volatile("" ::: "memory");
+}
+
+__device__ inline int again(int x) {                 // what is derived from it is computed where it is used, not kept in registers
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(x));
+#endif
+  return x;
+}
+
+__device__ inline float max_of_halves(float x) {      // of lanes l and l ^ 32
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+  return fmaxf(__builtin_bit_cast(float, r[0]), __builtin_bit_cast(float, r[1]));
+#else
+  return x;
+#endif
+}
 
 // ENGINE: items {slot, first row of the sequence, its tokens, first position of the tile} of er.q_tile positions (see launch_attn_prefill).
 template <int DH, bool ENGINE>
@@ -876,9 +914,12 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
   constexpr int KC = DH / 16, DT = DH / 32, CT = 2, NV = DH == 128 ? 2 : 1;
   constexpr int KS = DH + 8, VS = DH + 16;                   // row strides in LDS
   constexpr float RESCALE = 8.0f;
-  __shared__ __align__(16) bf16_t s_k[2][RA_STAGE * KS], s_v[2][RA_STAGE * VS];       // [buffer][token][dim]
+  __shared__ __align__(16) bf16_t s_kv[2 * RA_STAGE * (KS + VS)];
+  bf16_t (*s_k)[RA_STAGE * KS] = reinterpret_cast<bf16_t (*)[RA_STAGE * KS]>(s_kv);                            // [buffer][token][dim]
+  bf16_t (*s_v)[RA_STAGE * VS] = reinterpret_cast<bf16_t (*)[RA_STAGE * VS]>(s_kv + 2 * RA_STAGE * KS);
+  __shared__ __align__(16) uint4 s_raw[4][NV][64];           // the next stage's codes, each wavefront's own
   __shared__ int s_nan;                                      // some block of the values is NaN
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cl = lane & 31, hf = lane >> 5, hh = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cl = lane & 31, hf = lane >> 5;
   const int G = a.Hq / a.Hkv;
   // KV heads first (different XCDs), the tiles with the most tokens before the others, splits last
   const int kvh = (int)(blockIdx.x % a.Hkv);
@@ -911,13 +952,12 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
   const int* bt = a.block_table + (size_t)b * a.table_stride + t_begin / CACHE_PAGE;
 
   // what this thread opens of a stage
-  const int my_pg = DH == 128 ? wave : DH == 64 ? 2 * (wave & 1) + (g >> 1) : g, my_blk = DH == 128 ? g : DH == 64 ? g & 1 : 0;
-  const int my_row = my_pg * CACHE_PAGE + hh;
   const bool opens = DH > 32 || wave < 2;
   int my_page = 0;                                   // page ids of 16 stages, one per lane
-  uint4 code[NV];
   unsigned scale = 127;                              // (dh 128: of the key and, above it, of the value)
   auto request = [&](int st) {
+    const int lane = again(threadIdx.x) & 63, hh = lane & 15, g = lane >> 4;
+    const int my_pg = DH == 128 ? wave : DH == 64 ? 2 * (wave & 1) + (g >> 1) : g, my_blk = DH == 128 ? g : DH == 64 ? g & 1 : 0;
     if ((st & 15) == 0) {
       const int i = st * 4 + lane;
       my_page = bt[i < last_page ? i : last_page];
@@ -931,20 +971,24 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
     const unsigned char* blk = a.pool + ((size_t)page * a.Hkv + kvh) * cache_block_bytes(DH);
     if constexpr (DH == 128) {
 #pragma unroll
-      for (int p = 0; p < NV; ++p) code[p] = *reinterpret_cast<const uint4*>(blk + cache_code_off(DH, p, my_blk, hh));
+      for (int p = 0; p < NV; ++p) copy_to_lds(blk + cache_code_off(DH, p, my_blk, hh), s_raw[wave][p]);
       scale = *reinterpret_cast<const unsigned short*>(blk + cache_scale_off(DH, 0, my_blk, hh));
     } else {
       const int value = DH == 64 ? wave >> 1 : wave;
-      code[0] = *reinterpret_cast<const uint4*>(blk + cache_code_off(DH, value, my_blk, hh));
+      copy_to_lds(blk + cache_code_off(DH, value, my_blk, hh), s_raw[wave][0]);
       scale = blk[cache_scale_off(DH, value, my_blk, hh)];
     }
   };
   auto open = [&](int st) {
+    const int lane = again(threadIdx.x) & 63, hh = lane & 15, g = lane >> 4;
+    const int my_pg = DH == 128 ? wave : DH == 64 ? 2 * (wave & 1) + (g >> 1) : g, my_blk = DH == 128 ? g : DH == 64 ? g & 1 : 0;
+    const int my_row = my_pg * CACHE_PAGE + hh;
     const int buf = st & 1;
+    loads_done();
 #pragma unroll
     for (int p = 0; p < NV; ++p) {
       const int value = DH == 128 ? p : DH == 64 ? wave >> 1 : wave;
-      uint4 c = code[p];
+      uint4 c = s_raw[wave][p][lane];
       unsigned e = DH == 128 ? (p ? scale >> 8 : scale & 255) : scale;
       if (value == 1) {
         // zeros behind the context's end, where anything may lie, and for blocks of NaN: the columns that see them are marked
@@ -962,21 +1006,42 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
   if (threadIdx.x == 0) s_nan = 0;
   if (n_stages > 0) request(0);
 
-  // queries: column cl of tile ct; lane half hf holds dims 16 c + 8 hf .. + 7
+  // Queries: whole rows into LDS, 16 bytes a lane (a row's pieces exchanged by its number: rows apart by a multiple of 256 bytes are then
+  // read from different banks), from there column cl of tile ct; lane half hf holds dims 16 c + 8 hf .. + 7.  Outputs go the same way back.
+  constexpr int P = DH / 8, RPI = 64 / P;                    // pieces of a row, rows of an access
+  bf16_t* s_mine = s_kv + wave * 64 * DH;
+  const int c_first = col0 + wave * 64, i_first = c_first / G, c_rem = c_first - i_first * G;
+  const unsigned inv_g = ((1u << 20) + G - 1) / G;           // (c * inv_g) >> 20 == c / G for c < 64 + G
+  auto head_row = [&](int row, int& i, int& h) {             // of row `row` of the wavefront's 64
+    const int c = c_rem + row, di = (int)((unsigned)c * inv_g >> 20);
+    i = i_first + di; h = kvh * G + c - di * G;
+  };
+  auto swap_piece = [](int row, int piece) { return piece ^ ((row * P / 16) & (P - 1)); };
+  if (c_first < n_cols) {
+#pragma unroll
+    for (int n = 0; n < 64 / RPI; ++n) {
+      const int row = n * RPI + lane / P, piece = swap_piece(row, lane % P);
+      int i, h;
+      head_row(min(row, n_cols - 1 - c_first), i, h);
+      copy_to_lds(a.q + (first + i) * a.q_row + h * a.q_head + 8 * piece, reinterpret_cast<uint4*>(s_mine + n * RPI * DH));
+    }
+  }
+  loads_done();
   bf16x8 qf[CT][KC];
   int vis[CT], vis_first[CT];
   int wave_seen = 0;
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
-    const int c0 = col0 + wave * 64 + ct * 32, col = c0 + cl, i = col / G;
-    const bool used = col < n_cols;
+    const int c0 = c_first + ct * 32, row = ct * 32 + cl;
+    int i, h;
+    head_row(row, i, h);
+    const bool used = c_first + row < n_cols;
     vis[ct] = used ? len - count + i + 1 : 0;
     vis_first[ct] = len - count + c0 / G + 1;
     if (c0 < n_cols) wave_seen = max(wave_seen, len - count + min(n_cols - 1, c0 + 31) / G + 1);
-    const bf16_t* q = a.q + (first + (used ? i : col0 / G)) * a.q_row + (kvh * G + (col - i * G)) * a.q_head + 8 * hf;
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
-      const bf16x8 v = *reinterpret_cast<const bf16x8*>(q + 16 * c);
+      const bf16x8 v = *reinterpret_cast<const bf16x8*>(s_mine + row * DH + 8 * swap_piece(row, 2 * c + hf));
       qf[ct][c] = used ? v : bf16x8{};
     }
   }
@@ -985,7 +1050,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
   f32x16 oacc[CT][DT];
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
-    m_run[ct] = -INFINITY; l_run[ct] = 0.f; poison[ct] = 0;
+    m_run[ct] = -FLT_MAX; l_run[ct] = 0.f; poison[ct] = 0;
 #pragma unroll
     for (int d = 0; d < DT; ++d) oacc[ct][d] = f32x16{};
   }
@@ -1005,54 +1070,95 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
       f32x16 sacc[CT];
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) sacc[ct] = f32x16{};
-      const bf16_t* kl = &s_k[buf][(half * 32 + cl) * KS + 8 * hf];
+      const int ln = again(threadIdx.x) & 63;
+      const bf16_t* kl = &s_k[buf][(half * 32 + (ln & 31)) * KS + 8 * (ln >> 5)];
+      {
+        constexpr int AHEAD = KC < 2 ? KC : 2;
+        bf16x8 kf[KC];
 #pragma unroll
-      for (int c = 0; c < KC; ++c) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kl + 16 * c);
+        for (int c = 0; c < KC; ++c) kf[c] = *reinterpret_cast<const bf16x8*>(kl + 16 * c);
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) sacc[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ct][c], sacc[ct], 0, 0, 0);
+        for (int c = 0; c < KC; ++c)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) sacc[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], qf[ct][c], sacc[ct], 0, 0, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          __builtin_amdgcn_sched_group_barrier(0x8, CT, 0);
+          if (c + AHEAD < KC) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
       }
-      bf16x8 pf[CT][2];
+      float mx[CT];
+      bool grow[CT];
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
         if (t0 + 32 > vis_first[ct]) {               // some column of the tile does not see all 32 tokens
+          const int lim = vis[ct] - t0 - 4 * ((again(threadIdx.x) >> 5) & 1);
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (t0 + 8 * (i >> 2) + 4 * hf + (i & 3) >= vis[ct]) sacc[ct][i] = -INFINITY;
+            if (8 * (i >> 2) + (i & 3) >= lim) sacc[ct][i] = -INFINITY;
         }
-        float mx = sacc[ct][0];
+      }
 #pragma unroll
-        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sacc[ct][i]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.c2;
-        const bool grow = mx > m_run[ct] + RESCALE;
-        if (__any(grow)) {
-          const float corr = grow ? __builtin_amdgcn_exp2f(m_run[ct] - mx) : 1.0f;
-          m_run[ct] = grow ? mx : m_run[ct];
+      for (int ct = 0; ct < CT; ++ct) {
+        mx[ct] = sacc[ct][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx[ct] = fmaxf(mx[ct], sacc[ct][i]);
+        mx[ct] = max_of_halves(mx[ct]) * a.c2;
+        grow[ct] = mx[ct] > m_run[ct] + RESCALE;
+      }
+      if (__any(grow[0] || grow[1])) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          const float corr = grow[ct] ? __builtin_amdgcn_exp2f(m_run[ct] - mx[ct]) : 1.0f;
+          m_run[ct] = grow[ct] ? mx[ct] : m_run[ct];
           l_run[ct] *= corr;
 #pragma unroll
           for (int d = 0; d < DT; ++d) oacc[ct][d] *= corr;
         }
-        const float m = m_run[ct] == -INFINITY ? 0.f : m_run[ct];
-        float sum[2] = {0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float pe = __builtin_amdgcn_exp2f(__fmaf_rn(sacc[ct][i], a.c2, -m));
-          sum[i & 1] += pe;
-          pf[ct][i >> 3][i & 7] = (bf16_t)pe;
-        }
-        l_run[ct] += sum[0] + sum[1];
       }
-      const bf16_t* vl = &s_v[buf][(half * 32 + 4 * hf + (hh >> 2)) * VS + 16 * (g & 1) + 4 * (hh & 3)];
+      bf16x8 pf[CT][2];
+      const int lv = again(threadIdx.x) & 63;
+      const bf16_t* vl = &s_v[buf][(half * 32 + 4 * (lv >> 5) + ((lv & 15) >> 2)) * VS + 16 * (lv >> 4 & 1) + 4 * (lv & 3)];
+      float sum[CT][2] = {};
+      __builtin_amdgcn_sched_barrier(0);
+      {
+        constexpr int VA = 2;
+        union vfrag { bf16x4 h[2]; bf16x8 v; } vf[2 * DT];
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
+        for (int n = 0; n < 2 * DT; ++n)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) vf[n].h[j] = read_transposed(vl + (n / DT * 16 + j * 8) * VS + n % DT * 32);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          union { bf16x4 h[2]; bf16x8 v; } vf;
 #pragma unroll
-          for (int j = 0; j < 2; ++j) vf.h[j] = read_transposed(vl + (k * 16 + j * 8) * VS + d * 32);
+          for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) oacc[ct][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[ct][k], oacc[ct][d], 0, 0, 0);
+            for (int i = 8 * k; i < 8 * k + 8; ++i) {
+              const float pe = __builtin_amdgcn_exp2f(__fmaf_rn(sacc[ct][i], a.c2, -m_run[ct]));
+              sum[ct][i & 1] += pe;
+              pf[ct][k][i & 7] = (bf16_t)pe;
+            }
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) oacc[ct][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k * DT + d].v, pf[ct][k], oacc[ct][d], 0, 0, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * VA, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, 56, 0);
+#pragma unroll
+        for (int n = 0; n < 2 * DT; ++n) {
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            if (n < DT) __builtin_amdgcn_sched_group_barrier(0x2, 7, 0);
+          }
+          if (n + VA < 2 * DT) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) l_run[ct] += sum[ct][0] + sum[ct][1];
     }
     __syncthreads();
   }
@@ -1062,37 +1168,47 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) poison[ct] |= nan_blocks<DH>(a, bt[pg], kvh, t_begin + pg * CACHE_PAGE, len, vis[ct]);
 
+  const int n_mine = min(64, n_cols - c_first), lane_o = again(threadIdx.x) & 63, cl_o = lane_o & 31, hf_o = lane_o >> 5;
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
     unsigned p = poison[ct];
     float l = l_run[ct] + __shfl_xor(l_run[ct], 32, 64);
     if (bad) { l = NAN; p = 15; }
-    const int col = col0 + wave * 64 + ct * 32 + cl, i = col / G;
-    if (col >= n_cols || (split > 0 && vis[ct] <= t_begin)) continue;
+    const int row = ct * 32 + cl_o;
+    int i, h;
+    head_row(row, i, h);
     const bool whole = vis[ct] <= sp.chunk;
-    const int r = first + i, h = kvh * G + (col - i * G), pr = part_row(a, r, b, i);
+    const int r = first + i, pr = part_row(a, r, b, i);
     const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const bool mine = row < n_mine && !(split > 0 && vis[ct] <= t_begin);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int dim = d * 32 + 8 * q + 4 * hf;
+        const int dim = d * 32 + 8 * q + 4 * hf_o;
         f32x4 o;
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = p >> d & 1 ? NAN : oacc[ct][d][4 * q + e];
-        if (whole) {
-          bf16x4 ob;
+        if (mine && !whole) *reinterpret_cast<f32x4*>(part_o<DH>(a, sp.n, split, pr, h) + dim) = o;
+        bf16x4 ob;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) ob[e] = (bf16_t)(o[e] * inv);
-          *reinterpret_cast<bf16x4*>(out_at<DH, ENGINE>(a, r, h, dim)) = ob;
-        } else {
-          *reinterpret_cast<f32x4*>(part_o<DH>(a, sp.n, split, pr, h) + dim) = o;
-        }
+        for (int e = 0; e < 4; ++e) ob[e] = (bf16_t)(o[e] * inv);
+        *reinterpret_cast<bf16x4*>(s_mine + row * DH + 8 * swap_piece(row, dim / 8) + 4 * hf_o) = ob;
       }
-    if (hf == 0) {
+    if (hf_o == 0 && mine) {
       if (!whole) *reinterpret_cast<float2*>(part_ml(a, split, pr, h)) = float2{m_run[ct], l};
       else if (a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = l == 0.f ? -INFINITY : (m_run[ct] + log2f(l)) * 0.6931471805599453f;
     }
+  }
+  asm volatile("" ::: "memory");                     // (LDS serves a wavefront's accesses in their order)
+#pragma unroll
+  for (int n = 0; n < 64 / RPI; ++n) {
+    const int row = n * RPI + lane_o / P, piece = lane_o % P;
+    int i, h;
+    head_row(row, i, h);
+    const int seen_here = len - count + i + 1;
+    if (row >= n_mine || seen_here > sp.chunk || (split > 0 && seen_here <= t_begin)) continue;
+    *reinterpret_cast<u32x4_8*>(out_at<DH, ENGINE>(a, first + i, h, 8 * piece)) = *reinterpret_cast<const u32x4_8*>(s_mine + row * DH + 8 * swap_piece(row, piece));
   }
 }
 
