@@ -39,6 +39,11 @@ hipError_t launch_cache_append(hipStream_t st, const CacheAppend& a, bool f32);
 struct CacheAttn {
   int Hq, Hkv, n_pages, n_seqs, max_pages, n_rows, max_q, max_len;
   float c2;                        // scale * log2(e)
+  float lag;                       // by how much a score may pass the running maximum: its exponential then is 2^8
+  void set_scale(float scale) {
+    c2 = 1.4426950408889634f * scale;
+    lag = 8.0f / c2 < 1e38f ? 8.0f / c2 : 1e38f;
+  }
   long long table_stride, q_row, q_head, out_row, out_head;
   const bf16_t* q;
   const unsigned char* pool;

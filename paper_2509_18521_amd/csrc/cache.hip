@@ -25,7 +25,7 @@ int attention_sizes(const april_cache_attention_args* a, CacheAttn* o) {
     REFUSE("april_cache_attention: n_q_heads must be a multiple of n_kv_heads, at most 16 times it");
   if (a->n_pages < 1 || a->n_seqs < 0 || a->n_rows < 0 || a->max_pages < 1 || a->max_q < 1 || a->max_len < 0)
     REFUSE("april_cache_attention: bad n_pages, n_seqs, n_rows, max_pages, max_q or max_len");
-  if (!(a->scale >= 0.f) || std::isinf(a->scale)) REFUSE("april_cache_attention: scale must be positive, or 0 for 1 / sqrt(head_dim)");
+  if (!(a->scale >= 0.f) || std::isinf(1.4426950408889634f * a->scale)) REFUSE("april_cache_attention: scale must be positive, or 0 for 1 / sqrt(head_dim)");
   *o = CacheAttn{};
   o->Hq = a->n_q_heads; o->Hkv = a->n_kv_heads; o->n_pages = a->n_pages; o->n_seqs = a->n_seqs; o->max_pages = a->max_pages;
   o->n_rows = a->n_rows;
@@ -35,7 +35,7 @@ int attention_sizes(const april_cache_attention_args* a, CacheAttn* o) {
   // workgroups are counted in 31 bits: splits of 128 tokens and tiles of 256 columns bound them from above
   if ((double)a->n_seqs * o->max_q >= 2e9 || (double)a->n_seqs * a->n_kv_heads * ((double)o->max_len / 128 + 1) * ((double)o->max_q * 16 / 256 + 1) >= 2e9)
     REFUSE("april_cache_attention: n_seqs, max_q and max_len bound more work than one call takes");
-  o->c2 = 1.4426950408889634f * (a->scale > 0.f ? a->scale : 1.0f / sqrtf((float)a->head_dim));
+  o->set_scale(a->scale > 0.f ? a->scale : 1.0f / sqrtf((float)a->head_dim));
   return APRIL_OK;
 }
 

@@ -705,7 +705,7 @@ void forward(april_ctx* c, RowCtx rows, RowCtx srows, const int* gather, double 
     if (c->kv4) {
       CacheAttn ca{};
       ca.Hq = Hq; ca.Hkv = Hkv; ca.n_pages = c->n_pages; ca.max_pages = c->max_blocks; ca.n_rows = ca.ws_rows = c->attn_ws_rows; ca.max_q = 1; ca.max_len = c->max_ctx;
-      ca.c2 = 1.4426950408889634f / sqrtf((float)dh);
+      ca.set_scale(1.0f / sqrtf((float)dh));
       ca.table_stride = c->max_blocks; ca.q_row = nq; ca.q_head = dh; ca.q = q16; ca.pool = pool4; ca.block_table = c->ds.block_table;
       ca.out = (bf16_t*)c->attn_out; ca.ws = c->attn_ws;
       ProfScope p(c, KC_ATTN, C * 2.0 * nkv * ekv + B * nq * 2 * e, 4.0 * C * nq);

@@ -420,7 +420,6 @@ __global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_a
   constexpr int VS = DH + 16, OS = DH + 4;            // row strides in LDS: opened values, merged outputs
   constexpr int REC = CT * 16 * (2 + OS);             // floats of a wavefront's result
   constexpr int REGION = REC * 4 > 32 * VS * 2 ? REC * 4 : 32 * VS * 2;
-  constexpr float RESCALE = 8.0f;
   typedef typename KRaw<DH>::type kraw_t;
   __shared__ __align__(16) unsigned char lds[W][REGION];
   __shared__ __align__(16) uint4 s_new[FUSED ? 2 * (DH / 32) : 1];       // the new token's codes, key and value, and their scales
@@ -678,7 +677,8 @@ __global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_a
     }
     __builtin_amdgcn_sched_barrier(0);
     // Softmax in base 2; the running maximum may lag by 2^8 (probabilities then reach 256, which costs no precision), so that a
-    // tile seldom needs a shuffle.  Probabilities are rounded to bf16 for the second product, their sum is not.
+    // tile seldom needs a shuffle.  It is a score, subtracted before the scale: of scores beyond 2^30 a rounded multiple of it would leave
+    // exponents of hundreds.  Probabilities are rounded to bf16 for the second product, their sum is not.
     bf16x8 pf[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
@@ -690,12 +690,12 @@ __global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_a
         for (int e = 0; e < 8; ++e)
           if (t0 + (e >> 2) * 16 + 4 * g + (e & 3) >= vis[ct]) s[e] = -INFINITY;
       }
-      float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7]))) * a.c2;
-      if (__any(mx > m_run[ct] + RESCALE)) {
+      float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+      if (__any(mx > m_run[ct] + a.lag)) {
         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const bool grow = mx > m_run[ct] + RESCALE;
-        const float corr = grow ? __builtin_amdgcn_exp2f(m_run[ct] - mx) : 1.0f;
+        const bool grow = mx > m_run[ct] + a.lag;
+        const float corr = grow ? __builtin_amdgcn_exp2f((m_run[ct] - mx) * a.c2) : 1.0f;
         m_run[ct] = grow ? mx : m_run[ct];
         l_run[ct] *= corr;
 #pragma unroll
@@ -705,7 +705,7 @@ __global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_a
       float sum[2] = {0.f, 0.f};
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float pe = __builtin_amdgcn_exp2f(__fmaf_rn(s[e], a.c2, -m));
+        const float pe = __builtin_amdgcn_exp2f((s[e] - m) * a.c2);
         sum[e & 1] += pe;
         pf[ct][e] = (bf16_t)pe;
       }
@@ -776,7 +776,7 @@ __global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_a
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const float* p = reinterpret_cast<const float*>(lds[w]);
-      wgt[w] = __builtin_amdgcn_exp2f(p[col] - Mu);
+      wgt[w] = __builtin_amdgcn_exp2f((p[col] - Mu) * a.c2);
       lsum += wgt[w] * p[CT * 16 + col];
     }
     const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;
@@ -798,7 +798,7 @@ __global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_a
     }
     if (wave == 0 && g == 0) {
       if (!whole) *reinterpret_cast<float2*>(part_ml(a, split, pr, h)) = float2{M, lsum};
-      else if (a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = lsum == 0.f ? -INFINITY : (M + log2f(lsum)) * 0.6931471805599453f;
+      else if (a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = lsum == 0.f ? -INFINITY : (M * a.c2 + log2f(lsum)) * 0.6931471805599453f;
     }
   }
 }
@@ -844,7 +844,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttn a, Split sp, 
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (s + u < n_splits) {
-        const float w = __builtin_amdgcn_exp2f(v[u].x - Mu);
+        const float w = __builtin_amdgcn_exp2f((v[u].x - Mu) * a.c2);
         lsum += w * v[u].y;
         o += x[u] * w;
       }
@@ -854,7 +854,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttn a, Split sp, 
 #pragma unroll
   for (int q = 0; q < 4; ++q) ob[q] = (bf16_t)(o[q] * inv);
   *reinterpret_cast<bf16x4*>(out_at<DH, ENGINE>(a, r, h, d)) = ob;
-  if (!ENGINE && d == 0 && a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = lsum == 0.f ? -INFINITY : (M + log2f(lsum)) * 0.6931471805599453f;
+  if (!ENGINE && d == 0 && a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = lsum == 0.f ? -INFINITY : (M * a.c2 + log2f(lsum)) * 0.6931471805599453f;
 }
 template <int DH> dim3 join_grid(const CacheAttn& a, int rows) { return dim3(rows, (a.Hq * (DH / 4) + 255) / 256); }
 
@@ -901,8 +901,9 @@ __device__ inline int again(int x) {                 // what is derived from it 
 
 __device__ inline float max_of_halves(float x) {      // of lanes l and l ^ 32
 #if defined(__HIP_DEVICE_COMPILE__)
-  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
-  return fmaxf(__builtin_bit_cast(float, r[0]), __builtin_bit_cast(float, r[1]));
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const unsigned lower = r[0], upper = r[1];
+  return fmaxf(__uint_as_float(lower), __uint_as_float(upper));
 #else
   return x;
 #endif
@@ -913,7 +914,6 @@ template <int DH, bool ENGINE>
 __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Split sp, int n_qt, CacheRows er) {
   constexpr int KC = DH / 16, DT = DH / 32, CT = 2, NV = DH == 128 ? 2 : 1;
   constexpr int KS = DH + 8, VS = DH + 16;                   // row strides in LDS
-  constexpr float RESCALE = 8.0f;
   __shared__ __align__(16) bf16_t s_kv[2 * RA_STAGE * (KS + VS)];
   bf16_t (*s_k)[RA_STAGE * KS] = reinterpret_cast<bf16_t (*)[RA_STAGE * KS]>(s_kv);                            // [buffer][token][dim]
   bf16_t (*s_v)[RA_STAGE * VS] = reinterpret_cast<bf16_t (*)[RA_STAGE * VS]>(s_kv + 2 * RA_STAGE * KS);
@@ -1104,13 +1104,13 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
         mx[ct] = sacc[ct][0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) mx[ct] = fmaxf(mx[ct], sacc[ct][i]);
-        mx[ct] = max_of_halves(mx[ct]) * a.c2;
-        grow[ct] = mx[ct] > m_run[ct] + RESCALE;
+        mx[ct] = max_of_halves(mx[ct]);
+        grow[ct] = mx[ct] > m_run[ct] + a.lag;
       }
       if (__any(grow[0] || grow[1])) {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-          const float corr = grow[ct] ? __builtin_amdgcn_exp2f(m_run[ct] - mx[ct]) : 1.0f;
+          const float corr = grow[ct] ? __builtin_amdgcn_exp2f((m_run[ct] - mx[ct]) * a.c2) : 1.0f;
           m_run[ct] = grow[ct] ? mx[ct] : m_run[ct];
           l_run[ct] *= corr;
 #pragma unroll
@@ -1135,7 +1135,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
           for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
             for (int i = 8 * k; i < 8 * k + 8; ++i) {
-              const float pe = __builtin_amdgcn_exp2f(__fmaf_rn(sacc[ct][i], a.c2, -m_run[ct]));
+              const float pe = __builtin_amdgcn_exp2f((sacc[ct][i] - m_run[ct]) * a.c2);
               sum[ct][i & 1] += pe;
               pf[ct][k][i & 7] = (bf16_t)pe;
             }
@@ -1196,8 +1196,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttn a, Sp
         *reinterpret_cast<bf16x4*>(s_mine + row * DH + 8 * swap_piece(row, dim / 8) + 4 * hf_o) = ob;
       }
     if (hf_o == 0 && mine) {
-      if (!whole) *reinterpret_cast<float2*>(part_ml(a, split, pr, h)) = float2{m_run[ct], l};
-      else if (a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = l == 0.f ? -INFINITY : (m_run[ct] + log2f(l)) * 0.6931471805599453f;
+      if (!whole) *reinterpret_cast<float2*>(part_ml(a, split, pr, h)) = float2{l == 0.f ? -INFINITY : m_run[ct], l};
+      else if (a.lse != nullptr) a.lse[(size_t)r * a.Hq + h] = l == 0.f ? -INFINITY : (m_run[ct] * a.c2 + log2f(l)) * 0.6931471805599453f;
     }
   }
   asm volatile("" ::: "memory");                     // (LDS serves a wavefront's accesses in their order)

@@ -369,6 +369,76 @@ def test_strides_scale_and_first_rows():
     assert np.all(host(out)[[0, 1, 8]] == 5.0) and np.all(host(lse)[[0, 1, 8]] == 5.0)
 
 
+@pytest.mark.parametrize("hq,hkv,dh", [(12, 4, 64), (10, 2, 128), (26, 2, 32)])
+def test_strides_of_many_rows(hq, hkv, dh):
+    """The same for pieces of prompts: results that are 8-byte aligned and no more, heads outermost, rows that belong to nobody."""
+    import torch
+    rng = np.random.default_rng([12, dh])
+    lens, counts = [190, 33, 470], [101, 33, 77]
+    cache = Cache(rng, lens, hkv, dh)
+    starts = np.concatenate([[0], np.cumsum(counts)]) + 3
+    n = int(starts[-1]) + 4
+    q, qv = bf16(rng.standard_normal((n, hq, dh)))
+    wide_q = torch.zeros((hq + 3, n, dh + 8), dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    wide_q[:, 2:2 + hq, 8:] = q
+    wide = torch.full((n, hq + 1, dh + 4), 5.0, dtype=torch.bfloat16, device="cuda")
+    out = wide[:, 1:, 4:]
+    lse = torch.full((n, hq), 5.0, device="cuda")
+    ap().april_cache_attention(wide_q[:, 2:2 + hq, 8:], cache.pool, dev(cache.table), i32(lens), 470, q_start=i32(starts), max_q=120, scale=0.17, out=out, lse=lse)
+    check_attention(host(out), host(lse), qv, starts, cache, float(np.float32(0.17)))
+    nobody = [0, 1, 2, n - 4, n - 3, n - 2, n - 1]
+    assert np.all(host(out)[nobody] == 5.0) and np.all(host(lse)[nobody] == 5.0)
+    assert torch.all(wide[:, 0] == 5.0) and torch.all(wide[:, :, :4] == 5.0)
+
+
+@pytest.mark.parametrize("hq,hkv,dh,count", [(8, 4, 64, 1), (20, 4, 128, 1), (12, 4, 32, 3), (16, 4, 128, 5)])
+def test_many_sequences(hq, hkv, dh, count):
+    """More sequences and KV heads than workgroups of 8 wavefronts are made for; some without rows' tokens, one with a block of NaN."""
+    rng = np.random.default_rng([19, dh, count])
+    lens = [int(x) for x in rng.integers(0, 700, 150)]
+    lens[:4] = [0, 1, 640, 129]
+    cache = Cache(rng, lens, hkv, dh)
+    t = lens[2] - 100
+    cache.pool[int(cache.table[2, t // 16]), 1, 16 * dh + (t % 16) * 2 + 1] = 255
+    q, qv = bf16(rng.standard_normal((len(lens) * count, hq, dh)))
+    starts = np.arange(len(lens) + 1) * count
+    out, lse, _, _ = attend(cache, q, starts)
+    check_attention(out, lse, qv, starts, cache, 1 / np.sqrt(dh), seqs=[b for b in range(len(lens)) if b != 2])
+    g = hq // hkv
+    nan = np.zeros((count, hq, dh), dtype=bool)
+    nan[:, g:2 * g, :32] = True
+    assert np.array_equal(np.isnan(out[starts[2]:starts[3]]), nan)
+
+
+@pytest.mark.parametrize("count", [1, 3, 60])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_near_the_end_of_the_range(sign, count):
+    """Scores of some 1e36, all positive or all negative: a row's output is the value of its largest score, and its lse that score.  err: fp32 sums of
+    64 products of one sign, the scale and lse's change of base, 80 steps of 2^-24."""
+    import torch
+    rng = np.random.default_rng([21, count])
+    hq, hkv, dh, n = 4, 2, 64, 200
+    cache = Cache(rng, [n], hkv, dh)
+    k = torch.as_tensor(np.abs(rng.standard_normal((n, hkv, dh))) * 5e17, dtype=torch.bfloat16).cuda()
+    v = torch.as_tensor(cache.v[0], dtype=torch.bfloat16).cuda()
+    kv, vv = torch.empty_like(k), torch.empty_like(v)
+    slots = [int(cache.table[0, t // 16]) * 16 + t % 16 for t in range(n)]
+    ap().april_cache_append(cache.pool, k, v, dev(np.array(slots, dtype=np.int64)), k_values=kv, v_values=vv)
+    q, qv = bf16(sign * np.abs(rng.standard_normal((count, hq, dh))) * 5e17)
+    out, lse, _, _ = attend(cache, q, np.array([0, count]))
+    rows = 0
+    for i in range(count):
+        for h in range(hq):
+            s = host(kv)[:n - count + i + 1, h // 2] @ qv[i, h] / 8
+            order, err = np.sort(s), 80 * 2.0 ** -24 * np.abs(s).max()
+            if order[-1] - order[-2] <= 4 * err:                # (as good as equal)
+                continue
+            rows += 1
+            assert np.all(np.abs(out[i, h] - host(vv)[np.argmax(s), h // 2]) <= 2.0 ** -8 * np.abs(host(vv)[np.argmax(s), h // 2]))
+            assert abs(lse[i, h] - order[-1]) <= err
+    assert rows > 0.9 * count * hq
+
+
 @pytest.mark.parametrize("count", [1, 3, 40])
 def test_nan_reaches_the_rows_that_see_it_and_no_others(count):
     """A block of NaN keys, one of NaN values, one of each far back, in each of 40 tokens' places: per row and dimension as in the plain form."""
