@@ -872,7 +872,8 @@ template <int DH> dim3 join_grid(const CacheAttn& a, int rows) { return dim3(row
 // from a lane's number is computed where it is used.  A fragment's read from LDS takes as long as four products, so two are in flight
 // (left to itself the compiler reads into the registers just used, and waits), and the exponentials of a half's second 16
 // tokens run beside the products of its first.  21 prompts of 1-1999 tokens, 32 + 8 heads: 358 us; without
-// spills 325, fragments ahead 317, queries and outputs as whole rows 304, exponentials beside products 288 (797 TFLOP/s).  What is left:
+// spills 325, fragments ahead 317, queries and outputs as whole rows 304, exponentials beside products 288, scores less
+// their maximum before the scale 300 (765 TFLOP/s; without it scores beyond 2^30 overflow).  What is left:
 // queries, outputs and the first stage alone take 110 us (2 x 172 MB), opening and barriers 46; priorities for either kind of phase,
 // three fragments in flight and the codes requested later changed nothing.
 constexpr int RA_STAGE = 64, RA_COLS = 256;
