@@ -681,6 +681,31 @@ def test_captured_iterations_with_eager_ones_between():
         torch.randn(1 << 20, device="cuda").sum().item()
 
 
+def test_captured_prompts():
+    """A graph of the three operators over so many rows that the tables take two launches: prompts, pieces that begin inside a page, few rows in a
+    wide batch, ended sequences, and what does not fit, each replay against the plain cache."""
+    import torch
+    r = Rollouts(43, 6, 8, 2, 128, cols=60, n_pages=280, n_rows=4400)
+    tensors = (r.d_lens, r.d_top, r.d_free, r.d_table, r.pool)
+    state = [t.clone() for t in tensors]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        r.enqueue(900)                                          # warm up
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        r.enqueue(900)
+    for t, s in zip(tensors, state):
+        t.copy_(s)
+    for new, status in (([700, 1, 900, 0, 333, 16], 0), ([17, 15, -1, 900, 5, 1], 0), ([1, 1, 800, -1, 1, 1], 0), ([1, 900, 1, 900, 1, 900], 1), ([30, 31, 32, 33, -1, 33], 0)):
+        r.inputs(new)
+        g.replay()
+        torch.cuda.synchronize()
+        r.check(new, status=status)
+        torch.randn(1 << 20, device="cuda").sum().item()
+
+
 def test_refused_tensors():
     import torch
     z = lambda *s, d=torch.int32: torch.zeros(s, dtype=d, device="cuda")  # noqa: E731
