@@ -218,6 +218,7 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(CacheExtend a) {
   if (tid == 0) s_begin = b;
   __syncthreads();
   int sum[2] = {0, 0};                               // pages taken by the sequences before the first row's; by all
+#pragma unroll 4
   for (int s = tid; s < a.n_seqs; s += 256) {
     const int n = a.lens_out[s], lack = pages(n) - pages(n - (a.q_start[s + 1] - a.q_start[s]));
     sum[0] += s < s_begin ? lack : 0;
