@@ -269,7 +269,8 @@ def check_attention(out, lse, q, starts, cache, scale, seqs=None, rows=None):
             gl = lse[r][:m]
             empty = np.isneginf(wl)
             assert np.array_equal(np.isneginf(gl), empty)
-            assert np.all(np.abs(gl - wl)[~empty] <= (score + n * u + 4 * u * (1 + np.abs(wl)))[~empty]), (b, float(np.max(np.abs(gl - wl)[~empty])))
+            gl, wl = gl[~empty], wl[~empty]
+            assert np.all(np.abs(gl - wl) <= score + n * u + 4 * u * (1 + np.abs(wl))), (b, float(np.max(np.abs(gl - wl))))
 
 
 def attend(cache, q, starts, scale=0.0, max_len=None, max_q=None, **kw):
