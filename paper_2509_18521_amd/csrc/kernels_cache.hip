@@ -1258,7 +1258,9 @@ int row_tiles(const CacheAttn& a) { return (int)(((long long)a.max_q * (a.Hq / a
 // Splits of the longest context, and the wavefronts that share a split's tiles.  Few rows: 8 wavefronts where the sequences and their KV heads
 // leave compute units with one or two workgroups.  A split saves 0.6 to 0.75 us for each of its 128 tokens and 4 wavefronts and costs 0.1 us of
 // the join, which takes 2.5 us besides: least in all for about 10 sqrt(length) tokens, until the workgroups fill the chip; from 128 sequences and heads on
-// it does not pay below what a workgroup can hold.  us, one row of 32 + 8 heads of 128, 4 wavefronts in splits of 512 | 1024 | 4096, 8 in 512 | 1024 | 4096:
+// it does not pay below what a workgroup can hold; half of that, up to 1280 workgroups, where the longest context has to be split anyway: 40 of
+// 4000-9000 73 | 68, 30 of 8000-16000 96 | 93, 70 of 1000-9000 with 14 + 2 heads of 64 25 | 21 (but 20 of 1000-4000 24.4 | 25.8, 100 of 500-4000 18.4 | 19.6).
+// us, one row of 32 + 8 heads of 128, 4 wavefronts in splits of 512 | 1024 | 4096, 8 in 512 | 1024 | 4096:
 //   1 sequence of 300 tokens 7.1 (whole), 6.4; 1000 10.6 | 11.0, 9.9 | 9.1; 2000 10.9 | 13.7 | 17.4, 10.1 | 11.7 | 13.3; 4000 11.6 | 14.1 | 30.5, 11.0 | 12.3 | 21.8;
 //     16000 19.7 | 18.2 | 35.2, 19.9 | 16.9 | 26.7
 //   8 of 1000 11.5 | 11.4, 10.6 | 9.7; 4000 16.8 | 16.3 | 32.1, 17.4 | 15.5 | 23.8;   20 of 1000 14.6 | 12.1, 15.4 | 11.0; 4000 26 | 24.6 | 33.3, 30.6 | 26.7 | 25.2
@@ -1272,8 +1274,9 @@ int row_tiles(const CacheAttn& a) { return (int)(((long long)a.max_q * (a.Hq / a
 Split split_of(const CacheAttn& a) {
   const bool few = few_rows(a);
   const long long groups = std::max<long long>(1, (long long)a.n_seqs * a.Hkv * (few ? 1 : row_tiles(a)));
-  const int least = !few ? 256 : groups >= 128 ? CA_MOST : a.max_len <= 1152 ? 1152 : ((int)(10 * std::sqrt((double)a.max_len)) + 127) / 128 * 128;
-  const long long most = few ? (640 + groups - 1) / groups : std::max<long long>(1, (2ll * a.max_q > a.max_len ? 768 : 512) / groups);
+  const bool joined = groups >= 128 && a.max_len > CA_MOST;
+  const int least = !few ? 256 : joined ? CA_MOST / 2 : groups >= 128 ? CA_MOST : a.max_len <= 1152 ? 1152 : ((int)(10 * std::sqrt((double)a.max_len)) + 127) / 128 * 128;
+  const long long most = few ? ((joined ? 1280 : 640) + groups - 1) / groups : std::max<long long>(1, (2ll * a.max_q > a.max_len ? 768 : 512) / groups);
   long long n = std::max<long long>(1, std::min<long long>(most, few ? (a.max_len + least - 1) / least : a.max_len / least));
   if (few) n = std::max<long long>(n, (a.max_len + CA_MOST - 1) / CA_MOST);
   Split s;

@@ -411,6 +411,19 @@ def test_many_sequences(hq, hkv, dh, count):
     assert np.array_equal(np.isnan(out[starts[2]:starts[3]]), nan)
 
 
+@pytest.mark.parametrize("hq,hkv,dh,count", [(14, 2, 64, 1), (8, 4, 128, 1), (4, 4, 32, 5)])
+def test_many_sequences_one_of_them_long(hq, hkv, dh, count):
+    """Contexts so long that the longest is split however many there are, and then in shorter pieces."""
+    rng = np.random.default_rng([20, dh, count])
+    lens = [int(x) for x in rng.integers(0, 300, 66)]
+    lens[7], lens[40], lens[65] = 6001, 2049, 4100
+    cache = Cache(rng, lens, hkv, dh)
+    q, qv = bf16(rng.standard_normal((len(lens) * count, hq, dh)))
+    starts = np.arange(len(lens) + 1) * count
+    out, lse, _, _ = attend(cache, q, starts)
+    check_attention(out, lse, qv, starts, cache, 1 / np.sqrt(dh))
+
+
 @pytest.mark.parametrize("count", [1, 3, 60])
 @pytest.mark.parametrize("sign", [1, -1])
 def test_scores_near_the_end_of_the_range(sign, count):
