@@ -351,7 +351,10 @@ int april_cache_append(const april_cache_append_args* args);
  * A row that sees no token is 0 and its lse -infinity.  Rows of no sequence are left as they were.  A NaN in the
  * cache reaches the rows that see it.  A page id outside the pool makes the rows that see a token on it NaN (and
  * may others of their sequence); a length outside 0 .. max_len, beyond the block table or
- * beyond 2^30, all rows of its sequence. */
+ * beyond 2^30, all rows of its sequence.
+ * Sizes that bound more work than one launch takes are refused (APRIL_EINVAL, here and by the workspace query): 2^24 workgroups,
+ * of which each KV head of a sequence has one, or one for every 256 of max_q x (query heads of the KV head) where those are more than 64, and
+ * that for every split of max_len tokens (at most 4096 a split up to those 64); where there are splits, 2^24 rows n_seqs x max_q. */
 typedef struct {
   int32_t n_q_heads, n_kv_heads, head_dim;
   int32_t n_pages, n_seqs;

@@ -74,6 +74,7 @@ void launch_cache_rope(hipStream_t st, RowCtx rc, Slots s, const CacheRope& f, i
 // f: the kernel does launch_cache_rope's work itself (a.q is not read); its rows' keys and values are then the tokens of this iteration.
 void launch_cache_decode(hipStream_t st, const CacheAttn& a, int dh, const CacheRows& er, int rows, int chunk, int max_splits, int grid_splits, const CacheRope* f);
 void launch_cache_prefill(hipStream_t st, const CacheAttn& a, int dh, const CacheRows& er, int n_items);
+bool cache_attention_fits(const CacheAttn& a);       // of the sizes alone; workspace and launch only where it is true
 size_t cache_attention_workspace(const CacheAttn& a, int dh);
 hipError_t launch_cache_attention(hipStream_t st, const CacheAttn& a, int dh);
 

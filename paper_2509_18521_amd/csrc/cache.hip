@@ -32,9 +32,7 @@ int attention_sizes(const april_cache_attention_args* a, CacheAttn* o) {
   o->max_q = a->max_q < a->n_rows ? a->max_q : (a->n_rows > 0 ? a->n_rows : 1);
   // (the block table bounds a length too, and positions are counted in 30 bits)
   o->max_len = (int)std::min<long long>({a->max_len, (long long)a->max_pages * CACHE_PAGE, 1ll << 30});
-  // workgroups are counted in 31 bits: splits of 128 tokens and tiles of 256 columns bound them from above
-  if ((double)a->n_seqs * o->max_q >= 2e9 || (double)a->n_seqs * a->n_kv_heads * ((double)o->max_len / 128 + 1) * ((double)o->max_q * 16 / 256 + 1) >= 2e9)
-    REFUSE("april_cache_attention: n_seqs, max_q and max_len bound more work than one call takes");
+  if (!cache_attention_fits(*o)) REFUSE("april_cache_attention: n_seqs, n_kv_heads, max_q and max_len bound more work than one call takes");
   o->set_scale(a->scale > 0.f ? a->scale : 1.0f / sqrtf((float)a->head_dim));
   return APRIL_OK;
 }

@@ -1283,15 +1283,18 @@ Split split_of(const CacheAttn& a) {
   s.chunk = (int)std::max<long long>(128, ((a.max_len + n - 1) / n + 127) / 128 * 128);
   if (few) s.chunk = std::min(s.chunk, CA_MOST);
   s.n = std::max(1, (a.max_len + s.chunk - 1) / s.chunk);
-  s.waves = groups <= 512 && a.max_len > 128 ? 8 : 4;
+  s.waves = groups <= 512 && a.max_len > 128 && (long long)a.max_q * (a.Hq / a.Hkv) <= 32 ? 8 : 4;
   return s;
 }
 
+long long attention_groups(const CacheAttn& a, const Split& sp) { return (long long)a.Hkv * a.n_seqs * sp.n * (few_rows(a) ? 1 : row_tiles(a)); }
+
 template <int DH> hipError_t attention(hipStream_t st, CacheAttn a) {
   const Split sp = split_of(a);
-  const int n_qt = row_tiles(a), cols = a.max_q * (a.Hq / a.Hkv);
+  const int n_qt = row_tiles(a);
+  const long long cols = (long long)a.max_q * (a.Hq / a.Hkv);
   a.ws_rows = ws_rows(a);
-  const dim3 grid((unsigned)a.Hkv * a.n_seqs * sp.n * (few_rows(a) ? 1 : n_qt));
+  const dim3 grid((unsigned)attention_groups(a, sp));
   hipError_t e = !few_rows(a) ? launch(cache_attn_rows_kernel<DH, false>, grid, dim3(256), st, a, sp, n_qt, CacheRows{})
                  : cols <= 16 ? (sp.waves == 8 ? launch(cache_attn_kernel<DH, 1, 8, CA_ROWS>, grid, dim3(512), st, a, sp, CacheRows{}, CacheRope{})
                                                : launch(cache_attn_kernel<DH, 1, 4, CA_ROWS>, grid, dim3(256), st, a, sp, CacheRows{}, CacheRope{}))
@@ -1303,6 +1306,14 @@ template <int DH> hipError_t attention(hipStream_t st, CacheAttn a) {
 }
 
 }  // namespace
+
+// Whether the launches of a call are: a dimension of a grid has fewer than 2^32 threads.
+bool cache_attention_fits(const CacheAttn& a) {
+  // (before splits, in floating point: nothing below this bound overflows)
+  if ((double)a.n_seqs * a.Hkv * (few_rows(a) ? 1.0 : (double)row_tiles(a)) * 256 >= 4294967296.0) return false;
+  const Split sp = split_of(a);
+  return attention_groups(a, sp) * 64 * (few_rows(a) ? sp.waves : 4) < 1ll << 32 && (sp.n == 1 || (long long)a.n_seqs * a.max_q * 256 < 1ll << 32);
+}
 
 size_t cache_attention_workspace(const CacheAttn& a, int dh) {
   const Split sp = split_of(a);

@@ -57,6 +57,34 @@ def test_attention_needs_its_workspace():
     assert "head_dim" in refused(lib.april_cache_attention_workspace, attention_args(head_dim=96))
 
 
+# A launch has fewer than 2^32 threads in a dimension.  The largest that fits, the first that does not, and which of them it is:
+# tiles of 256 columns, workgroups of 256 threads; sequences alone; their splits (two for 5000 tokens, 8 for 32768); the join's workgroup a row.
+LAUNCHES = [(dict(n_q_heads=32, n_kv_heads=8, n_seqs=4096, max_len=2048, n_rows=1 << 20), "max_q", 511 * 64, 511 * 64 + 1),
+            (dict(n_q_heads=32, n_kv_heads=8, n_seqs=2048, max_len=2048, n_rows=1 << 20), "max_q", 1023 * 64, 1023 * 64 + 1),
+            (dict(n_q_heads=1, n_kv_heads=1, n_rows=1 << 25, max_len=60), "n_seqs", (1 << 24) - 1, 1 << 24),
+            (dict(n_q_heads=4, n_kv_heads=4, n_rows=1 << 25, max_len=5000), "n_seqs", (1 << 21) - 1, 1 << 21),
+            (dict(n_q_heads=4, n_kv_heads=4, n_rows=1 << 25, max_len=32768), "n_seqs", (1 << 19) - 1, 1 << 19),
+            (dict(n_q_heads=1, n_kv_heads=1, n_rows=1 << 25, max_len=5000, max_q=64), "n_seqs", (1 << 18) - 1, 1 << 18),
+            (dict(n_q_heads=65536, n_kv_heads=65536, n_rows=1 << 30, max_q=1 << 30, n_seqs=1 << 30), "max_len", None, 0)]
+
+
+@pytest.mark.parametrize("sizes,name,fits,first", LAUNCHES)
+def test_attention_larger_than_a_launch(sizes, name, fits, first):
+    lib = ap.load_library()
+    sizes = dict(dict(max_pages=4096, table_stride=4096), **sizes)
+    if fits is not None:
+        assert lib.april_cache_attention_workspace(C.byref(attention_args(**sizes, **{name: fits}))) >= 0
+    args = attention_args(**sizes, **{name: first})
+    for call in (lib.april_cache_attention_workspace, lib.april_cache_attention):
+        assert "more work than one call takes" in refused(call, args)
+
+
+def test_long_contexts_of_many_rows_that_fit_a_launch():
+    """2064384 workgroups: far below the limit, whatever the bounds on rows and length would allow together."""
+    a = attention_args(n_q_heads=32, n_kv_heads=8, n_seqs=4096, max_q=4000, n_rows=1 << 20, max_len=32768, max_pages=4096, table_stride=4096)
+    assert ap.load_library().april_cache_attention_workspace(C.byref(a)) == 0
+
+
 @pytest.mark.parametrize("over", [
     dict(head_dim=48), dict(n_pages=0), dict(n_kv_heads=0), dict(n_rows=-1), dict(dtype=2), dict(reserved=1), dict(k=None), dict(v=None), dict(slot_map=None),
     dict(pool=None), dict(pool=P + 4), dict(slot_map=P + 4), dict(k=P + 1), dict(v=P + 1), dict(dtype=0, k=P + 2), dict(k_values=P + 8), dict(v_values=P + 8)])
