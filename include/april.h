@@ -331,7 +331,8 @@ int april_cache_extend(const april_cache_extend_args* args);
  * them).  Rows whose slot lies outside the pool are left out; two rows with the same slot leave one of them,
  * or parts of both. */
 typedef struct {
-  int32_t n_pages, n_kv_heads, head_dim, n_rows;
+  int32_t n_pages, n_kv_heads, head_dim;
+  int32_t n_rows;                /* at most 2^28 - 16                                          */
   int32_t dtype;                 /* APRIL_DTYPE_* of k, v and the values                       */
   int32_t reserved;              /* 0                                                          */
   int64_t k_row, k_head, v_row, v_head;   /* elements between rows and heads; dimensions are adjacent.

@@ -66,6 +66,7 @@ int april_cache_append(const april_cache_append_args* a) {
   if (!head_dim_ok(a->head_dim)) REFUSE("april_cache_append: head_dim must be 32, 64 or 128");
   if (a->n_pages < 1 || a->n_kv_heads < 1 || a->n_kv_heads > 4096 || a->n_rows < 0)
     REFUSE("april_cache_append: n_pages must be positive, n_kv_heads in 1..4096, n_rows not negative");
+  if (a->n_rows > 16 * ((1 << 24) - 1)) REFUSE("april_cache_append: n_rows beyond 2^28 - 16");      // (16 a workgroup; a launch has fewer than 2^32 threads)
   if (a->dtype != APRIL_DTYPE_FP32 && a->dtype != APRIL_DTYPE_BF16) REFUSE("april_cache_append: bad dtype");
   if (a->reserved) REFUSE("april_cache_append: reserved must be 0");
   if (a->n_rows == 0) return APRIL_OK;

@@ -92,6 +92,11 @@ def test_append(over):
     assert "april_cache_append" in refused(ap.load_library().april_cache_append, append_args(**over))
 
 
+@pytest.mark.parametrize("rows", [(1 << 28) - 15, 1 << 30, (1 << 31) - 1])
+def test_append_larger_than_a_launch(rows):
+    assert "n_rows" in refused(ap.load_library().april_cache_append, append_args(n_rows=rows))
+
+
 @pytest.mark.parametrize("over", [
     dict(n_seqs=0), dict(n_seqs=65537), dict(max_pages=0), dict(max_pages=(1 << 27) + 1), dict(n_pages=0), dict(n_rows=-1), dict(table_stride=3), dict(slot_map=P + 4)] +
     [{n: None} for n in ("lens", "new_lens", "free_top", "block_table", "free_pages", "lens_out", "free_top_out", "q_start", "slot_map", "positions", "status")])
