@@ -252,7 +252,7 @@ hipError_t launch_cache_extend(hipStream_t st, const CacheExtend& a) {
   const int what = rows ? EXT_ROWS : a.n_rows > 0 ? EXT_SUMS : EXT_PAGES;
   hipError_t e = small ? launch(cache_extend_kernel<int>, dim3(1), dim3(EXT_THREADS), st, a, what)
                        : launch(cache_extend_kernel<long long>, dim3(1), dim3(EXT_THREADS), st, a, what);
-  if (e == hipSuccess && what == EXT_SUMS) e = launch(cache_rows_kernel, dim3((a.n_rows + 255) / 256), dim3(256), st, a);
+  if (e == hipSuccess && what == EXT_SUMS) e = launch(cache_rows_kernel, dim3(((unsigned)a.n_rows + 255) / 256), dim3(256), st, a);
   return e;
 }
 

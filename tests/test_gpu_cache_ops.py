@@ -211,6 +211,22 @@ def test_refused_tables_change_nothing(what, status, n, rows):
     assert np.array_equal(host(tab), before[0]) and np.array_equal(host(stack), before[1])
 
 
+def test_tables_of_as_many_rows_as_are_counted():
+    """slot_map and positions of 2^31 - 1 entries (26 GB): the two of one sequence, and what lies behind them."""
+    import torch
+    n_rows, few = (1 << 31) - 1, 40
+    out = [torch.empty(s, dtype=torch.int32, device="cuda") for s in (1, 1, 2)]
+    out += [torch.full((n_rows,), 7, dtype=torch.int64, device="cuda"), torch.full((n_rows,), 7, dtype=torch.int32, device="cuda"), i32([7])]
+    table = i32([[5, -9, -9, -9]])
+    got = ap().april_cache_extend(i32([3]), i32([few]), table, i32([9, 8, 7, 6]), i32([3]), n_rows, out=out)
+    assert int(got.status) == 0 and host(got.q_start).tolist() == [0, few] and host(table).tolist() == [[5, 7, 8, -9]] and int(got.free_top) == 1
+    pos = np.arange(3, 3 + few)
+    assert host(got.positions[:few]).tolist() == pos.tolist()
+    assert host(got.slot_map[:few]).tolist() == (np.array([5, 7, 8])[pos // 16] * 16 + pos % 16).tolist()
+    for t in (got.slot_map, got.positions):
+        assert all(int(t[a:a + (1 << 28)].max()) == int(t[a:a + (1 << 28)].min()) == -1 for a in range(few, n_rows, 1 << 28))
+
+
 # --- attention -----------------------------------------------------------------------------------------------------------
 
 
