@@ -319,9 +319,9 @@ typedef struct {
   int32_t* q_start;              /* [n_seqs + 1] first row of each sequence's new tokens       */
   int64_t* slot_map;             /* [n_rows] page * 16 + token of each row; -1 behind the last */
   int32_t* positions;            /* [n_rows] position in its sequence; -1 behind the last      */
-  int32_t* status;               /* [1] 0; 1: too few free pages; 2: a length below zero or beyond the
-                                    block table, more rows than n_rows, or a stack that does not fit its
-                                    array.  Not 0: nothing was entered or taken, lens_out = lens,
+  int32_t* status;               /* [1] 0; 1: too few free pages; 2: a length below zero, beyond the
+                                    block table or beyond 2^31 - 16, more rows than n_rows, or a stack that
+                                    does not fit its array.  Not 0: nothing was entered or taken, lens_out = lens,
                                     free_top_out = free_top, no rows (q_start 0, slots and positions -1) */
   void* stream;
 } april_cache_extend_args;

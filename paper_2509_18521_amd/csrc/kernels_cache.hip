@@ -88,7 +88,7 @@ __global__ __launch_bounds__(EXT_THREADS) void cache_extend_kernel(CacheExtend a
   __shared__ int s_len[EXT_THREADS], s_flags;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_chunks = (a.n_seqs + EXT_THREADS - 1) / EXT_THREADS;
   const int top = *a.free_top;
-  const long long cap = (long long)a.max_pages * CACHE_PAGE;
+  const long long cap = min((long long)a.max_pages * CACHE_PAGE, (1ll << 31) - CACHE_PAGE);       // (rounded up to pages, still 31 bits)
   I sum[3], total[3];                                // this thread's sequence: sums before it in its chunk; the chunk's totals
   int len, add;
   bool bad = false;

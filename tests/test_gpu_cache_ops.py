@@ -227,6 +227,62 @@ def test_tables_of_as_many_rows_as_are_counted():
         assert all(int(t[a:a + (1 << 28)].max()) == int(t[a:a + (1 << 28)].min()) == -1 for a in range(few, n_rows, 1 << 28))
 
 
+@pytest.mark.parametrize("n_rows", [64, 5000])
+def test_tables_of_the_longest_lengths(n_rows):
+    """A block table of 2^27 columns: lengths up to 2^31 - 16, nothing beyond."""
+    import torch
+    top = (1 << 31) - 16
+    table = torch.full((1, 1 << 27), -9, dtype=torch.int32, device="cuda")
+    for length, new, status in ((top - 16, 16, 0), (top - 16, 17, 2), (top - 1, 1, 0), (top - 1, 2, 2), (top, 0, 0), (top, 1, 2), (top + 1, 0, 2), (top + 15, 0, 2), (top + 15, -1, 2),
+                                (top - 20, 35, 2)):
+        last = (length - 1) // 16 if status == 0 else 5
+        table[0, last] = 3                                      # the page that is not full
+        stack = i32([8, 6, 4, 2])
+        got = ap().april_cache_extend(i32([length]), i32([new]), table, stack, i32([2]), n_rows)
+        assert int(got.status) == status, (length, new)
+        want = list(range(length, length + new)) if status == 0 else []
+        page = {p // 16: 3 if p // 16 == last else 6 for p in want}
+        pad = [-1] * (n_rows - len(want))
+        assert host(got.positions).tolist() == want + pad and host(got.slot_map).tolist() == [page[p // 16] * 16 + p % 16 for p in want] + pad
+        taken = sum(p != last for p in page)
+        assert int(got.lens) == (length + new if status == 0 else length) and int(got.free_top) == 2 - taken and host(stack).tolist() == [8, 6, 4, 2]
+        at = torch.nonzero(table[0] != -9)[:, 0].tolist()
+        assert at == sorted({last, *page}) and all(int(table[0, c]) == page.get(c, 3) for c in at)
+        table[0, at] = -9
+
+
+@pytest.mark.parametrize("n,cols", [(1025, 65536), (4, 1 << 24), (3, 1 << 25)])
+@pytest.mark.parametrize("new_hi", [3, 60])
+@pytest.mark.parametrize("n_rows", [4000, 70000])
+def test_tables_of_wide_block_tables(n, cols, new_hi, n_rows):
+    """Sequences and columns that could hold 2^30 tokens and more, so that sums are counted in 64 bits: few tokens of each, in one launch and in two."""
+    import torch
+    rng = np.random.default_rng([n, new_hi, n_rows])
+    lens, new = rng.integers(0, 70, size=n).tolist(), rng.integers(0, new_hi + 1, size=n).tolist()
+    for b in rng.permutation(n)[:n // 3]:
+        new[b] = -1
+    held = [-(-x // 16) for x in lens]
+    n_pages = sum(held) + sum(max(0, -(-(x + a) // 16) - h) for x, a, h in zip(lens, new, held) if a >= 0) + 1
+    order = rng.permutation(n_pages).tolist()
+    at = np.cumsum([0] + held)
+    table, free = [order[a:b] for a, b in zip(at, at[1:])], order[at[-1]:]
+    tab = torch.full((n, cols), -9, dtype=torch.int32, device="cuda")
+    first = np.full((n, 16), -9, dtype=np.int32)
+    for b, t in enumerate(table):
+        first[b, :len(t)] = t
+    tab[:, :16] = dev(first)
+    stack = i32(free + [0] * (n_pages - len(free)))
+    got = ap().april_cache_extend(i32(lens), i32(new), tab, stack, i32([len(free)]), n_rows)
+    w_table, w_free = [list(t) for t in table], list(free)
+    w_lens, starts, slots, pos, status = kc.extend(lens, new, w_table, w_free, cols, n_pages, n_rows)
+    assert int(got.status) == status == (2 if sum(max(a, 0) for a in new) > n_rows else 0)
+    assert host(got.lens).tolist() == w_lens and host(got.q_start).tolist() == starts and int(got.free_top) == len(w_free)
+    assert host(got.slot_map).tolist() == slots and host(got.positions).tolist() == pos and host(stack)[:len(w_free)].tolist() == w_free
+    for b, t in enumerate(w_table):
+        first[b, :len(t)] = t
+    assert np.array_equal(host(tab[:, :16]), first) and int(tab[:, 16:].max()) == int(tab[:, 16:].min()) == -9
+
+
 # --- attention -----------------------------------------------------------------------------------------------------------
 
 
