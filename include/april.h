@@ -370,7 +370,7 @@ typedef struct {
   const int32_t* block_table;    /* [n_seqs][max_pages]                                        */
   const int32_t* lens;           /* [n_seqs] tokens in the cache, those of the rows included   */
   const int32_t* q_start;        /* [n_seqs + 1], or NULL: row b is sequence b's (n_rows >= n_seqs) */
-  void* out;                     /* bf16, as q (8-byte aligned heads)                          */
+  void* out;                     /* bf16, as q (8-byte aligned heads; no two overlap)          */
   float* lse;                    /* [n_rows][n_q_heads] log of the sum of exp(scale q k), or NULL */
   void* workspace;               /* april_cache_attention_workspace bytes, 16-byte aligned; NULL if 0.  Calls that may
                                     run at the same time need one each                         */

@@ -1,6 +1,7 @@
 // C entry points of the 4-bit KV cache's operators: the arguments' checks, then the launch.  They need no context.
 #include <algorithm>
 #include <cmath>
+#include <utility>
 
 #include "../../include/april.h"
 #include "cache.h"
@@ -13,6 +14,25 @@ bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % 
 bool head_dim_ok(int dh) { return dh == 32 || dh == 64 || dh == 128; }
 int launched(const char* name, hipError_t e) {
   return e == hipSuccess ? APRIL_OK : fail_no_ctx(APRIL_EDEVICE, "%s: launch failed: %s", name, hipGetErrorString(e));
+}
+
+// Whether some two of n x m runs of `len` elements, `row` and `head` elements apart, share one.
+bool runs_overlap(int64_t n, int64_t row, int64_t m, int64_t head, int64_t len) {
+  auto dist = [](int64_t x) { return x < 0 ? 0 - (uint64_t)x : (uint64_t)x; };      // (as is the order of rows and heads, a sign is nothing here)
+  uint64_t s[2] = {dist(row), dist(head)}, c[2] = {(uint64_t)n, (uint64_t)m}, l = (uint64_t)len;
+  if (c[0] <= 1 || (c[1] > 1 && s[1] < s[0])) { std::swap(s[0], s[1]); std::swap(c[0], c[1]); }
+  if (c[0] <= 1) return false;
+  if (s[0] < l) return true;
+  if (c[1] <= 1) return false;
+  const unsigned __int128 span = (unsigned __int128)s[0] * (c[0] - 1) + l;           // of the nearer ones
+  if (s[1] >= span) return false;
+  for (uint64_t j = 1; j < c[1]; ++j) {                                            // rare: the two interleave
+    const unsigned __int128 at = (unsigned __int128)s[1] * j;
+    if (at >= span) return false;
+    const uint64_t rest = (uint64_t)(at % s[0]), below = (uint64_t)(at / s[0]);
+    if ((rest < l && below < c[0]) || (s[0] - rest < l && below + 1 < c[0])) return true;
+  }
+  return false;
 }
 
 #define REFUSE(...) return fail_no_ctx(APRIL_EINVAL, __VA_ARGS__)
@@ -100,6 +120,7 @@ int april_cache_attention(const april_cache_attention_args* a) {
                 out_head = a->n_q_heads > 1 ? a->out_head : 0;
   if (!aligned(a->q, 16) || q_row % 8 || q_head % 8 || !aligned(a->pool, 16)) REFUSE("april_cache_attention: q's heads and the pool must be 16-byte aligned");
   if (!aligned(a->out, 8) || out_row % 4 || out_head % 4) REFUSE("april_cache_attention: out's heads must be 8-byte aligned");
+  if (runs_overlap(a->n_rows, out_row, a->n_q_heads, out_head, a->head_dim)) REFUSE("april_cache_attention: heads of out overlap");
   if (a->table_stride < a->max_pages && a->n_seqs > 1) REFUSE("april_cache_attention: rows of the block table overlap");
   const size_t need = cache_attention_workspace(k, a->head_dim);
   if (need > 0 && (!a->workspace || a->workspace_bytes < (int64_t)need || !aligned(a->workspace, 16)))

@@ -46,6 +46,33 @@ def test_attention(over):
     assert "april_cache_attention" in refused(ap.load_library().april_cache_attention, attention_args(**over))
 
 
+def overlap(n, row, m, head, length):
+    """By listing the elements."""
+    seen = [i * row + j * head + d for i in range(n) for j in range(m) for d in range(length)]
+    return len(set(seen)) < len(seen)
+
+
+def test_attention_refuses_results_that_overlap():
+    """Rows and heads in either order, interleaved, backwards, and alone (a stride is then not used), for all strides about a head's length."""
+    call = ap.load_library().april_cache_attention
+    refusals = 0
+    for rows, heads in ((3, 2), (2, 4), (5, 3), (1, 4), (4, 1), (1, 1)):
+        for row in (0, 28, 32, 36, 40, 64, 72, 96, 100, 128, 160, 1000, -32, -96, -28):
+            for head in (0, 28, 32, 36, 48, 64, 68, 96, 128, 160, 192, 1000, -64, -20):
+                # (another refusal comes behind this one: nothing is launched)
+                args = attention_args(head_dim=32, n_q_heads=heads, n_kv_heads=1, n_rows=rows, n_seqs=2, q_start=P, out_row=row, out_head=head, table_stride=3)
+                message = refused(call, args)
+                assert ("heads of out overlap" in message) == overlap(rows, row, heads, head, 32), (rows, heads, row, head, message)
+                refusals += "heads of out overlap" in message
+    assert refusals > 200
+
+
+@pytest.mark.parametrize("row,head,bad", [(1 << 62, 64, False), (-(1 << 62), 1 << 61, True), (-(1 << 63), -(1 << 63), True), (1 << 40, 1 << 40, True), (1 << 40, (1 << 40) + 32, True),
+                                          (1 << 40, (1 << 40) + 64, False)])
+def test_attention_of_large_strides(row, head, bad):
+    assert ("heads of out overlap" in refused(ap.load_library().april_cache_attention, attention_args(out_row=row, out_head=head, table_stride=3))) == bad
+
+
 def test_attention_needs_its_workspace():
     lib = ap.load_library()
     a = attention_args(max_pages=4096, table_stride=4096, max_len=60000)
