@@ -484,6 +484,14 @@ def _table(t, rows, dev):
     return t.data_ptr(), cols, max(stride[0], cols) if rows == 1 else stride[0]
 
 
+def _differentiable(name):
+    """A tensor that asks for a gradient: refused where one would be recorded, since none is."""
+    if _torch is None:
+        _need_torch()
+    if _torch.is_grad_enabled():
+        _refuse("%s requires a gradient, and the operator has none: call it under torch.no_grad(), or on %s.detach()", name, name)
+
+
 def _gpu(name, t):
     dev = t.get_device()
     if dev < 0:
@@ -557,7 +565,16 @@ def april_cache_extend(lens, new_lens, block_table, free_pages, free_top, n_rows
 
 def april_cache_append(pool, k, v, slot_map, k_values=None, v_values=None) -> None:
     """Store k and v [n_rows, n_kv_heads, head_dim] (bf16 or fp32) in the pool at slot_map [n_rows] (int64); rows whose slot lies
-    outside the pool are left out.  k_values, v_values: contiguous, of k's type: what the cache now stands for."""
+    outside the pool are left out.  k_values, v_values: contiguous, of k's type: what the cache now stands for.  Not differentiable: refused
+    where autograd would record a gradient of one of them."""
+    if k.requires_grad:
+        _differentiable("k")
+    if v.requires_grad:
+        _differentiable("v")
+    if k_values is not None and k_values.requires_grad:
+        _differentiable("k_values")
+    if v_values is not None and v_values.requires_grad:
+        _differentiable("v_values")
     p, pages, heads, dh, dev = _pool(pool)
     t = k.dtype
     if t is not _torch.bfloat16 and t is not _torch.float32:
@@ -578,7 +595,14 @@ def april_cache_attention(q, pool, block_table, lens, max_len: int, *, q_start=N
     """Causal attention of q [n_rows, n_q_heads, head_dim] (bf16) over the cache: rows q_start[b] .. q_start[b + 1] - 1 are the last tokens
     of sequence b (q_start None: row b).  lens [n_seqs]: tokens in the cache, those of the rows included; max_len, max_q: bounds on
     lens and on a sequence's rows.  lse: fp32 [n_rows, n_q_heads], written if given.  Returns out (rows of no sequence are left as
-    they were; in a new `out` they are undefined)."""
+    they were; in a new `out` they are undefined).  Not differentiable: refused where autograd would record a gradient of q,
+    out or lse."""
+    if q.requires_grad:
+        _differentiable("q")
+    if out is not None and out.requires_grad:
+        _differentiable("out")
+    if lse is not None and lse.requires_grad:
+        _differentiable("lse")
     p, pages, heads, dh, dev = _pool(pool)
     bf16, i32 = _torch.bfloat16, _torch.int32
     shape = q.shape

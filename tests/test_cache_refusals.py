@@ -176,6 +176,23 @@ def test_the_binding_refuses_tensors_that_are_not_on_a_gpu_or_of_another_kind():
     assert binding._rows("x", t(3, 2, 40)[..., :32], i32, (3, 2, 32), -1)[1:] == (80, 40)
 
 
+def test_gradients_are_refused_and_not_silently_left_out():
+    import torch
+    bf16 = torch.bfloat16
+    pool, slots, table, lens = torch.zeros((2, 2, 544), dtype=torch.uint8), torch.zeros(3, dtype=torch.int64), torch.zeros((3, 4), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    x = lambda grad=False: torch.zeros((3, 2, 32), dtype=bf16, requires_grad=grad)  # noqa: E731
+    calls = [("q", lambda: ap.april_cache_attention(x(True), pool, table, lens, 60)), ("out", lambda: ap.april_cache_attention(x(), pool, table, lens, 60, out=x(True) * 1)),
+             ("lse", lambda: ap.april_cache_attention(x(), pool, table, lens, 60, lse=torch.zeros((3, 2), requires_grad=True))),
+             ("k", lambda: ap.april_cache_append(pool, x(True), x(), slots)), ("v", lambda: ap.april_cache_append(pool, x(), x(True) * 2, slots)),
+             ("k_values", lambda: ap.april_cache_append(pool, x(), x(), slots, k_values=x(True))), ("v_values", lambda: ap.april_cache_append(pool, x(), x(), slots, v_values=x(True)))]
+    for name, call in calls:
+        with pytest.raises(ap.AprilError, match="^april error -1: %s requires a gradient" % name):
+            call()
+        for off in (torch.no_grad, torch.inference_mode):
+            with off(), pytest.raises(ap.AprilError, match="not on a GPU"):       # nothing else is wrong with it
+                call()
+
+
 def test_numbers_beyond_their_type_are_refused():
     with pytest.raises(ap.AprilError, match="range"):
         binding._bytes(binding._PACK_EXTEND, 1 << 31, *range(16))

@@ -815,3 +815,18 @@ def test_refused_tensors():
         with pytest.raises(ap().AprilError) as e:
             call()
         assert e.value.code == ap().APRIL_EINVAL
+
+
+def test_tensors_that_require_a_gradient():
+    """Without autograd they are tensors as any other."""
+    import torch
+    rng = np.random.default_rng(47)
+    cache = Cache(rng, [40, 7], 2, 64)
+    q, qv = bf16(rng.standard_normal((2, 8, 64)))
+    args = (cache.pool, dev(cache.table), i32(cache.lens), 40)
+    with pytest.raises(ap().AprilError, match="gradient"):
+        ap().april_cache_attention(q.requires_grad_(), *args)
+    with torch.no_grad():
+        out = ap().april_cache_attention(q, *args)
+    assert not out.requires_grad and torch.equal(out, ap().april_cache_attention(q.detach(), *args))
+    check_attention(host(out), None, qv, np.arange(3), cache, 1 / 8)
