@@ -546,6 +546,8 @@ def april_cache_extend(lens, new_lens, block_table, free_pages, free_top, n_rows
     if _torch is None:
         _need_torch()
     i32 = _torch.int32
+    if n_rows < 0:
+        _refuse("n_rows: %d is below zero", n_rows)
     dev = _gpu("lens", lens)
     if len(lens.shape) != 1 or len(free_pages.shape) != 1:
         _refuse("lens and free_pages: one dimension wanted")

@@ -176,6 +176,13 @@ def test_the_binding_refuses_tensors_that_are_not_on_a_gpu_or_of_another_kind():
     assert binding._rows("x", t(3, 2, 40)[..., :32], i32, (3, 2, 32), -1)[1:] == (80, 40)
 
 
+def test_rows_below_zero():
+    import torch
+    t = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(ap.AprilError, match="n_rows"):
+        ap.april_cache_extend(t(3), t(3), t(3, 4), t(9), t(1), -1)
+
+
 def test_gradients_are_refused_and_not_silently_left_out():
     import torch
     bf16 = torch.bfloat16
