@@ -1936,6 +1936,7 @@ int april_rollout_step(april_ctx* c, const april_request* new_reqs, int32_t n_ne
       // the prefill must not run on block tables that were not filled: look at the error flag now
       HIPCHK(c, hipMemcpyAsync(c->h_ctrl, c->d_ctrl, sizeof(Ctrl), hipMemcpyDeviceToHost, st));
       HIPCHK(c, hipStreamSynchronize(st));
+      if (c->h_ctrl->error == 2) return fail(c, APRIL_EDEVICE, "a prompt is longer than its row of the block table, or the page stack does not fit the pool (prefill pages)");
       if (c->h_ctrl->error) return fail(c, APRIL_ENOMEM, "KV page stack underflow on device (prefill pages)");
     }
     // iteration 1: resident rollouts decode, the others are (re-)prefilled
