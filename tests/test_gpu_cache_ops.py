@@ -632,6 +632,54 @@ def test_same_bits_each_time_and_whatever_the_batch_holds_besides(count):
         assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("hq,hkv,dh,count,n", [(16, 4, 128, 1, 4500), (16, 4, 128, 60, 4500), (14, 2, 64, 1, 700), (8, 8, 32, 5, 5000), (5, 1, 128, 100, 130)])
+def test_a_sequence_has_the_same_bits_whatever_the_others_hold(hq, hkv, dh, count, n):
+    """Sequences and bounds stay, since they decide the splits; the others' lengths, rows and contents, and all pages, are others each time."""
+    import torch
+    rng = np.random.default_rng([53, dh, count])
+    k, v = (torch.as_tensor(rng.standard_normal((n, hkv, dh)), dtype=torch.bfloat16).cuda() for _ in range(2))
+    kept, _ = bf16(rng.standard_normal((count, hq, dh)))
+    results = []
+    for others, where in (([200, 3000, 0], 1), ([1, 1, 6000], 3), ([5999, 31, 64], 0), ([2048, 2049, 4096], 2)):
+        lens = others[:where] + [n] + others[where:]
+        counts = [min(int(rng.integers(1, count + 1)), max(x, 1)) for x in lens]
+        counts[where] = count
+        cache = Cache(rng, lens, hkv, dh, cols=375)             # (6000 tokens: the table's width is a bound, too)
+        slots = [int(cache.table[where, t // 16]) * 16 + t % 16 for t in range(n)]
+        ap().april_cache_append(cache.pool, k, v, dev(np.array(slots, dtype=np.int64)))
+        starts = np.concatenate([[0], np.cumsum(counts)])
+        q, _ = bf16(rng.standard_normal((starts[-1], hq, dh)))
+        q[starts[where]:starts[where + 1]] = kept
+        out, lse, _, _ = attend(cache, q, starts, max_len=6000, max_q=count, no_start=False)
+        results.append((out[starts[where]:starts[where + 1]], lse[starts[where]:starts[where + 1]]))
+    for out, lse in results[1:]:
+        assert np.array_equal(out, results[0][0]) and np.array_equal(lse, results[0][1])
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(16, 4, 128), (14, 2, 64)])
+def test_single_rows_beside_a_piece_of_many(hq, hkv, dh):
+    """In one call; and in two, of the rows up to max_q = 1 and of the last sequence alone, which a call leaves each to the other."""
+    import torch
+    rng = np.random.default_rng([59, dh])
+    lens, counts = [5000, 1, 300, 2047, 16, 900], [1, 1, 1, 1, 1, 400]
+    cache = Cache(rng, lens, hkv, dh)
+    starts = np.concatenate([[0], np.cumsum(counts)])
+    q, qv = bf16(rng.standard_normal((starts[-1], hq, dh)))
+    out, lse, _, _ = attend(cache, q, starts)
+    table, d_lens, d_starts = dev(cache.table), i32(lens), i32(starts)
+    out2, lse2 = torch.full_like(q, 5.0), torch.full((q.shape[0], hq), 5.0, device="cuda")
+    ap().april_cache_attention(q, cache.pool, table, d_lens, 5000, q_start=d_starts, out=out2, lse=lse2)
+    assert torch.all(out2[6:] == 5.0) and torch.all(lse2[6:] == 5.0)
+    singles = out2[:5].clone()
+    ap().april_cache_attention(q, cache.pool, table[5:], d_lens[5:], 900, q_start=d_starts[5:], max_q=400, out=out2, lse=lse2)
+    assert torch.equal(out2[:5], singles)
+    for o, s in ((out, lse), (host(out2), host(lse2))):
+        check_attention(o, s, qv, starts, cache, 1 / np.sqrt(dh), seqs=range(5))
+        for i in (0, 1, 255, 399):                              # of the piece
+            sub = type("S", (), dict(lens=[900], k=[cache.k[5][:501 + i]], v=[cache.v[5][:501 + i]]))
+            check_attention(o[5 + i:6 + i], s[5 + i:6 + i], qv[5 + i:6 + i], [0, 1], sub, 1 / np.sqrt(dh))
+
+
 # --- streams, graphs, the three together -------------------------------------------------------------------------------------
 
 
