@@ -42,7 +42,9 @@ extern "C" {
 #define APRIL_DTYPE_FP32 0
 #define APRIL_DTYPE_BF16 1
 #define APRIL_DTYPE_BF16_KV4 2   /* bf16, but the KV cache in 4 bits (the blocks of the 4-bit cache operators below): 3.8 times
-                                    the tokens in the same memory, and keys and values rounded to MXFP4         */
+                                    the tokens in the same memory, and keys and values rounded to MXFP4.  Decode is faster where
+                                    reading the cache bounds it (many rollouts, long contexts), a few percent slower for one
+                                    short rollout of a small model; so is prefill                               */
 #define APRIL_MEM_KV      1   /* memory tags of april_memory_pause / april_memory_resume */
 #define APRIL_MEM_WEIGHTS 2
 #define APRIL_SAMPLER_GREEDY 0
@@ -345,7 +347,8 @@ typedef struct {
 } april_cache_append_args;
 int april_cache_append(const april_cache_append_args* args);
 
-/* Causal attention over the cache, softmax(scale q k) v, bf16, sums in fp32.  The rows
+/* Causal attention over the cache, softmax(scale q k) v, bf16, sums in fp32; the softmax's weights are rounded to bf16
+ * before they multiply the values (their own sum is not), which puts an output off by at most 2^-8 of the mean |v| under them.  The rows
  * q_start[b] .. q_start[b + 1] - 1 of q are the last tokens of sequence b: row i of c sees the tokens
  * 0 .. lens[b] - c + i.  (One row: a decode iteration.  As many rows as tokens: a whole prompt.)
  * n_q_heads / n_kv_heads (at most 16) consecutive query heads share a KV head.
@@ -353,6 +356,10 @@ int april_cache_append(const april_cache_append_args* args);
  * cache reaches the rows that see it.  A page id outside the pool makes the rows that see a token on it NaN (and
  * may others of their sequence); a length outside 0 .. max_len, beyond the block table or
  * beyond 2^30, all rows of its sequence.
+ * n_seqs, the heads, max_q and max_len (or 16 max_pages, where that is less) decide how the work is shared out, for all sequences
+ * alike; with those given, a row's bits do not depend on the other sequences.  One sequence of many rows among many of one row has all of them
+ * take the way of many rows, without splits of long contexts: two calls are faster then, one with max_q 1 over all (it leaves the further rows as they
+ * were), one with the arrays of the long sequences alone (block_table, lens and q_start from theirs on).
  * Sizes that bound more work than one launch takes are refused (APRIL_EINVAL, here and by the workspace query): 2^24 workgroups,
  * of which each KV head of a sequence has one, or one for every 256 of max_q x (query heads of the KV head) where those are more than 64, and
  * that for every split of max_len tokens (at most 4096 a split up to those 64); where there are splits, 2^24 rows n_seqs x max_q. */
@@ -362,7 +369,7 @@ typedef struct {
   int32_t max_pages;             /* columns of the block table                                 */
   int32_t n_rows;                /* rows of q, out and lse                                     */
   int32_t max_q;                 /* bound on the rows of a sequence (rows beyond it are left as they were) */
-  int32_t max_len;               /* bound on lens.  Both decide how the work is split: tight bounds are faster */
+  int32_t max_len;               /* bound on lens.  Tight bounds are faster                    */
   float scale;                   /* > 0; 0: 1 / sqrt(head_dim)                                 */
   int64_t table_stride, q_row, q_head, out_row, out_head;   /* in elements; dimensions are adjacent */
   const void* q;                 /* bf16 [n_rows][n_q_heads][head_dim], heads 16-byte aligned  */

@@ -257,6 +257,8 @@ hipError_t launch_cache_extend(hipStream_t st, const CacheExtend& a) {
 
 // ---------------------------------------------------------------------------
 // Store.  A wavefront takes 16 rows of one (head, block of 32): 4 lanes to a row, 8 dimensions each, keys then values.
+// Bound by HBM where a page's rows come together, as a prompt's do: 32768 rows of 8 heads of 128 with the values 125 us in fp32 (4.6 TB/s), 63 in
+// bf16 (4.8); rows whose slots are a random permutation write lone pieces of 16 bytes, 160 and 97 us (3.6 and 3.1 TB/s).
 // ---------------------------------------------------------------------------
 namespace {
 
@@ -713,7 +715,9 @@ __global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_a
     __builtin_amdgcn_sched_barrier(0);
     // Softmax in base 2; the running maximum may lag by 2^8 (probabilities then reach 256, which costs no precision), so that a
     // tile seldom needs a shuffle.  It is a score, subtracted before the scale: of scores beyond 2^30 a rounded multiple of it would leave
-    // exponents of hundreds.  Probabilities are rounded to bf16 for the second product, their sum is not.
+    // exponents of hundreds.  Probabilities are rounded to bf16 for the second product, their sum is not: an output is off by at most
+    // 2^-8 of the mean |v| under its weights (relative 2-norm 0.0023, of which the rounded output alone is 0.0017).  A second bf16 term of
+    // each would take that away and double the second product, the opened values' reads with it.
     bf16x8 pf[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
@@ -762,7 +766,7 @@ __global__ __launch_bounds__(64 * W, CT == 1 ? 4 : CT == 2 ? 2 : 1) void cache_a
   // A slot is requested again as soon as its tile is done; behind the last tile that is the last tile once more, so that no load is in a
   // branch (a wait behind one would be for all loads).  Two copies of the loop's body: every compute unit has to fetch the code of a
   // launch (with steady state and tail apart, five copies, 61 sequences of 100-2003 tokens took 20.7 us and not 17.4; the loop has 124 registers then, not 168: 192 of
-  // 576-4608 tokens, 32 + 8 heads of 128, 131 and 121).
+  // 576-4608 tokens, 32 + 8 heads of 128, 131 and 121; with all that came later 15.2 and 116).
   for (int i = 0; i < cnt; i += R) {
 #pragma unroll
     for (int u = 0; u < R; ++u) {
@@ -906,9 +910,11 @@ template <int DH> dim3 join_grid(const CacheAttn& a, int rows) { return dim3(row
 // has the loop wait for its reload and with it for the codes on their way.  So the codes go past the registers (copied into LDS), and what follows
 // from a lane's number is computed where it is used.  A fragment's read from LDS takes as long as four products, so two are in flight
 // (left to itself the compiler reads into the registers just used, and waits), and the exponentials of a half's second 16
-// tokens run beside the products of its first.  21 prompts of 1-1999 tokens, 32 + 8 heads: 358 us; without
+// tokens run beside the products of its first.  Probabilities are rounded to bf16 for the second product, as above.
+// 21 prompts of 1-1999 tokens, 32 + 8 heads, us in short runs: 358; without
 // spills 325, fragments ahead 317, queries and outputs as whole rows 304, exponentials beside products 288, scores less
-// their maximum before the scale 300 (765 TFLOP/s; without it scores beyond 2^30 overflow).  What is left:
+// their maximum before the scale 300 (without it scores beyond 2^30 overflow).  Such a run is too short for the clock: of 300 calls in a row the
+// first 20 take 339 under the profiler, from the 150th on 269 to 278 (827 TFLOP/s and more).  What is left, in those runs:
 // queries, outputs and the first stage alone take 110 us (2 x 172 MB), opening and barriers 46; priorities for either kind of phase,
 // three fragments in flight and the codes requested later changed nothing.
 constexpr int RA_STAGE = 64, RA_COLS = 256;
@@ -1257,14 +1263,20 @@ int row_tiles(const CacheAttn& a) { return (int)(((long long)a.max_q * (a.Hq / a
 // Splits of the longest context, and the wavefronts that share a split's tiles.  Few rows: 8 wavefronts where the sequences and their KV heads
 // leave compute units with one or two workgroups.  A split saves 0.6 to 0.75 us for each of its 128 tokens and 4 wavefronts and costs 0.1 us of
 // the join, which takes 2.5 us besides: least in all for about 10 sqrt(length) tokens, until the workgroups fill the chip; from 128 sequences and heads on
-// it does not pay below what a workgroup can hold; half of that, up to 1280 workgroups, where the longest context has to be split anyway: 40 of
-// 4000-9000 73 | 68, 30 of 8000-16000 96 | 93, 70 of 1000-9000 with 14 + 2 heads of 64 25 | 21 (but 20 of 1000-4000 24.4 | 25.8, 100 of 500-4000 18.4 | 19.6).
-// us, one row of 32 + 8 heads of 128, 4 wavefronts in splits of 512 | 1024 | 4096, 8 in 512 | 1024 | 4096:
-//   1 sequence of 300 tokens 7.1 (whole), 6.4; 1000 10.6 | 11.0, 9.9 | 9.1; 2000 10.9 | 13.7 | 17.4, 10.1 | 11.7 | 13.3; 4000 11.6 | 14.1 | 30.5, 11.0 | 12.3 | 21.8;
-//     16000 19.7 | 18.2 | 35.2, 19.9 | 16.9 | 26.7
-//   8 of 1000 11.5 | 11.4, 10.6 | 9.7; 4000 16.8 | 16.3 | 32.1, 17.4 | 15.5 | 23.8;   20 of 1000 14.6 | 12.1, 15.4 | 11.0; 4000 26 | 24.6 | 33.3, 30.6 | 26.7 | 25.2
-//   40 of 40 6.0, 6.2; 1000 17.8 | 16.0, 20.3 | 16.1; 4000 47 | 44 | 46, 58 | 47 | 49;   192 of 576-4608 138 | 123 | 125, 177 | 148 | 122
-//   (16 wavefronts: 1 of 4000 11.9 | 12.8 | 20.0, 20 of 4000 46 | 37 | 23.5, 40 of 1000 28 | 21.6.)
+// it does not pay below what a workgroup can hold; half of that, up to 1280 workgroups, where the longest context has to be split anyway: with 4096 | 2048 and
+// 8 wavefronts 40 of 4000-9000 72 | 66, 30 of 8000-16000 89 | 86, 70 of 1000-9000 with 14 + 2 heads of 64 27 | 20 (but 20 of 1000-4000 23.4 | 24.9,
+// 100 of 500-4000 with 14 + 2 heads of 64 17.5 | 18.7).
+// us, one row of 32 + 8 heads of 128, 4 wavefronts in splits of 512 | 1024 | 2048 | 4096, 8 in the same (shorter contexts: whole), and by the rule:
+//   1 sequence of 300 tokens 6.9, 6.1, 6.1; 1000 10.2 | 10.6, 9.5 | 8.9, 8.9; 2000 10.6 | 13.3 | 17.3, 9.8 | 11.6 | 13.2, 9.8
+//     4000 11.3 | 13.7 | 20.1 | 30.3, 10.8 | 11.9 | 16.1 | 21.7, 11.0; 16000 19.0 | 17.8 | 22.4 | 34.8, 19.8 | 16.4 | 18.7 | 26.6, 17.3
+//   8 of 1000 10.9, 10.5 | 9.4, 9.4; 4000 16.6 | 15.8 | 21.6 | 31.7, 17.2 | 15.0 | 18.5 | 23.5, 17.5
+//   16 of 4000 22.3 | 19.9 | 22.2 | 31.8, 25.8 | 20.5 | 19.6 | 23.4, 23.7
+//   20 of 1000 14.5 | 11.6, 15.2 | 10.5, 10.6; 4000 26.3 | 24.5 | 27.4 | 31.9, 30.4 | 25.9 | 26.9 | 24.0, 24.1
+//   40 of 40 5.7, 5.9, 5.6; 1000 17.9 | 15.8, 19.7 | 15.5, 15.5; 4000 46.6 | 42.7 | 44.2 | 43.6, 56.8 | 44.7 | 42.8 | 46.1, 46.1
+//   40 of 4000-9000 72 | 66 | 68 | 73, 93 | 72 | 66 | 72, 64; 30 of 8000-16000 98 | 88 | 88 | 92, 124 | 95 | 86 | 89, 86
+//   192 of 576-4608 129 | 117 | 115 | 118, 173 | 134 | 116 | 111, 116
+//   (16 wavefronts, before the last steps: 1 of 4000 11.9 | 12.8 | 20.0 in 512 | 1024 | 4096, 20 of 4000 46 | 37 | 23.5, 40 of 1000 28 | 21.6.)
+// Where it is not best: 128 sequences and heads of up to 4096 tokens, whole (16 of 4000: 24 against 20; 40 of 4000: 46 against 43).
 //
 // Many rows: as many splits as fill the two workgroups that a compute unit holds, none shorter than 256 tokens; of whole prompts, whose
 // workgroups see half of the tokens on average, half again as many.  us with 256 | 512 | 1024 | 2048 | 4096 | no splits (32 + 8 heads of 128): 3 sequences of
