@@ -362,7 +362,8 @@ int april_cache_append(const april_cache_append_args* args);
  * were), one with the arrays of the long sequences alone (block_table, lens and q_start from theirs on).
  * Sizes that bound more work than one launch takes are refused (APRIL_EINVAL, here and by the workspace query): 2^24 workgroups,
  * of which each KV head of a sequence has one, or one for every 256 of max_q x (query heads of the KV head) where those are more than 64, and
- * that for every split of max_len tokens (at most 4096 a split up to those 64); where there are splits, 2^24 rows n_seqs x max_q. */
+ * that for every split of max_len tokens (at most 4096 a split up to those 64); where there are splits, 2^24 rows n_seqs x max_q;
+ * and 2^31 - 256 of max_q x (query heads of the KV head). */
 typedef struct {
   int32_t n_q_heads, n_kv_heads, head_dim;
   int32_t n_pages, n_seqs;

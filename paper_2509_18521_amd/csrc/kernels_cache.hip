@@ -1318,8 +1318,9 @@ template <int DH> hipError_t attention(hipStream_t st, CacheAttn a) {
 
 }  // namespace
 
-// Whether the launches of a call are: a dimension of a grid has fewer than 2^32 threads.
+// Whether the launches of a call are possible: a dimension of a grid has fewer than 2^32 threads, and columns are counted in 31 bits.
 bool cache_attention_fits(const CacheAttn& a) {
+  if ((long long)a.max_q * (a.Hq / a.Hkv) > (1ll << 31) - RA_COLS) return false;
   // (before splits, in floating point: nothing below this bound overflows)
   if ((double)a.n_seqs * a.Hkv * (few_rows(a) ? 1.0 : (double)row_tiles(a)) * 256 >= 4294967296.0) return false;
   const Split sp = split_of(a);

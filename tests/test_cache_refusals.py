@@ -106,6 +106,18 @@ def test_attention_larger_than_a_launch(sizes, name, fits, first):
         assert "more work than one call takes" in refused(call, args)
 
 
+@pytest.mark.parametrize("heads", [2, 8, 16])
+def test_attention_columns_are_counted_in_31_bits(heads):
+    """Rows times query heads of a KV head, up to whole tiles of 256; fewer workgroups than a launch takes."""
+    lib = ap.load_library()
+    most = ((1 << 31) - 256) // heads
+    sizes = dict(n_q_heads=heads, n_kv_heads=1, head_dim=32, n_seqs=1, n_rows=(1 << 31) - 1, max_len=60, q_start=P)
+    assert lib.april_cache_attention_workspace(C.byref(attention_args(max_q=most, **sizes))) == 0
+    for rows in (most + 1, (1 << 31) - 1):
+        for call in (lib.april_cache_attention_workspace, lib.april_cache_attention):
+            assert "more work than one call takes" in refused(call, attention_args(max_q=rows, **sizes))
+
+
 def test_long_contexts_of_many_rows_that_fit_a_launch():
     """2064384 workgroups: far below the limit, whatever the bounds on rows and length would allow together."""
     a = attention_args(n_q_heads=32, n_kv_heads=8, n_seqs=4096, max_q=4000, n_rows=1 << 20, max_len=32768, max_pages=4096, table_stride=4096)
