@@ -389,6 +389,153 @@ int april_cache_attention(const april_cache_attention_args* args);
 /* Bytes that a call of these sizes needs (pointers, strides and the stream are not looked at). */
 int64_t april_cache_attention_workspace(const april_cache_attention_args* args);
 
+/* ------------------------------------------------------------------------------------------
+ * Operators that score rollouts and train on them, on the caller's own device memory, each with its gradient: the
+ * log-probability of a given token, a token's row of the embedding, a token's rows in its experts' batches.  As the
+ * cache's operators they need no context, enqueue on `stream` of the current device, allocate and synchronise
+ * nothing (so they may be captured into a graph), and leave everything untouched where the host finds an error.
+ * Matrices are rows of adjacent elements, `*_row` elements apart (16-byte aligned rows are fastest); a stride over a
+ * single row is not used; inputs may repeat a row (stride 0), rows of a result may not overlap, nor a result an input where
+ * nothing else is said.  dtype: APRIL_DTYPE_FP32 or APRIL_DTYPE_BF16; sums are in fp32, a result is rounded once.
+ * Indexes (tokens, experts) are of index_bits 32 or 64.  Results do not depend on how the work is shared out between
+ * workgroups, nor from one call to the next.  Calls that may run at the same time need a workspace each. */
+
+/* x = logits / temperature, row by row: logprob = x[token] - lse, lse = log of the sum of exp(x), entropy = -sum of p log p, and the
+ * n_top largest x - lse with their columns, descending, equal logits by ascending column.
+ * A token below zero marks a padding row: its results are 0, its top_ids -1, and it is not read.  A token of vocab or more: logprob
+ * NaN.  Logits of -infinity have probability 0.  Rows that have a NaN, +infinity or nothing but -infinity: NaN (lse: NaN or
+ * -infinity), top_ids -1.  Results that are NULL are left out. */
+typedef struct {
+  int32_t n_rows, vocab;         /* vocab 1..2^30                                              */
+  int32_t dtype, index_bits;     /* of logits; of tokens                                       */
+  int32_t n_top;                 /* 0..64, at most vocab                                       */
+  float temperature;             /* > 0                                                        */
+  int64_t logits_row;
+  const void* logits;            /* [n_rows][vocab]                                            */
+  const void* tokens;            /* [n_rows]                                                   */
+  float *logprob, *entropy, *lse;   /* [n_rows]                                                */
+  float* norm;                   /* [n_rows][2], 8-byte aligned: what april_logprobs_grad needs of the row (its largest logit, log2 of
+                                    the sum of 2^((logit - largest) log2(e) / temperature))   */
+  float* top_logprobs;           /* [n_rows][n_top]                                            */
+  int32_t* top_ids;              /* [n_rows][n_top]                                            */
+  void* workspace;               /* april_logprobs_workspace bytes, 16-byte aligned; NULL if 0 */
+  int64_t workspace_bytes;
+  void* stream;
+} april_logprobs_args;
+int april_logprobs(const april_logprobs_args* args);
+/* Bytes that a call of these sizes needs (pointers, strides and the stream are not looked at). */
+int64_t april_logprobs_workspace(const april_logprobs_args* args);
+
+/* Gradient of the logits for gradients a, h, z of logprob, entropy, lse (NULL: 0):
+ * (a (1 at the token - p) - h p (log p + entropy) + z p) / temperature.  Padding rows: 0; a token of vocab or more: NaN. */
+typedef struct {
+  int32_t n_rows, vocab, dtype, index_bits;   /* as in april_logprobs; grad is of the logits' type */
+  float temperature;
+  int32_t reserved;              /* 0                                                          */
+  int64_t logits_row, grad_row;
+  const void *logits, *tokens;
+  const float* norm;             /* [n_rows][2] of april_logprobs                              */
+  const float* entropy;          /* [n_rows] of april_logprobs; NULL without grad_entropy      */
+  const float *grad_logprob, *grad_entropy, *grad_lse;   /* [n_rows]                           */
+  void* grad;                    /* [n_rows][vocab]; may be the logits themselves (the same address and stride) */
+  void* stream;
+} april_logprobs_grad_args;
+int april_logprobs_grad(const april_logprobs_grad_args* args);
+
+/* out[r] = scale * table[tokens[r]].  A token below zero marks padding: 0; one of vocab or more: NaN. */
+typedef struct {
+  int32_t n_rows, vocab, d;      /* vocab 1..2^30, d 1..2^24                                   */
+  int32_t table_dtype, out_dtype, index_bits;
+  float scale;
+  int32_t reserved;              /* 0                                                          */
+  int64_t table_row, out_row;
+  const void* table;             /* [vocab][d]                                                 */
+  const void* tokens;            /* [n_rows]                                                   */
+  void* out;                     /* [n_rows][d]                                                */
+  void* stream;
+} april_embed_args;
+int april_embed(const april_embed_args* args);
+
+/* grad_table[t] = scale * (sum of grad_out[r] over the rows of token t, in ascending order, in pieces of at most 128 rows where
+ * they are more).  accumulate 0: every row is written (0 where no row has the token); 1: added to what is there, and rows of no
+ * token are not touched.  Tokens outside 0..vocab - 1 are left out. */
+typedef struct {
+  int32_t n_rows, vocab, d;
+  int32_t out_dtype, table_dtype, index_bits;   /* of grad_out, of grad_table, of tokens       */
+  float scale;
+  int32_t accumulate;
+  int64_t out_row, table_row;
+  const void *grad_out, *tokens;
+  void* grad_table;
+  void* workspace;               /* april_embed_grad_workspace bytes, 16-byte aligned          */
+  int64_t workspace_bytes;
+  void* stream;
+} april_embed_grad_args;
+int april_embed_grad(const april_embed_grad_args* args);
+int64_t april_embed_grad_workspace(const april_embed_grad_args* args);
+
+/* Assignments (row r, place j) -> r * k + j, sorted by expert and then by number.  Expert e's packed rows begin at starts[e], a
+ * multiple of align, and starts[n_experts] is the end of the last one's; rows between hold no assignment.  Assignments of
+ * an expert outside 0..n_experts - 1 are left out (position -1).
+ * n_packed: rows of the packed arrays, at least (n + min(n_experts, n) * (align - 1)) / align * align for n = n_rows * k. */
+typedef struct {
+  int32_t n_rows, k;             /* n_rows * k below 2^31 - 4096; k 1..64                      */
+  int32_t n_experts, align;      /* 1..511; 1..4096                                            */
+  int32_t n_packed, index_bits;
+  const void* ids;               /* [n_rows][k]                                                */
+  int32_t* starts;               /* [n_experts + 1]                                            */
+  int32_t* source;               /* [n_packed] assignment of each packed row, -1: none         */
+  int32_t* position;             /* [n_rows][k] packed row of each assignment, -1: left out    */
+  void* workspace;               /* april_expert_sort_workspace bytes, 16-byte aligned; NULL if 0 */
+  int64_t workspace_bytes;
+  void* stream;
+} april_expert_sort_args;
+int april_expert_sort(const april_expert_sort_args* args);
+int64_t april_expert_sort_workspace(const april_expert_sort_args* args);
+
+/* packed[p] = x[source[p] / k]; packed rows of no assignment are 0.  (Its gradient is april_expert_combine of packed's, without weights.)
+ * source and position are april_expert_sort's; entries outside the arrays are as -1. */
+typedef struct {
+  int32_t n_rows, k, d;          /* d 1..2^24                                                  */
+  int32_t n_packed, dtype;
+  int32_t reserved;              /* 0                                                          */
+  int64_t x_row, packed_row;
+  const void* x;                 /* [n_rows][d]                                                */
+  const int32_t *source, *position;
+  void* packed;                  /* [n_packed][d]                                              */
+  void* stream;
+} april_expert_gather_args;
+int april_expert_gather(const april_expert_gather_args* args);
+
+/* out[r] = sum over j of weights[r][j] * packed[position[r][j]], in the order of j. */
+typedef struct {
+  int32_t n_rows, k, d, n_packed, dtype;
+  int32_t reserved;              /* 0                                                          */
+  int64_t packed_row, out_row;
+  const void* packed;            /* [n_packed][d]                                              */
+  const int32_t* position;       /* [n_rows][k]                                                */
+  const float* weights;          /* [n_rows][k], or NULL: 1                                    */
+  void* out;                     /* [n_rows][d]                                                */
+  void* stream;
+} april_expert_combine_args;
+int april_expert_combine(const april_expert_combine_args* args);
+
+/* Its gradients: grad_packed[p] = weight of p's assignment * grad_out of its row (0: no assignment);
+ * grad_weights[r][j] = sum over d of grad_out[r] * packed[position[r][j]] (0: left out). */
+typedef struct {
+  int32_t n_rows, k, d, n_packed, dtype;
+  int32_t reserved;              /* 0                                                          */
+  int64_t out_row, packed_row, grad_packed_row;
+  const void* grad_out;          /* [n_rows][d]                                                */
+  const void* packed;            /* [n_packed][d]; NULL without grad_weights                   */
+  const int32_t *source, *position;
+  const float* weights;          /* [n_rows][k], or NULL: 1                                    */
+  void* grad_packed;             /* [n_packed][d], or NULL                                     */
+  float* grad_weights;           /* [n_rows][k], or NULL                                       */
+  void* stream;
+} april_expert_combine_grad_args;
+int april_expert_combine_grad(const april_expert_combine_grad_args* args);
+
 /* Per-kernel-class timing, measured with HIP events on the context's stream around
  * sampled launches of the real decode loop (every `every`-th iteration; 0 = off).  Two extra
  * classes calibrate the method: "event_pair_no_kernel" is what a pair of event records reads

@@ -28,6 +28,8 @@ EXPORTS = [
     "april_debug_logits", "april_sample_rows", "april_sample_rows_logprobs", "april_sample_rows_noalloc", "april_profile_enable", "april_profile_get",
     "april_profile_reset", "april_get_info", "april_last_error", "april_destroy",
     "april_cache_block_bytes", "april_cache_extend", "april_cache_append", "april_cache_attention", "april_cache_attention_workspace",
+    "april_logprobs", "april_logprobs_workspace", "april_logprobs_grad", "april_embed", "april_embed_grad", "april_embed_grad_workspace",
+    "april_expert_sort", "april_expert_sort_workspace", "april_expert_gather", "april_expert_combine", "april_expert_combine_grad",
 ]
 APRIL_CACHE_PAGE = 16
 
@@ -113,10 +115,63 @@ class april_cache_attention_args(C.Structure):
         ("workspace_bytes", C.c_int64), ("stream", C.c_void_p)]
 
 
+class april_logprobs_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_rows", "vocab", "dtype", "index_bits", "n_top")] + [("temperature", C.c_float), ("logits_row", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("logits", "tokens", "logprob", "entropy", "lse", "norm", "top_logprobs", "top_ids", "workspace")] + [
+        ("workspace_bytes", C.c_int64), ("stream", C.c_void_p)]
+
+
+class april_logprobs_grad_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_rows", "vocab", "dtype", "index_bits")] + [("temperature", C.c_float), ("reserved", C.c_int32)] + [
+        (n, C.c_int64) for n in ("logits_row", "grad_row")] + [
+        (n, C.c_void_p) for n in ("logits", "tokens", "norm", "entropy", "grad_logprob", "grad_entropy", "grad_lse", "grad", "stream")]
+
+
+class april_embed_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_rows", "vocab", "d", "table_dtype", "out_dtype", "index_bits")] + [
+        ("scale", C.c_float), ("reserved", C.c_int32), ("table_row", C.c_int64), ("out_row", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("table", "tokens", "out", "stream")]
+
+
+class april_embed_grad_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_rows", "vocab", "d", "out_dtype", "table_dtype", "index_bits")] + [
+        ("scale", C.c_float), ("accumulate", C.c_int32), ("out_row", C.c_int64), ("table_row", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("grad_out", "tokens", "grad_table", "workspace")] + [("workspace_bytes", C.c_int64), ("stream", C.c_void_p)]
+
+
+class april_expert_sort_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_rows", "k", "n_experts", "align", "n_packed", "index_bits")] + [
+        (n, C.c_void_p) for n in ("ids", "starts", "source", "position", "workspace")] + [("workspace_bytes", C.c_int64), ("stream", C.c_void_p)]
+
+
+class april_expert_gather_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_rows", "k", "d", "n_packed", "dtype", "reserved")] + [
+        ("x_row", C.c_int64), ("packed_row", C.c_int64)] + [(n, C.c_void_p) for n in ("x", "source", "position", "packed", "stream")]
+
+
+class april_expert_combine_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_rows", "k", "d", "n_packed", "dtype", "reserved")] + [
+        ("packed_row", C.c_int64), ("out_row", C.c_int64)] + [(n, C.c_void_p) for n in ("packed", "position", "weights", "out", "stream")]
+
+
+class april_expert_combine_grad_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_rows", "k", "d", "n_packed", "dtype", "reserved")] + [
+        (n, C.c_int64) for n in ("out_row", "packed_row", "grad_packed_row")] + [
+        (n, C.c_void_p) for n in ("grad_out", "packed", "source", "position", "weights", "grad_packed", "grad_weights", "stream")]
+
+
 # The same structs as bytes: packing them is a third of the time of filling a ctypes structure.
 _PACK_EXTEND = struct.Struct("4iq12Q").pack
 _PACK_APPEND = struct.Struct("6i4q7Q").pack
 _PACK_ATTENTION = struct.Struct("9if5q8QqQ").pack
+_PACK_LOGPROBS = struct.Struct("5ifq9QqQ").pack
+_PACK_LOGPROBS_GRAD = struct.Struct("4ifi2q9Q").pack
+_PACK_EMBED = struct.Struct("6ifi2q4Q").pack
+_PACK_EMBED_GRAD = struct.Struct("6ifi2q4QqQ").pack
+_PACK_EXPERT_SORT = struct.Struct("6i5QqQ").pack
+_PACK_EXPERT_GATHER = struct.Struct("6i2q5Q").pack
+_PACK_EXPERT_COMBINE = struct.Struct("6i2q5Q").pack
+_PACK_EXPERT_COMBINE_GRAD = struct.Struct("6i3q8Q").pack
 
 _lib = None
 _calls = {}
@@ -174,10 +229,13 @@ def load_library():
     lib.april_cache_append.argtypes = [C.POINTER(april_cache_append_args)]
     lib.april_cache_attention.argtypes = [C.POINTER(april_cache_attention_args)]
     lib.april_cache_attention_workspace.argtypes = [C.POINTER(april_cache_attention_args)]
+    for name in ("logprobs", "logprobs_grad", "embed", "embed_grad", "expert_sort", "expert_gather", "expert_combine", "expert_combine_grad"):
+        for call in ("april_" + name, "april_%s_workspace" % name):
+            if call in EXPORTS:
+                getattr(lib, call).argtypes = [C.POINTER(globals()["april_%s_args" % name])]
     for name in EXPORTS:
         if name not in ("april_buffer_free", "april_destroy", "april_last_error"):
-            getattr(lib, name).restype = C.c_int
-    lib.april_cache_attention_workspace.restype = C.c_int64
+            getattr(lib, name).restype = C.c_int64 if name.endswith("_workspace") else C.c_int
     _lib = lib
     return lib
 
@@ -627,6 +685,345 @@ def april_cache_attention(q, pool, block_table, lens, max_len: int, *, q_start=N
     size = 0 if workspace is None else workspace.shape[0]
     _enqueue(_call("april_cache_attention"), dev, _PACK_ATTENTION, *fields, _ptr("workspace", workspace, _torch.uint8, (size,), dev) if size else 0, size)
     return out
+
+
+# ---------------------------------------------------------------------------
+# Operators that score rollouts and train on them, on torch tensors of one GPU, each with its gradient: where autograd would record one of
+# logits, table, x, packed or weights, the result carries it, else the call is the library's alone.  They run on torch's current stream and may
+# be captured into a graph.  What torch itself asks of a captured backward pass holds here too: no autograd graph of the
+# same leaf tensors that was recorded outside the capture may be alive meanwhile.  The gradients' own calls (april_*_grad) have no such bound.
+# ---------------------------------------------------------------------------
+class Logprobs(NamedTuple):
+    """What april_logprobs leaves, see april.h (entropy None, top_* None where they were not asked for)."""
+    logprob: object
+    entropy: object
+    lse: object
+    top_logprobs: object
+    top_ids: object
+    norm: object
+
+
+class ExpertRows(NamedTuple):
+    """What april_expert_sort leaves, see april.h (int32)."""
+    starts: object
+    source: object
+    position: object
+
+
+_functions = {}             # autograd's classes, made by the first call that records a gradient (torch is imported late)
+
+
+def _dtype(name, t):
+    if t is _torch.bfloat16:
+        return APRIL_DTYPE_BF16
+    if t is _torch.float32:
+        return APRIL_DTYPE_FP32
+    _refuse("%s: bfloat16 or float32 wanted, not %s", name, t)
+
+
+def _matrix(name, t, dtype, shape, dev):
+    """(pointer, stride of rows) of a tensor [rows][columns] whose rows may lie apart or be one."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        _refuse_tensor(name, t, dtype, shape, dev, True)
+    row, col = t.stride()
+    if col != 1 and shape[1] > 1:
+        _refuse("%s: the elements of a row have to be adjacent", name)
+    return t.data_ptr(), row
+
+
+def _index(name, t, shape, dev):
+    """(pointer, bits) of a contiguous tensor of int32 or int64."""
+    if t.dtype is _torch.int64:
+        return _ptr(name, t, _torch.int64, shape, dev), 64
+    return _ptr(name, t, _torch.int32, shape, dev), 32
+
+
+def _float_ptr(name, t, shape, dev):
+    return 0 if t is None else _ptr(name, t, _torch.float32, shape, dev)
+
+
+def _two(name, t):
+    if _torch is None:
+        _need_torch()
+    if len(t.shape) != 2:
+        _refuse("%s: two dimensions wanted, not %s", name, tuple(t.shape))
+    return t.shape
+
+
+def _records(*tensors):
+    """Whether autograd would record a gradient of one of them."""
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            if _torch is None:
+                _need_torch()
+            return _torch.is_grad_enabled()
+    return False
+
+
+def _no_gradient(**tensors):
+    for name, t in tensors.items():
+        if t is not None and t.requires_grad:
+            _differentiable(name)
+
+
+def _space(call, pack, fields, device):
+    """(tensor, pointer, bytes) of the workspace that the call asks for."""
+    need = _check(None, _call(call)(_bytes(pack, *fields, 0, 0, 0)))
+    space = _torch.empty(need, dtype=_torch.uint8, device=device) if need else None
+    return space, (space.data_ptr() if need else 0), need
+
+
+def _function(name):
+    """autograd's class of an operator."""
+    if not _functions:
+        t = _torch
+        once = t.autograd.function.once_differentiable
+        whole = lambda g: None if g is None else g.contiguous()  # noqa: E731
+
+        class AprilLogprobs(t.autograd.Function):
+            @staticmethod
+            def forward(ctx, logits, tokens, temperature, entropy, top):
+                got = _logprobs(logits, tokens, temperature, entropy, top)
+                ctx.set_materialize_grads(False)
+                ctx.mark_non_differentiable(*(x for x in got[3:] if x is not None))
+                ctx.save_for_backward(logits, tokens, got.norm, got.entropy)
+                ctx.temperature = temperature
+                return tuple(got)
+
+            @staticmethod
+            @once
+            def backward(ctx, g, h, z, *_):
+                if g is None and h is None and z is None:
+                    return (None,) * 5
+                logits, tokens, norm, entropy = ctx.saved_tensors
+                made = Logprobs(None, entropy, None, None, None, norm)
+                return april_logprobs_grad(logits, tokens, made, grad_logprob=whole(g), grad_entropy=whole(h), grad_lse=whole(z),
+                                           temperature=ctx.temperature), None, None, None, None
+
+        class AprilEmbed(t.autograd.Function):
+            @staticmethod
+            def forward(ctx, table, tokens, scale, dtype):
+                ctx.save_for_backward(tokens)
+                ctx.of = table.shape[0], table.dtype, scale
+                return _embed(table, tokens, scale, dtype, None)
+
+            @staticmethod
+            @once
+            def backward(ctx, g):
+                vocab, dtype, scale = ctx.of
+                g = g if g.stride(1) == 1 or g.shape[1] == 1 else g.contiguous()
+                return april_embed_grad(g, *ctx.saved_tensors, vocab, scale=scale, dtype=dtype), None, None, None
+
+        class AprilExpertGather(t.autograd.Function):
+            @staticmethod
+            def forward(ctx, x, starts, source, position):
+                ctx.save_for_backward(starts, source, position)
+                return _expert_gather(x, ExpertRows(starts, source, position), None)
+
+            @staticmethod
+            @once
+            def backward(ctx, g):
+                g = g if g.stride(1) == 1 or g.shape[1] == 1 else g.contiguous()
+                return _expert_combine(g, ExpertRows(*ctx.saved_tensors), None, None), None, None, None
+
+        class AprilExpertCombine(t.autograd.Function):
+            @staticmethod
+            def forward(ctx, packed, starts, source, position, weights):
+                ctx.save_for_backward(packed, starts, source, position, weights)
+                return _expert_combine(packed, ExpertRows(starts, source, position), weights, None)
+
+            @staticmethod
+            @once
+            def backward(ctx, g):
+                packed, starts, source, position, weights = ctx.saved_tensors
+                g = g if g.stride(1) == 1 or g.shape[1] == 1 else g.contiguous()
+                of_packed, of_weights = april_expert_combine_grad(g, packed, ExpertRows(starts, source, position), weights, of_packed=ctx.needs_input_grad[0],
+                                                                  of_weights=ctx.needs_input_grad[4])
+                return of_packed, None, None, None, of_weights
+
+        _functions.update(logprobs=AprilLogprobs, embed=AprilEmbed, gather=AprilExpertGather, combine=AprilExpertCombine)
+    return _functions[name]
+
+
+def _logprobs(logits, tokens, temperature, entropy, top):
+    n, vocab = _two("logits", logits)
+    dev, dtype = _gpu("logits", logits), _dtype("logits", logits.dtype)
+    if top < 0:
+        _refuse("top: %d is below zero", top)
+    p, row = _matrix("logits", logits, logits.dtype, (n, vocab), dev)
+    tp, bits = _index("tokens", tokens, (n,), dev)
+    e = lambda *shape, t=_torch.float32: _torch.empty(shape, dtype=t, device=logits.device)  # noqa: E731
+    got = Logprobs(e(n), e(n) if entropy else None, e(n), e(n, top) if top else None, e(n, top, t=_torch.int32) if top else None, e(n, 2))
+    fields = (n, vocab, dtype, bits, top, temperature, row, p, tp, got.logprob.data_ptr(), got.entropy.data_ptr() if entropy else 0, got.lse.data_ptr(),
+              got.norm.data_ptr(), got.top_logprobs.data_ptr() if top else 0, got.top_ids.data_ptr() if top else 0)
+    space, at, need = _space("april_logprobs_workspace", _PACK_LOGPROBS, fields, logits.device)
+    _enqueue(_call("april_logprobs"), dev, _PACK_LOGPROBS, *fields, at, need)
+    return got
+
+
+def april_logprobs(logits, tokens, *, temperature: float = 1.0, entropy: bool = False, top: int = 0) -> Logprobs:
+    """log softmax(logits / temperature)[token] of each row of logits [n_rows, vocab] (bf16 or fp32), tokens [n_rows] (int32 or int64; below zero: a
+    padding row, zeros), log of the sum of exponentials, and as asked for the entropy and the `top` (at most 64) most likely tokens with their
+    log-probabilities.  Differentiable: logprob, entropy, lse."""
+    if _records(logits):
+        return Logprobs(*_function("logprobs").apply(logits, tokens, temperature, entropy, top))
+    return _logprobs(logits, tokens, temperature, entropy, top)
+
+
+def april_logprobs_grad(logits, tokens, made: Logprobs, *, grad_logprob=None, grad_entropy=None, grad_lse=None, temperature: float = 1.0, out=None):
+    """Gradient of the logits, of their type.  made: april_logprobs' of the same arguments (its norm, and its entropy for grad_entropy); grad_*
+    [n_rows]: fp32, None is zero.  out may be the logits themselves, which are then overwritten.  Not differentiable."""
+    _no_gradient(logits=logits, grad_logprob=grad_logprob, grad_entropy=grad_entropy, grad_lse=grad_lse, out=out)
+    n, vocab = _two("logits", logits)
+    dev, dtype = _gpu("logits", logits), _dtype("logits", logits.dtype)
+    p, row = _matrix("logits", logits, logits.dtype, (n, vocab), dev)
+    tp, bits = _index("tokens", tokens, (n,), dev)
+    if grad_entropy is not None and made.entropy is None:
+        _refuse("grad_entropy: april_logprobs was not asked for the entropy")
+    if out is None:
+        out = _torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
+    op, o_row = _matrix("out", out, logits.dtype, (n, vocab), dev)
+    _enqueue(_call("april_logprobs_grad"), dev, _PACK_LOGPROBS_GRAD, n, vocab, dtype, bits, temperature, 0, row, o_row, p, tp, _float_ptr("made.norm", made.norm, (n, 2), dev),
+             0 if grad_entropy is None else _float_ptr("made.entropy", made.entropy, (n,), dev), _float_ptr("grad_logprob", grad_logprob, (n,), dev),
+             _float_ptr("grad_entropy", grad_entropy, (n,), dev), _float_ptr("grad_lse", grad_lse, (n,), dev), op)
+    return out
+
+
+def _embed(table, tokens, scale, dtype, out):
+    vocab, d = _two("table", table)
+    dev, of = _gpu("table", table), _dtype("table", table.dtype)
+    if len(tokens.shape) != 1:
+        _refuse("tokens: one dimension wanted, not %s", tuple(tokens.shape))
+    n = tokens.shape[0]
+    if out is None:
+        out = _torch.empty((n, d), dtype=table.dtype if dtype is None else dtype, device=table.device)
+    elif dtype is not None and out.dtype is not dtype:
+        _refuse("out: %s wanted, not %s", dtype, out.dtype)
+    to = _dtype("out", out.dtype)
+    p, row = _matrix("table", table, table.dtype, (vocab, d), dev)
+    op, o_row = _matrix("out", out, out.dtype, (n, d), dev)
+    tp, bits = _index("tokens", tokens, (n,), dev)
+    _enqueue(_call("april_embed"), dev, _PACK_EMBED, n, vocab, d, of, to, bits, scale, 0, row, o_row, p, tp, op)
+    return out
+
+
+def april_embed(table, tokens, *, scale: float = 1.0, dtype=None, out=None):
+    """scale * table[tokens] [n_rows, d] (bf16 or fp32, as dtype or out says; else of the table's type) for tokens [n_rows] (int32 or int64; below zero:
+    padding, zeros).  Differentiable in the table, but not into an `out`."""
+    if _records(table, out):
+        if out is not None:
+            _differentiable("table" if table.requires_grad else "out")
+        return _function("embed").apply(table, tokens, scale, dtype)
+    return _embed(table, tokens, scale, dtype, out)
+
+
+def april_embed_grad(grad_out, tokens, vocab: int, *, scale: float = 1.0, dtype=None, out=None, accumulate: bool = False):
+    """Gradient [vocab, d] of april_embed's table (of type dtype or out's; else of grad_out's) for the gradient [n_rows, d] of its result.  accumulate: added to
+    `out`, of which the rows of no token are not touched.  Not differentiable."""
+    _no_gradient(grad_out=grad_out, out=out)
+    n, d = _two("grad_out", grad_out)
+    dev, of = _gpu("grad_out", grad_out), _dtype("grad_out", grad_out.dtype)
+    if out is None:
+        if accumulate:
+            _refuse("accumulate: no `out` to add to")
+        if vocab < 1:
+            _refuse("vocab: %d is below one", vocab)
+        out = _torch.empty((vocab, d), dtype=grad_out.dtype if dtype is None else dtype, device=grad_out.device)
+    elif dtype is not None and out.dtype is not dtype:
+        _refuse("out: %s wanted, not %s", dtype, out.dtype)
+    to = _dtype("out", out.dtype)
+    p, row = _matrix("grad_out", grad_out, grad_out.dtype, (n, d), dev)
+    op, o_row = _matrix("out", out, out.dtype, (vocab, d), dev)
+    tp, bits = _index("tokens", tokens, (n,), dev)
+    fields = n, vocab, d, of, to, bits, scale, 1 if accumulate else 0, row, o_row, p, tp, op
+    space, at, need = _space("april_embed_grad_workspace", _PACK_EMBED_GRAD, fields, grad_out.device)
+    _enqueue(_call("april_embed_grad"), dev, _PACK_EMBED_GRAD, *fields, at, need)
+    return out
+
+
+def april_expert_sort(ids, n_experts: int, *, align: int = 1) -> ExpertRows:
+    """The assignments ids [n_rows, k] (int32 or int64; outside 0..n_experts - 1: left out) sorted by expert, each expert's packed rows from a multiple of
+    `align` on.  The packed arrays have as many rows as the largest shares of the experts could take: source.shape[0]."""
+    n, k = _two("ids", ids)
+    dev = _gpu("ids", ids)
+    p, bits = _index("ids", ids, (n, k), dev)
+    if n_experts < 1 or align < 1:
+        _refuse("n_experts and align: at least one wanted")
+    m = (n * k + min(n_experts, n * k) * (align - 1)) // align * align
+    e = lambda *shape: _torch.empty(shape, dtype=_torch.int32, device=ids.device)  # noqa: E731
+    rows = ExpertRows(e(n_experts + 1), e(m), e(n, k))
+    fields = n, k, n_experts, align, m, bits, p, rows.starts.data_ptr(), rows.source.data_ptr(), rows.position.data_ptr()
+    space, at, need = _space("april_expert_sort_workspace", _PACK_EXPERT_SORT, fields, ids.device)
+    _enqueue(_call("april_expert_sort"), dev, _PACK_EXPERT_SORT, *fields, at, need)
+    return rows
+
+
+def _expert_sizes(rows, dev):
+    """(rows, experts of a row, packed rows, pointer of source, of position)."""
+    n, k = _two("rows.position", rows.position)
+    if len(rows.source.shape) != 1:
+        _refuse("rows.source: one dimension wanted")
+    m = rows.source.shape[0]
+    return n, k, m, _ptr("rows.source", rows.source, _torch.int32, (m,), dev), _ptr("rows.position", rows.position, _torch.int32, (n, k), dev)
+
+
+def _expert_gather(x, rows, out):
+    d = _two("x", x)[1]
+    dev, dtype = _gpu("x", x), _dtype("x", x.dtype)
+    n, k, m, source, position = _expert_sizes(rows, dev)
+    if out is None:
+        out = _torch.empty((m, d), dtype=x.dtype, device=x.device)
+    p, row = _matrix("x", x, x.dtype, (n, d), dev)
+    op, o_row = _matrix("out", out, x.dtype, (m, d), dev)
+    _enqueue(_call("april_expert_gather"), dev, _PACK_EXPERT_GATHER, n, k, d, m, dtype, 0, row, o_row, p, source, position, op)
+    return out
+
+
+def april_expert_gather(x, rows: ExpertRows, *, out=None):
+    """The tokens' rows x [n_rows, d] (bf16 or fp32) in the order of their experts; packed rows of no assignment are zeros.  Differentiable in x, but not
+    into an `out`."""
+    if _records(x, out):
+        if out is not None:
+            _differentiable("x" if x.requires_grad else "out")
+        return _function("gather").apply(x, *rows)
+    return _expert_gather(x, rows, out)
+
+
+def _expert_combine(packed, rows, weights, out):
+    m, d = _two("packed", packed)
+    dev, dtype = _gpu("packed", packed), _dtype("packed", packed.dtype)
+    n, k, m, _, position = _expert_sizes(rows, dev)
+    if out is None:
+        out = _torch.empty((n, d), dtype=packed.dtype, device=packed.device)
+    p, row = _matrix("packed", packed, packed.dtype, (m, d), dev)
+    op, o_row = _matrix("out", out, packed.dtype, (n, d), dev)
+    _enqueue(_call("april_expert_combine"), dev, _PACK_EXPERT_COMBINE, n, k, d, m, dtype, 0, row, o_row, p, position, _float_ptr("weights", weights, (n, k), dev), op)
+    return out
+
+
+def april_expert_combine(packed, rows: ExpertRows, weights=None, *, out=None):
+    """What the experts made of their rows, packed [source.shape[0], d] (bf16 or fp32), summed for each token by weights [n_rows, k] (fp32; None: 1), in the order
+    of the token's experts.  Differentiable in packed and weights, but not into an `out`."""
+    if _records(packed, weights, out):
+        if out is not None:
+            _differentiable("packed" if packed.requires_grad else "weights" if weights is not None and weights.requires_grad else "out")
+        return _function("combine").apply(packed, *rows, weights)
+    return _expert_combine(packed, rows, weights, out)
+
+
+def april_expert_combine_grad(grad_out, packed, rows: ExpertRows, weights=None, *, of_packed: bool = True, of_weights: bool = True):
+    """(gradient of packed, gradient of weights) for the gradient [n_rows, d] of april_expert_combine's result; None where not asked for.  Not differentiable."""
+    _no_gradient(grad_out=grad_out, packed=packed, weights=weights)
+    d = _two("grad_out", grad_out)[1]
+    dev, dtype = _gpu("grad_out", grad_out), _dtype("grad_out", grad_out.dtype)
+    n, k, m, source, position = _expert_sizes(rows, dev)
+    g, row = _matrix("grad_out", grad_out, grad_out.dtype, (n, d), dev)
+    p, p_row = _matrix("packed", packed, grad_out.dtype, (m, d), dev)
+    g_packed = _torch.empty((m, d), dtype=packed.dtype, device=packed.device) if of_packed else None
+    g_weights = _torch.empty((n, k), dtype=_torch.float32, device=packed.device) if of_weights else None
+    _enqueue(_call("april_expert_combine_grad"), dev, _PACK_EXPERT_COMBINE_GRAD, n, k, d, m, dtype, 0, row, p_row, d, g, p, source, position,
+             _float_ptr("weights", weights, (n, k), dev), g_packed.data_ptr() if of_packed else 0, g_weights.data_ptr() if of_weights else 0)
+    return g_packed, g_weights
 
 
 # ---------------------------------------------------------------------------
