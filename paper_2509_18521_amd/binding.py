@@ -694,7 +694,7 @@ def april_cache_attention(q, pool, block_table, lens, max_len: int, *, q_start=N
 # same leaf tensors that was recorded outside the capture may be alive meanwhile.  The gradients' own calls (april_*_grad) have no such bound.
 # ---------------------------------------------------------------------------
 class Logprobs(NamedTuple):
-    """What april_logprobs leaves, see april.h (entropy None, top_* None where they were not asked for)."""
+    """What april_logprobs leaves, see april.h (None: not asked for)."""
     logprob: object
     entropy: object
     lse: object
@@ -782,8 +782,8 @@ def _function(name):
 
         class AprilLogprobs(t.autograd.Function):
             @staticmethod
-            def forward(ctx, logits, tokens, temperature, entropy, top):
-                got = _logprobs(logits, tokens, temperature, entropy, top)
+            def forward(ctx, logits, tokens, temperature, entropy, lse, top):
+                got = _logprobs(logits, tokens, temperature, entropy, lse, top)
                 ctx.set_materialize_grads(False)
                 ctx.mark_non_differentiable(*(x for x in got[3:] if x is not None))
                 ctx.save_for_backward(logits, tokens, got.norm, got.entropy)
@@ -794,11 +794,11 @@ def _function(name):
             @once
             def backward(ctx, g, h, z, *_):
                 if g is None and h is None and z is None:
-                    return (None,) * 5
+                    return (None,) * 6
                 logits, tokens, norm, entropy = ctx.saved_tensors
                 made = Logprobs(None, entropy, None, None, None, norm)
                 return april_logprobs_grad(logits, tokens, made, grad_logprob=whole(g), grad_entropy=whole(h), grad_lse=whole(z),
-                                           temperature=ctx.temperature), None, None, None, None
+                                           temperature=ctx.temperature), None, None, None, None, None
 
         class AprilEmbed(t.autograd.Function):
             @staticmethod
@@ -845,29 +845,33 @@ def _function(name):
     return _functions[name]
 
 
-def _logprobs(logits, tokens, temperature, entropy, top):
+def _logprobs(logits, tokens, temperature, entropy, lse, top):
     n, vocab = _two("logits", logits)
     dev, dtype = _gpu("logits", logits), _dtype("logits", logits.dtype)
     if top < 0:
         _refuse("top: %d is below zero", top)
     p, row = _matrix("logits", logits, logits.dtype, (n, vocab), dev)
     tp, bits = _index("tokens", tokens, (n,), dev)
-    e = lambda *shape, t=_torch.float32: _torch.empty(shape, dtype=t, device=logits.device)  # noqa: E731
-    got = Logprobs(e(n), e(n) if entropy else None, e(n), e(n, top) if top else None, e(n, top, t=_torch.int32) if top else None, e(n, 2))
-    fields = (n, vocab, dtype, bits, top, temperature, row, p, tp, got.logprob.data_ptr(), got.entropy.data_ptr() if entropy else 0, got.lse.data_ptr(),
-              got.norm.data_ptr(), got.top_logprobs.data_ptr() if top else 0, got.top_ids.data_ptr() if top else 0)
-    space, at, need = _space("april_logprobs_workspace", _PACK_LOGPROBS, fields, logits.device)
+    empty, f32, device = _torch.empty, _torch.float32, logits.device
+    logprob, norm = empty(n, dtype=f32, device=device), empty((n, 2), dtype=f32, device=device)
+    entropy = empty(n, dtype=f32, device=device) if entropy else None
+    lse = empty(n, dtype=f32, device=device) if lse else None
+    best = empty((n, top), dtype=f32, device=device) if top else None
+    ids = empty((n, top), dtype=_torch.int32, device=device) if top else None
+    fields = (n, vocab, dtype, bits, top, temperature, row, p, tp, logprob.data_ptr(), 0 if entropy is None else entropy.data_ptr(), 0 if lse is None else lse.data_ptr(),
+              norm.data_ptr(), best.data_ptr() if top else 0, ids.data_ptr() if top else 0)
+    space, at, need = _space("april_logprobs_workspace", _PACK_LOGPROBS, fields, device)
     _enqueue(_call("april_logprobs"), dev, _PACK_LOGPROBS, *fields, at, need)
-    return got
+    return Logprobs(logprob, entropy, lse, best, ids, norm)
 
 
-def april_logprobs(logits, tokens, *, temperature: float = 1.0, entropy: bool = False, top: int = 0) -> Logprobs:
+def april_logprobs(logits, tokens, *, temperature: float = 1.0, entropy: bool = False, lse: bool = False, top: int = 0) -> Logprobs:
     """log softmax(logits / temperature)[token] of each row of logits [n_rows, vocab] (bf16 or fp32), tokens [n_rows] (int32 or int64; below zero: a
-    padding row, zeros), log of the sum of exponentials, and as asked for the entropy and the `top` (at most 64) most likely tokens with their
+    padding row, zeros), and as asked for the entropy, the log of the sum of exponentials, and the `top` (at most 64) most likely tokens with their
     log-probabilities.  Differentiable: logprob, entropy, lse."""
     if _records(logits):
-        return Logprobs(*_function("logprobs").apply(logits, tokens, temperature, entropy, top))
-    return _logprobs(logits, tokens, temperature, entropy, top)
+        return Logprobs(*_function("logprobs").apply(logits, tokens, temperature, entropy, lse, top))
+    return _logprobs(logits, tokens, temperature, entropy, lse, top)
 
 
 def april_logprobs_grad(logits, tokens, made: Logprobs, *, grad_logprob=None, grad_entropy=None, grad_lse=None, temperature: float = 1.0, out=None):

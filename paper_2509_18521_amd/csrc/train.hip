@@ -243,7 +243,7 @@ int april_expert_combine_grad(const april_expert_combine_grad_args* a) {
   if (!a) REFUSE("april_expert_combine_grad: null argument");
   ExpertRows k;
   if (const int rc = expert_rows("april_expert_combine_grad", a->n_rows, a->k, a->d, a->n_packed, a->dtype, a->reserved, &k); rc != APRIL_OK) return rc;
-  if ((a->n_rows == 0 && a->n_packed == 0) || (!a->grad_packed && !a->grad_weights)) return APRIL_OK;
+  if ((a->n_packed == 0 || !a->grad_packed) && (a->n_rows == 0 || !a->grad_weights)) return APRIL_OK;
   if ((a->n_packed > 0 && (!a->source || (a->grad_weights && !a->packed))) || (a->n_rows > 0 && (!a->grad_out || !a->position))) REFUSE("april_expert_combine_grad: null array");
   const size_t e = element(a->dtype);
   if (!aligned(a->grad_out, e) || !aligned(a->packed, e) || !aligned(a->grad_packed, e) || !aligned(a->source, 4) || !aligned(a->position, 4) || !aligned(a->weights, 4) ||

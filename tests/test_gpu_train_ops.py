@@ -122,7 +122,7 @@ def check_logprobs(x, tokens, t, *, temperature=1.0, top=0, bits=64, pad=0, off=
     """The operator on these logits against the plain form; returns (logits on the GPU, its result, the logits in 64 bits)."""
     logits = place(x, t, pad, off)
     x = host(logits)
-    got = ap().april_logprobs(logits, index(tokens, bits), temperature=temperature, entropy=True, top=top)
+    got = ap().april_logprobs(logits, index(tokens, bits), temperature=temperature, entropy=True, lse=True, top=top)
     lp, ent, lse, best, ids = tr.logprobs(x, tokens, temperature, top)
     vocab = x.shape[1]
     m = np.max(np.where(np.isfinite(x), x, -np.inf), axis=1)
@@ -168,7 +168,7 @@ def test_logprobs_of_few_and_many_rows(n):
     x = hard_logits(rng, n, 9000, "bf16")
     tokens = rng.integers(0, 9000, size=n)
     logits, got, _ = check_logprobs(x, tokens, "bf16", top=20)
-    again = ap().april_logprobs(logits, index(tokens, 32), entropy=True, top=20)
+    again = ap().april_logprobs(logits, index(tokens, 32), entropy=True, lse=True, top=20)
     for a, b in zip(got, again):
         assert np.array_equal(host(a), host(b), equal_nan=True)
 
@@ -250,7 +250,7 @@ def test_logprobs_autograd_is_the_gradient():
     x = rng.standard_normal((6, 50)).astype(np.float32)
     tokens = index([3, 49, -1, 0, 7, 7], 64)
     leaf = torch.as_tensor(x).cuda().requires_grad_()
-    got = ap().april_logprobs(leaf, tokens, temperature=0.8, entropy=True, top=4)
+    got = ap().april_logprobs(leaf, tokens, temperature=0.8, entropy=True, lse=True, top=4)
     assert not got.top_logprobs.requires_grad and not got.top_ids.requires_grad and not got.norm.requires_grad
     (got.logprob.sum() + 0.3 * got.entropy.mean() - got.lse.square().sum()).backward()
     lse = tr.logprobs(x, host(tokens), 0.8)[2]
@@ -640,14 +640,14 @@ def test_on_another_stream():
     import torch
     rng = np.random.default_rng(22)
     x, tokens = place(rng.standard_normal((50, 3001)), "bf16"), index(rng.integers(0, 3001, size=50), 32)
-    want = ap().april_logprobs(x, tokens, entropy=True, top=9)
+    want = ap().april_logprobs(x, tokens, entropy=True, lse=True, top=9)
     side = torch.cuda.Stream()
     y = torch.zeros_like(x)
     torch.cuda.synchronize()
     with torch.cuda.stream(side):
         torch.cuda._sleep(2_000_000)
         y.copy_(x)                                           # (only that stream waits for this)
-        got = ap().april_logprobs(y, tokens, entropy=True, top=9)
+        got = ap().april_logprobs(y, tokens, entropy=True, lse=True, top=9)
     side.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
