@@ -150,7 +150,7 @@ struct TopShared {
   alignas(16) unsigned group[GROUPS];
   float tops[SECTIONS][NT];
   unsigned short hot[SECTIONS * NT];      // section * NT + thread
-  alignas(16) unsigned long long cand[MAX_CAND];
+  alignas(16) unsigned long long cand[MAX_CAND + 8];
   unsigned long long best[NT / 64];
   static_assert(NT == GROUPS || NT == 2 * GROUPS, "one or two threads a group");
   alignas(8) unsigned char bits[NT];
@@ -176,21 +176,33 @@ template <typename T, int NT>
 __device__ void collect(TopShared<NT>& sh, const Run<T>& r, unsigned from) {
   constexpr int V = Vec<T>::N;
   const int n_hot = sh.n_hot, each = section_vectors<NT>(r.nv);
-  auto take = [&](float x, int place) {
-    const unsigned key = f2key(x);
-    if (key >= from) {
-      const int at = atomicAdd(&sh.n_cand, 1);
-      if (at < MAX_CAND) sh.cand[at] = pair_of(key, place);
-    }
-  };
   for (int i = threadIdx.x; i < n_hot * each; i += NT) {
     const int h = i / each, at = sh.hot[h], v = ((at / NT) * each + i - h * each) * NT + at % NT;
     if (v >= r.nv) continue;
     const auto x = r.vector(v);
+    unsigned key[V], hits = 0;
 #pragma unroll
-    for (int j = 0; j < V; ++j) take((float)x[j], r.place(v) + j);
+    for (int j = 0; j < V; ++j) {
+      key[j] = f2key((float)x[j]);
+      hits |= (key[j] >= from ? 1u : 0u) << j;
+    }
+    if (hits == 0) continue;
+    int to = atomicAdd(&sh.n_cand, __popc(hits));
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (hits >> j & 1) {
+        if (to < MAX_CAND) sh.cand[to] = pair_of(key[j], r.place(v) + j);
+        ++to;
+      }
   }
-  if ((int)threadIdx.x < r.singles) take((float)r.p[r.single(threadIdx.x)], r.single(threadIdx.x));
+  if ((int)threadIdx.x < r.singles) {
+    const int place = r.single(threadIdx.x);
+    const unsigned key = f2key((float)r.p[place]);
+    if (key >= from) {
+      const int to = atomicAdd(&sh.n_cand, 1);
+      if (to < MAX_CAND) sh.cand[to] = pair_of(key, place);
+    }
+  }
   __syncthreads();
 }
 
@@ -304,12 +316,22 @@ __device__ void find_top(TopShared<NT>& sh, const Run<T>& r, int k, float top, b
 }
 
 // put(rank, candidate) for the k first of n candidates (no two are equal).
+// All threads call; the list has room for 7 more.
 template <int NT, class F>
-__device__ inline void rank_candidates(const unsigned long long* cand, int n, int k, F put) {
+__device__ inline void rank_candidates(unsigned long long* cand, int n, int k, F put) {
+  const int end = (n + 7) / 8 * 8;
+  if ((int)threadIdx.x < end - n) cand[n + threadIdx.x] = 0ull;
+  __syncthreads();
   for (int c = threadIdx.x; c < n; c += NT) {
     const unsigned long long own = cand[c];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += cand[j] > own;
+    for (int j = 0; j < end; j += 8) {
+      ulonglong2 x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = reinterpret_cast<const ulonglong2*>(cand + j)[i];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rank += (x[i].x > own) + (x[i].y > own);
+    }
     if (rank < k) put(rank, own);
   }
 }
@@ -437,7 +459,7 @@ constexpr int JOIN_THREADS = 256, MAX_PARTS = 32;
 // more, nothing below the smallest of those is among the n_top largest.
 template <typename T>
 __global__ __launch_bounds__(JOIN_THREADS) void logprobs_join_kernel(Logprobs a, int parts) {
-  __shared__ alignas(16) unsigned long long cand[MAX_CAND];
+  __shared__ alignas(16) unsigned long long cand[MAX_CAND + 8];
   __shared__ unsigned long long least;
   __shared__ int n_cand;
   const int tid = threadIdx.x, r = blockIdx.x;
