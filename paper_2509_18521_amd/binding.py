@@ -796,9 +796,7 @@ def _function(name):
                 if g is None and h is None and z is None:
                     return (None,) * 6
                 logits, tokens, norm, entropy = ctx.saved_tensors
-                made = Logprobs(None, entropy, None, None, None, norm)
-                return april_logprobs_grad(logits, tokens, made, grad_logprob=whole(g), grad_entropy=whole(h), grad_lse=whole(z),
-                                           temperature=ctx.temperature), None, None, None, None, None
+                return _logprobs_grad(logits, tokens, norm, None if h is None else entropy, whole(g), whole(h), whole(z), ctx.temperature), None, None, None, None, None
 
         class AprilEmbed(t.autograd.Function):
             @staticmethod
@@ -874,23 +872,36 @@ def april_logprobs(logits, tokens, *, temperature: float = 1.0, entropy: bool = 
     return _logprobs(logits, tokens, temperature, entropy, lse, top)
 
 
+def _logprobs_grad(logits, tokens, norm, entropy, g, h, z, temperature, out=None):
+    """(The arguments are checked.)"""
+    n, vocab = logits.shape
+    if out is None:
+        out = _torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
+    ptr = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
+    _enqueue(_call("april_logprobs_grad"), logits.get_device(), _PACK_LOGPROBS_GRAD, n, vocab, APRIL_DTYPE_FP32 if logits.dtype is _torch.float32 else APRIL_DTYPE_BF16,
+             64 if tokens.dtype is _torch.int64 else 32, temperature, 0, logits.stride(0), out.stride(0), logits.data_ptr(), tokens.data_ptr(), norm.data_ptr(), ptr(entropy),
+             ptr(g), ptr(h), ptr(z), out.data_ptr())
+    return out
+
+
 def april_logprobs_grad(logits, tokens, made: Logprobs, *, grad_logprob=None, grad_entropy=None, grad_lse=None, temperature: float = 1.0, out=None):
     """Gradient of the logits, of their type.  made: april_logprobs' of the same arguments (its norm, and its entropy for grad_entropy); grad_*
     [n_rows]: fp32, None is zero.  out may be the logits themselves, which are then overwritten.  Not differentiable."""
     _no_gradient(logits=logits, grad_logprob=grad_logprob, grad_entropy=grad_entropy, grad_lse=grad_lse, out=out)
     n, vocab = _two("logits", logits)
-    dev, dtype = _gpu("logits", logits), _dtype("logits", logits.dtype)
-    p, row = _matrix("logits", logits, logits.dtype, (n, vocab), dev)
-    tp, bits = _index("tokens", tokens, (n,), dev)
+    dev = _gpu("logits", logits)
+    _dtype("logits", logits.dtype)
+    _matrix("logits", logits, logits.dtype, (n, vocab), dev)
+    _index("tokens", tokens, (n,), dev)
+    if out is not None:
+        _matrix("out", out, logits.dtype, (n, vocab), dev)
     if grad_entropy is not None and made.entropy is None:
         _refuse("grad_entropy: april_logprobs was not asked for the entropy")
-    if out is None:
-        out = _torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
-    op, o_row = _matrix("out", out, logits.dtype, (n, vocab), dev)
-    _enqueue(_call("april_logprobs_grad"), dev, _PACK_LOGPROBS_GRAD, n, vocab, dtype, bits, temperature, 0, row, o_row, p, tp, _float_ptr("made.norm", made.norm, (n, 2), dev),
-             0 if grad_entropy is None else _float_ptr("made.entropy", made.entropy, (n,), dev), _float_ptr("grad_logprob", grad_logprob, (n,), dev),
-             _float_ptr("grad_entropy", grad_entropy, (n,), dev), _float_ptr("grad_lse", grad_lse, (n,), dev), op)
-    return out
+    _float_ptr("made.norm", made.norm, (n, 2), dev)
+    entropy = None if grad_entropy is None else made.entropy
+    for name, t in (("made.entropy", entropy), ("grad_logprob", grad_logprob), ("grad_entropy", grad_entropy), ("grad_lse", grad_lse)):
+        _float_ptr(name, t, (n,), dev)
+    return _logprobs_grad(logits, tokens, made.norm, entropy, grad_logprob, grad_entropy, grad_lse, temperature, out)
 
 
 def _embed(table, tokens, scale, dtype, out):
