@@ -177,6 +177,7 @@ __device__ void collect(TopShared<NT>& sh, const Run<T>& r, unsigned from) {
   constexpr int V = Vec<T>::N;
   const int n_hot = sh.n_hot, each = section_vectors<NT>(r.nv);
   for (int i = threadIdx.x; i < n_hot * each; i += NT) {
+    if (*static_cast<volatile int*>(&sh.n_cand) > MAX_CAND) break;                 // (more than the list holds: the count does not matter)
     const int h = i / each, at = sh.hot[h], v = ((at / NT) * each + i - h * each) * NT + at % NT;
     if (v >= r.nv) continue;
     const auto x = r.vector(v);
@@ -532,10 +533,11 @@ struct GradRow {
   }
 };
 
-template <typename T, bool ENT, bool VEC>
+template <typename T, bool ENT>
 __global__ __launch_bounds__(GRAD_THREADS) void logprobs_grad_kernel(LogprobsGrad a, int chunks) {
   typedef typename Vec<T>::type vec;
-  constexpr int V = VEC ? Vec<T>::N : 1;
+  typedef vec at_element __attribute__((aligned(sizeof(T))));     // (grad's rows may lie to a 16-byte border otherwise than the logits')
+  constexpr int V = Vec<T>::N;
   const long long items = (long long)a.n_rows * chunks;
   for (long long item = blockIdx.x; item < items; item += gridDim.x) {
     const int r = (int)(item / chunks), chunk = (int)(item - (long long)r * chunks);
@@ -551,50 +553,41 @@ __global__ __launch_bounds__(GRAD_THREADS) void logprobs_grad_kernel(LogprobsGra
       const float v = pad ? 0.f : f((float)row[i]) + (i == tok ? f.add : 0.f);
       out[i] = (T)v;
     };
-    if constexpr (!VEC) {
-      const int i0 = chunk * (GRAD_THREADS * 16), i1 = min(a.vocab - i0, GRAD_THREADS * 16);
-      for (int i = threadIdx.x; i < i1; i += GRAD_THREADS) single(i0 + i);
-      continue;
-    } else {
-      const Run<T> run(row, a.vocab);
-      T* to = out + run.head;
-      const int v0 = chunk * (GRAD_THREADS * GRAD_VECS) + threadIdx.x;
-      vec x[GRAD_VECS];
-      if (!pad) {
+    const Run<T> run(row, a.vocab);
+    T* to = out + run.head;
+    const int v0 = chunk * (GRAD_THREADS * GRAD_VECS) + threadIdx.x;
+    vec x[GRAD_VECS];
+    if (!pad) {
 #pragma unroll
-        for (int u = 0; u < GRAD_VECS; ++u)
-          if (v0 + u * GRAD_THREADS < run.nv) x[u] = run.vector(v0 + u * GRAD_THREADS);
-      }
-#pragma unroll
-      for (int u = 0; u < GRAD_VECS; ++u) {
-        const int v = v0 + u * GRAD_THREADS;
-        if (v >= run.nv) break;
-        vec y{};
-        if (!pad) {
-          const long long at = tok - run.place(v);
-#pragma unroll
-          for (int i = 0; i < V; ++i) y[i] = (T)f((float)x[u][i]);
-          if (at >= 0 && at < V) {
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-              if (i == at) y[i] = (T)(f((float)x[u][i]) + f.add);
-          }
-        }
-        *reinterpret_cast<vec*>(to + (size_t)v * V) = y;
-      }
-      if (chunk == 0 && (int)threadIdx.x < run.singles) single(run.single(threadIdx.x));
+      for (int u = 0; u < GRAD_VECS; ++u)
+        if (v0 + u * GRAD_THREADS < run.nv) x[u] = run.vector(v0 + u * GRAD_THREADS);
     }
+#pragma unroll
+    for (int u = 0; u < GRAD_VECS; ++u) {
+      const int v = v0 + u * GRAD_THREADS;
+      if (v >= run.nv) break;
+      vec y{};
+      if (!pad) {
+        const long long at = tok - run.place(v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) y[i] = (T)f((float)x[u][i]);
+        if (at >= 0 && at < V) {
+#pragma unroll
+          for (int i = 0; i < V; ++i)
+            if (i == at) y[i] = (T)(f((float)x[u][i]) + f.add);
+        }
+      }
+      *reinterpret_cast<at_element*>(to + (size_t)v * V) = y;
+    }
+    if (chunk == 0 && (int)threadIdx.x < run.singles) single(run.single(threadIdx.x));
   }
 }
 
 template <typename T, bool ENT>
 hipError_t logprobs_grad(hipStream_t st, const LogprobsGrad& a) {
-  // vectors where both arrays' rows lie alike to a 16-byte border
-  const long long diff = (long long)(reinterpret_cast<uintptr_t>(a.logits) - reinterpret_cast<uintptr_t>(a.grad));
-  const bool vec = diff % 16 == 0 && (a.row - a.grad_row) * (long long)sizeof(T) % 16 == 0;
-  const int per = GRAD_THREADS * (vec ? GRAD_VECS * Vec<T>::N : 16), chunks = std::max(1, (a.vocab - 1) / per + 1);
+  const int per = GRAD_THREADS * GRAD_VECS * Vec<T>::N, chunks = std::max(1, (a.vocab - 1) / per + 1);
   const dim3 grid((unsigned)std::min<long long>((long long)a.n_rows * chunks, 1 << 22));
-  return vec ? enqueue(logprobs_grad_kernel<T, ENT, true>, grid, dim3(GRAD_THREADS), st, a, chunks) : enqueue(logprobs_grad_kernel<T, ENT, false>, grid, dim3(GRAD_THREADS), st, a, chunks);
+  return enqueue(logprobs_grad_kernel<T, ENT>, grid, dim3(GRAD_THREADS), st, a, chunks);
 }
 
 }  // namespace

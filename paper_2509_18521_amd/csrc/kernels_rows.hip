@@ -265,73 +265,65 @@ __global__ __launch_bounds__(SORT_THREADS) void expert_place_kernel(SortIn in, i
 int blocks_of(long long n, int per) { return (int)((n + per - 1) / per); }
 
 // ---------------------------------------------------------------------------
-// Rows as vectors of V elements: loads and stores of 16 bytes of the wider type where every row allows them, else single elements.
+// Rows as vectors of V elements, 16 bytes of the wider type, at any address of an element (the hardware takes 16-byte accesses there; rows of single elements took
+// 2 to 4 times as long); a row's last vector may have fewer, n (TAIL: rows where it has).
 // ---------------------------------------------------------------------------
-template <typename T, int V>
-struct Pack {
-  typedef T type __attribute__((ext_vector_type(V)));
-};
-template <typename T>
-struct Pack<T, 1> {
-  typedef T type;
-};
-template <typename T, int V>
-__device__ inline void load(float (&x)[V], const T* p) {
-  if constexpr (V * sizeof(T) > 16) {
-    float a[V / 2], b[V / 2];
-    load<T, V / 2>(a, p);
-    load<T, V / 2>(b, p + V / 2);
-#pragma unroll
-    for (int i = 0; i < V / 2; ++i) { x[i] = a[i]; x[V / 2 + i] = b[i]; }
-  } else if constexpr (V == 1) {
-    x[0] = (float)*p;
-  } else {
-    const auto v = *reinterpret_cast<const typename Pack<T, V>::type*>(p);
-#pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = (float)v[i];
-  }
-}
-template <typename T, int V>
-__device__ inline void store(T* p, const float (&x)[V]) {
-  if constexpr (V == 1) {
-    *p = (T)x[0];
-  } else {
-    typename Pack<T, V>::type v;
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = (T)x[i];
-    *reinterpret_cast<typename Pack<T, V>::type*>(p) = v;
-  }
-}
-// A vector as it lies in memory, and its elements.
 template <typename T, int V>
 struct Raw {
   static constexpr int PARTS = V * sizeof(T) > 16 ? 2 : 1, N = V / PARTS;
-  typename Pack<T, N>::type v[PARTS];
-  __device__ __forceinline__ void load(const T* p) {
-#pragma unroll
-    for (int i = 0; i < PARTS; ++i) v[i] = *reinterpret_cast<const typename Pack<T, N>::type*>(p + i * N);
-  }
+  typedef T vec __attribute__((ext_vector_type(N)));
+  typedef vec at_element __attribute__((aligned(sizeof(T))));
+  vec v[PARTS];
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int i = 0; i < PARTS; ++i) v[i] = typename Pack<T, N>::type{};
+    for (int i = 0; i < PARTS; ++i) v[i] = vec{};
   }
-  __device__ __forceinline__ float operator[](int i) const {
-    if constexpr (N == 1) return (float)v[i];
-    else return (float)v[i / N][i % N];
+  __device__ __forceinline__ void load(const T* p, int n = V) {
+    if (n == V) {
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) v[i] = *reinterpret_cast<const at_element*>(p + i * N);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i / N][i % N] = i < n ? p[i] : (T)0.f;
+    }
   }
+  __device__ __forceinline__ void store(T* p, int n = V) const {
+    if (n == V) {
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) *reinterpret_cast<at_element*>(p + i * N) = v[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (i < n) p[i] = v[i / N][i % N];
+    }
+  }
+  __device__ __forceinline__ float operator[](int i) const { return (float)v[i / N][i % N]; }
 };
+template <typename T, int V>
+__device__ inline void load(float (&x)[V], const T* p, int n) {
+  Raw<T, V> r;
+  r.load(p, n);
+#pragma unroll
+  for (int i = 0; i < V; ++i) x[i] = r[i];
+}
+template <typename T, int V>
+__device__ inline void store(T* p, const float (&x)[V], int n) {
+  Raw<T, V> r;
+#pragma unroll
+  for (int i = 0; i < V; ++i) r.v[i / r.N][i % r.N] = (T)x[i];
+  r.store(p, n);
+}
 template <int V>
 __device__ inline void zero(float (&x)[V]) {
 #pragma unroll
   for (int i = 0; i < V; ++i) x[i] = 0.f;
 }
+// Elements of vector `col` of a row of d.
+template <int V, bool TAIL>
+__device__ inline int elements(int d, int col) { return TAIL ? min(V, d - col * V) : V; }
 
 template <typename T> constexpr int wide() { return 16 / (int)sizeof(T); }
 template <typename A, typename B> constexpr int wide() { return 16 / (int)std::max(sizeof(A), sizeof(B)); }
-
-bool rows_aligned(const void* p, long long row, size_t element, int v) {
-  return reinterpret_cast<uintptr_t>(p) % (v * element) == 0 && row % v == 0;
-}
 
 // A workgroup of 256 threads takes 256 vectors at a time of the `per_row` x rows ones.
 constexpr int ROWS_THREADS = 256;
@@ -355,27 +347,26 @@ dim3 vector_grid(long long rows, int per_row) {
 // ---------------------------------------------------------------------------
 // Embedding: rows of the table, scaled.
 // ---------------------------------------------------------------------------
-template <typename TT, typename TO, int V>
+template <typename TT, typename TO, int V, bool TAIL>
 __global__ __launch_bounds__(ROWS_THREADS) void embed_kernel(Embed a, int per_row) {
   FOR_VECTORS(a.n_rows, per_row) {
     const long long tok = index_at(a.tokens, a.i64, at.row);
+    const int n = elements<V, TAIL>(a.d, at.col);
     float x[V];
     zero(x);
-    if (tok >= 0 && tok < a.vocab) load<TT, V>(x, static_cast<const TT*>(a.table) + tok * a.table_row + (long long)at.col * V);
+    if (tok >= 0 && tok < a.vocab) load<TT, V>(x, static_cast<const TT*>(a.table) + tok * a.table_row + (long long)at.col * V, n);
 #pragma unroll
     for (int i = 0; i < V; ++i) x[i] = tok < a.vocab ? x[i] * a.scale : NAN;
     if (tok < 0) zero(x);
-    store<TO, V>(static_cast<TO*>(a.out) + at.row * a.out_row + (long long)at.col * V, x);
+    store<TO, V>(static_cast<TO*>(a.out) + at.row * a.out_row + (long long)at.col * V, x, n);
   }
 }
 
 template <typename TT, typename TO>
 hipError_t embed(hipStream_t st, const Embed& a) {
   constexpr int V = wide<TT, TO>();
-  const bool vec = a.d % V == 0 && rows_aligned(a.table, a.table_row, sizeof(TT), V) && rows_aligned(a.out, a.out_row, sizeof(TO), V);
-  const int per_row = vec ? a.d / V : a.d;
-  const dim3 grid = vector_grid(a.n_rows, per_row), block(ROWS_THREADS);
-  return vec ? enqueue(embed_kernel<TT, TO, V>, grid, block, st, a, per_row) : enqueue(embed_kernel<TT, TO, 1>, grid, block, st, a, per_row);
+  const int per_row = blocks_of(a.d, V);
+  return enqueue(a.d % V == 0 ? embed_kernel<TT, TO, V, false> : embed_kernel<TT, TO, V, true>, vector_grid(a.n_rows, per_row), dim3(ROWS_THREADS), st, a, per_row);
 }
 
 // ---------------------------------------------------------------------------
@@ -392,17 +383,17 @@ struct Sorted {
 };
 
 template <typename TT, int V>
-__device__ inline void put_sum(const EmbedGrad& a, int token, int col, const float (&sum)[V]) {
+__device__ inline void put_sum(const EmbedGrad& a, int token, int col, const float (&sum)[V], int n) {
   TT* to = static_cast<TT*>(a.grad_table) + (long long)token * a.table_row + (long long)col * V;
   float x[V];
   zero(x);
-  if (a.accumulate) load<TT, V>(x, to);
+  if (a.accumulate) load<TT, V>(x, to, n);
 #pragma unroll
   for (int j = 0; j < V; ++j) x[j] += a.scale * sum[j];
-  store<TT, V>(to, x);
+  store<TT, V>(to, x, n);
 }
 
-template <typename TO, typename TT, int V>
+template <typename TO, typename TT, int V, bool TAIL>
 __global__ __launch_bounds__(256) void embed_sums_kernel(EmbedGrad a, Sorted s, int per_row, int chunks) {
   const int lane = threadIdx.x & 63;
   for (long long id = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);; id += (long long)gridDim.x * 4) {
@@ -415,6 +406,7 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(EmbedGrad a, Sorted s, 
     const int n = __popcll(__ballot(lane < PIECE && key >= 0 && key < a.vocab));
     const TO* g = static_cast<const TO*>(a.grad_out) + (long long)col * V;
     const bool mine = col < per_row;
+    const int here = elements<V, TAIL>(a.d, col);
     float sum[V];
     zero(sum);
     int last = __builtin_amdgcn_readlane(key, PIECE + 1);      // the token of the row before
@@ -425,7 +417,7 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(EmbedGrad a, Sorted s, 
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         x[u].clear();
-        if (i0 + u < n && mine) x[u].load(g + (long long)__builtin_amdgcn_readlane(row, i0 + u) * a.out_row);
+        if (i0 + u < n && mine) x[u].load(g + (long long)__builtin_amdgcn_readlane(row, i0 + u) * a.out_row, here);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -440,10 +432,10 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(EmbedGrad a, Sorted s, 
 #pragma unroll
         for (int j = 0; j < V; ++j) sum[j] += x[u][j];
         if (token == __builtin_amdgcn_readlane(key, i + 1)) {  // it goes on, in the block or behind it
-          if (i == PIECE - 1 && mine) store<float, V>(s.partial + ((size_t)block * 2 + (inside ? 1 : 0)) * a.d + (size_t)col * V, sum);
+          if (i == PIECE - 1 && mine) store<float, V>(s.partial + ((size_t)block * 2 + (inside ? 1 : 0)) * a.d + (size_t)col * V, sum, here);
         } else if (mine) {
-          if (inside) put_sum<TT, V>(a, token, col, sum);
-          else store<float, V>(s.partial + (size_t)block * 2 * a.d + (size_t)col * V, sum);
+          if (inside) put_sum<TT, V>(a, token, col, sum, here);
+          else store<float, V>(s.partial + (size_t)block * 2 * a.d + (size_t)col * V, sum, here);
         }
       }
     }
@@ -451,7 +443,7 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(EmbedGrad a, Sorted s, 
 }
 
 // A token that begins in the block and goes on behind it: four wavefronts a quarter of its partial sums each, then theirs in order.
-template <typename TT, int V>
+template <typename TT, int V, bool TAIL>
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGrad a, Sorted s, int per_row, int chunks) {
   __shared__ float part[4][64 * V];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -470,6 +462,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGrad a, Sorted s, 
     }
     const int n = (lo - 1) / PIECE - block + 1, from = (int)((long long)n * wave / 4), to = (int)((long long)n * (wave + 1) / 4);
     const bool mine = col < per_row;
+    const int here = elements<V, TAIL>(a.d, col);
     float sum[V];
     zero(sum);
     constexpr int U = 8;
@@ -478,7 +471,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGrad a, Sorted s, 
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         zero(x[u]);
-        if (i0 + u < to && mine) load<float, V>(x[u], s.partial + (((size_t)block + i0 + u) * 2 + (i0 + u == 0 ? 1 : 0)) * a.d + (size_t)col * V);
+        if (i0 + u < to && mine) load<float, V>(x[u], s.partial + (((size_t)block + i0 + u) * 2 + (i0 + u == 0 ? 1 : 0)) * a.d + (size_t)col * V, here);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -494,7 +487,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGrad a, Sorted s, 
     for (int w = 1; w < 4; ++w)
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[j] += part[w][j * 64 + lane];
-    put_sum<TT, V>(a, token, col, sum);
+    put_sum<TT, V>(a, token, col, sum, here);
   }
 }
 
@@ -556,12 +549,12 @@ hipError_t embed_grad(hipStream_t st, const EmbedGrad& a) {
   if (a.n_rows == 0) return e;
   const Sorted s{in.keys, in.rows, w.partial};
   constexpr int V = wide<TO, TT>();
-  const bool vec = a.d % V == 0 && rows_aligned(a.grad_out, a.out_row, sizeof(TO), V) && rows_aligned(a.grad_table, a.table_row, sizeof(TT), V);
-  const int per_row = vec ? a.d / V : a.d, chunks = blocks_of(per_row, 64), blocks = blocks_of(a.n_rows, PIECE);
+  const bool whole = a.d % V == 0;
+  const int per_row = blocks_of(a.d, V), chunks = blocks_of(per_row, 64), blocks = blocks_of(a.n_rows, PIECE);
   const long long groups = (long long)blocks * chunks;
   auto most = [](long long n) { return dim3((unsigned)std::min<long long>(n, 1 << 22)); };
-  run(vec ? embed_sums_kernel<TO, TT, V> : embed_sums_kernel<TO, TT, 1>, most((groups + 3) / 4), dim3(256), st, a, s, per_row, chunks);
-  if (a.n_rows > PIECE) run(vec ? embed_join_kernel<TT, V> : embed_join_kernel<TT, 1>, most(groups), dim3(256), st, a, s, per_row, chunks);
+  run(whole ? embed_sums_kernel<TO, TT, V, false> : embed_sums_kernel<TO, TT, V, true>, most((groups + 3) / 4), dim3(256), st, a, s, per_row, chunks);
+  if (a.n_rows > PIECE) run(whole ? embed_join_kernel<TT, V, false> : embed_join_kernel<TT, V, true>, most(groups), dim3(256), st, a, s, per_row, chunks);
   return e;
 }
 
@@ -569,7 +562,7 @@ hipError_t embed_grad(hipStream_t st, const EmbedGrad& a) {
 // Tokens' rows in their experts' batches.
 // ---------------------------------------------------------------------------
 // The tokens' rows, each read once and stored at its k places; workgroups behind those write zeros to the packed rows of no assignment, a wavefront 16 of them.
-template <typename T, int V>
+template <typename T, int V, bool TAIL>
 __global__ __launch_bounds__(ROWS_THREADS) void expert_gather_kernel(ExpertRows a, int per_row, int row_groups) {
   T* out = static_cast<T*>(a.out);
   if ((int)blockIdx.x >= row_groups) {
@@ -580,15 +573,16 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_gather_kernel(ExpertRows 
       float x[V];
       zero(x);
       for (unsigned long long none = __ballot(lane < 16 && p0 + lane < a.n_packed && (from < 0 || from >= n)); none != 0; none &= none - 1)
-        for (int col = lane; col < per_row; col += 64) store<T, V>(out + (p0 + __ffsll((long long)none) - 1) * a.packed_row + (long long)col * V, x);
+        for (int col = lane; col < per_row; col += 64) store<T, V>(out + (p0 + __ffsll((long long)none) - 1) * a.packed_row + (long long)col * V, x, elements<V, TAIL>(a.d, col));
     }
     return;
   }
   for (long long first = (long long)blockIdx.x * ROWS_THREADS; first < (long long)a.n_rows * per_row; first += (long long)row_groups * ROWS_THREADS) {
     const At at = vector_at(first, threadIdx.x, per_row);
     if (at.row >= a.n_rows) continue;
-    float x[V];
-    load<T, V>(x, static_cast<const T*>(a.rows) + at.row * a.row + (long long)at.col * V);
+    const int n = elements<V, TAIL>(a.d, at.col);
+    Raw<T, V> x;
+    x.load(static_cast<const T*>(a.rows) + at.row * a.row + (long long)at.col * V, n);
     const int* position = a.position + at.row * a.k;
     for (int j0 = 0; j0 < a.k; j0 += 8) {
       int to[8];
@@ -596,15 +590,16 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_gather_kernel(ExpertRows 
       for (int j = 0; j < 8; ++j) to[j] = j0 + j < a.k ? position[j0 + j] : -1;
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (to[j] >= 0 && to[j] < a.n_packed) store<T, V>(out + (long long)to[j] * a.packed_row + (long long)at.col * V, x);
+        if (to[j] >= 0 && to[j] < a.n_packed) x.store(out + (long long)to[j] * a.packed_row + (long long)at.col * V, n);
     }
   }
 }
 
 // Eight of a token's packed rows in flight, added in order.
-template <typename T, int V>
+template <typename T, int V, bool TAIL>
 __global__ __launch_bounds__(ROWS_THREADS) void expert_combine_kernel(ExpertRows a, int per_row) {
   FOR_VECTORS(a.n_rows, per_row) {
+    const int n = elements<V, TAIL>(a.d, at.col);
     float sum[V];
     zero(sum);
     const int* position = a.position + at.row * a.k;
@@ -621,7 +616,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_combine_kernel(ExpertRows
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (from[j] >= 0 && from[j] < a.n_packed) x[j].load(packed + (long long)from[j] * a.packed_row);
+        if (from[j] >= 0 && from[j] < a.n_packed) x[j].load(packed + (long long)from[j] * a.packed_row, n);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
         if (from[j] >= 0 && from[j] < a.n_packed) {
@@ -629,13 +624,13 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_combine_kernel(ExpertRows
           for (int i = 0; i < V; ++i) sum[i] = fmaf(w[j], x[j][i], sum[i]);
         }
     }
-    store<T, V>(static_cast<T*>(a.out) + at.row * a.row + (long long)at.col * V, sum);
+    store<T, V>(static_cast<T*>(a.out) + at.row * a.row + (long long)at.col * V, sum, n);
   }
 }
 
 // One wavefront a packed row: its gradient, and its weight's.  Workgroups behind those write the weights' of assignments that are nowhere.  Bound by HBM: 16384 tokens of
 // 2048 in bf16 with 8 experts each 206 us (5.2 TB/s).
-template <typename T, int V>
+template <typename T, int V, bool TAIL>
 __global__ __launch_bounds__(ROWS_THREADS) void expert_combine_grad_kernel(ExpertRows a, int per_row, int row_groups) {
   const int lane = threadIdx.x & 63;
   const long long n = (long long)a.n_rows * a.k;
@@ -650,29 +645,45 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_combine_grad_kernel(Exper
     const float w = there && a.weights ? a.weights[from] : 1.f;
     float dot = 0.f;
     for (int col = lane; col < per_row; col += 64) {
+      const int here = elements<V, TAIL>(a.d, col);
       float g[V], y[V];
       zero(g);
       if (there) {
-        load<T, V>(g, static_cast<const T*>(a.rows) + (long long)(from / a.k) * a.row + (long long)col * V);
+        load<T, V>(g, static_cast<const T*>(a.rows) + (long long)(from / a.k) * a.row + (long long)col * V, here);
         if (a.grad_weights) {
-          load<T, V>(y, static_cast<const T*>(a.packed) + p * a.packed_row + (long long)col * V);
+          load<T, V>(y, static_cast<const T*>(a.packed) + p * a.packed_row + (long long)col * V, here);
 #pragma unroll
           for (int i = 0; i < V; ++i) dot = fmaf(g[i], y[i], dot);
         }
       }
 #pragma unroll
       for (int i = 0; i < V; ++i) g[i] *= w;
-      if (a.grad_packed) store<T, V>(static_cast<T*>(a.grad_packed) + p * a.grad_row + (long long)col * V, g);
+      if (a.grad_packed) store<T, V>(static_cast<T*>(a.grad_packed) + p * a.grad_row + (long long)col * V, g, here);
     }
     dot = wave_sum_f32(dot);
     if (there && a.grad_weights && lane == 0) a.grad_weights[from] = dot;
   }
 }
 
-bool vectors(const ExpertRows& a, int v) {
-  const size_t e = a.f32 ? 4 : 2;
-  auto fine = [&](const void* p, long long row) { return p == nullptr || rows_aligned(p, row, e, v); };
-  return a.d % v == 0 && fine(a.rows, a.row) && fine(a.packed, a.packed_row) && fine(a.grad_packed, a.grad_row);
+template <typename T>
+hipError_t expert_gather(hipStream_t st, const ExpertRows& a) {
+  constexpr int V = wide<T>();
+  const int per_row = blocks_of(a.d, V), row_groups = a.n_rows > 0 ? (int)vector_grid(a.n_rows, per_row).x : 0;
+  const dim3 grid(row_groups + std::min(blocks_of(a.n_packed, 64), 1 << 20));
+  return enqueue(a.d % V == 0 ? expert_gather_kernel<T, V, false> : expert_gather_kernel<T, V, true>, grid, dim3(ROWS_THREADS), st, a, per_row, row_groups);
+}
+template <typename T>
+hipError_t expert_combine(hipStream_t st, const ExpertRows& a) {
+  constexpr int V = wide<T>();
+  const int per_row = blocks_of(a.d, V);
+  return enqueue(a.d % V == 0 ? expert_combine_kernel<T, V, false> : expert_combine_kernel<T, V, true>, vector_grid(a.n_rows, per_row), dim3(ROWS_THREADS), st, a, per_row);
+}
+template <typename T>
+hipError_t expert_combine_grad(hipStream_t st, const ExpertRows& a) {
+  constexpr int V = wide<T>();
+  const int row_groups = std::min(blocks_of(a.n_packed, 4), 1 << 22);
+  const dim3 grid(row_groups + (a.grad_weights ? std::min(blocks_of((long long)a.n_rows * a.k, ROWS_THREADS), 1 << 16) : 0));
+  return enqueue(a.d % V == 0 ? expert_combine_grad_kernel<T, V, false> : expert_combine_grad_kernel<T, V, true>, grid, dim3(ROWS_THREADS), st, a, blocks_of(a.d, V), row_groups);
 }
 
 }  // namespace
@@ -702,36 +713,8 @@ hipError_t launch_expert_sort(hipStream_t st, const ExpertSort& a) {
   return e == hipSuccess ? enqueue(expert_place_kernel, dim3(tiles), dim3(SORT_THREADS), st, in, tiles, (const int*)hist, a.align, a.n_packed, a.starts, a.source, a.position) : e;
 }
 
-hipError_t launch_expert_gather(hipStream_t st, const ExpertRows& a) {
-  constexpr int F = wide<float>(), B = wide<bf16_t>();
-  ExpertRows c = a;
-  c.packed = a.out;                                     // (for the alignment's test)
-  const bool vec = vectors(c, a.f32 ? F : B);
-  const int per_row = vec ? a.d / (a.f32 ? F : B) : a.d, row_groups = a.n_rows > 0 ? (int)vector_grid(a.n_rows, per_row).x : 0;
-  const dim3 grid(row_groups + std::min(blocks_of(a.n_packed, 64), 1 << 20)), block(ROWS_THREADS);
-  if (a.f32) return enqueue(vec ? expert_gather_kernel<float, F> : expert_gather_kernel<float, 1>, grid, block, st, a, per_row, row_groups);
-  return enqueue(vec ? expert_gather_kernel<bf16_t, B> : expert_gather_kernel<bf16_t, 1>, grid, block, st, a, per_row, row_groups);
-}
-
-hipError_t launch_expert_combine(hipStream_t st, const ExpertRows& a) {
-  constexpr int F = wide<float>(), B = wide<bf16_t>();
-  ExpertRows c = a;
-  c.rows = a.out;
-  const bool vec = vectors(c, a.f32 ? F : B);
-  const int per_row = vec ? a.d / (a.f32 ? F : B) : a.d;
-  const dim3 grid = vector_grid(a.n_rows, per_row), block(ROWS_THREADS);
-  if (a.f32) return enqueue(vec ? expert_combine_kernel<float, F> : expert_combine_kernel<float, 1>, grid, block, st, a, per_row);
-  return enqueue(vec ? expert_combine_kernel<bf16_t, B> : expert_combine_kernel<bf16_t, 1>, grid, block, st, a, per_row);
-}
-
-hipError_t launch_expert_combine_grad(hipStream_t st, const ExpertRows& a) {
-  constexpr int F = wide<float>(), B = wide<bf16_t>();
-  const bool vec = vectors(a, a.f32 ? F : B);
-  const int per_row = vec ? a.d / (a.f32 ? F : B) : a.d;
-  const int row_groups = std::min(blocks_of(a.n_packed, 4), 1 << 22);
-  const dim3 grid(row_groups + (a.grad_weights ? std::min(blocks_of((long long)a.n_rows * a.k, ROWS_THREADS), 1 << 16) : 0)), block(ROWS_THREADS);
-  if (a.f32) return enqueue(vec ? expert_combine_grad_kernel<float, F> : expert_combine_grad_kernel<float, 1>, grid, block, st, a, per_row, row_groups);
-  return enqueue(vec ? expert_combine_grad_kernel<bf16_t, B> : expert_combine_grad_kernel<bf16_t, 1>, grid, block, st, a, per_row, row_groups);
-}
+hipError_t launch_expert_gather(hipStream_t st, const ExpertRows& a) { return a.f32 ? expert_gather<float>(st, a) : expert_gather<bf16_t>(st, a); }
+hipError_t launch_expert_combine(hipStream_t st, const ExpertRows& a) { return a.f32 ? expert_combine<float>(st, a) : expert_combine<bf16_t>(st, a); }
+hipError_t launch_expert_combine_grad(hipStream_t st, const ExpertRows& a) { return a.f32 ? expert_combine_grad<float>(st, a) : expert_combine_grad<bf16_t>(st, a); }
 
 }  // namespace april
