@@ -456,9 +456,9 @@ typedef struct {
 } april_embed_args;
 int april_embed(const april_embed_args* args);
 
-/* grad_table[t] = scale * (sum of grad_out[r] over the rows of token t, in ascending order, in pieces of at most 128 rows where
- * they are more).  accumulate 0: every row is written (0 where no row has the token); 1: added to what is there, and rows of no
- * token are not touched.  Tokens outside 0..vocab - 1 are left out. */
+/* grad_table[t] = scale * (sum of grad_out[r] over the rows of token t, in ascending order; added up in pieces of at most 32 rows, whose
+ * borders depend on the other tokens).  accumulate 0: every row is written (0 where no row has the token); 1: added to what is there, and
+ * rows of no token are not touched.  Tokens outside 0..vocab - 1 are left out. */
 typedef struct {
   int32_t n_rows, vocab, d;
   int32_t out_dtype, table_dtype, index_bits;   /* of grad_out, of grad_table, of tokens       */

@@ -472,6 +472,119 @@ def test_experts_autograd():
     assert x.grad is not None
 
 
+# --- what is not read, and what is large --------------------------------------------------------------------------------------
+
+
+def test_padding_is_not_read():
+    """NaN in rows of padding, in weights of assignments that are left out, in packed rows of none."""
+    import torch
+    rng = np.random.default_rng(30)
+    n, vocab, d, k, e = 60, 1000, 40, 3, 8
+    tokens = rng.integers(0, vocab, size=n)
+    tokens[::3] = -1
+    off = torch.as_tensor(tokens < 0).cuda()
+    idx = index(tokens, 64)
+    logits = place(rng.standard_normal((n, vocab)), "f32")
+    want = ap().april_logprobs(logits, idx, entropy=True, top=4)
+    g = f32(rng.standard_normal(n))
+    want_grad = ap().april_logprobs_grad(logits, idx, want, grad_logprob=g, grad_entropy=g)
+    logits[off] = float("nan")
+    got = ap().april_logprobs(logits, idx, entropy=True, top=4)
+    g[off] = float("nan")
+    for a, b in zip(got, want):
+        assert a is b is None or torch.equal(a, b)
+    assert torch.equal(ap().april_logprobs_grad(logits, idx, got, grad_logprob=g, grad_entropy=g), want_grad) and not bool(want_grad[off].any())
+    grad = place(rng.standard_normal((n, d)), "bf16")
+    want = ap().april_embed_grad(grad, idx, vocab)
+    grad[off] = float("nan")
+    assert torch.equal(ap().april_embed_grad(grad, idx, vocab), want) and not bool(want.isnan().any())
+    ids = expert_ids(rng, n, k, e, True)
+    rows = ap().april_expert_sort(index(ids, 64), e, align=16)
+    w = f32(rng.random((n, k)))
+    y = place(rng.standard_normal((rows.source.shape[0], d)), "f32")
+    want = [ap().april_expert_combine(y, rows, w), *ap().april_expert_combine_grad(f32(np.ones((n, d))), y, rows, w)]
+    w[rows.position < 0] = float("nan")
+    y[rows.source < 0] = float("nan")
+    got = [ap().april_expert_combine(y, rows, w), *ap().april_expert_combine_grad(f32(np.ones((n, d))), y, rows, w)]
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+def test_logprobs_of_more_elements_than_31_bits_count():
+    import torch
+    n, vocab = 14200, 151936
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    logits = torch.empty((n, vocab), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    tokens = torch.randint(vocab, (n,), generator=gen, device="cuda")
+    got = ap().april_logprobs(logits, tokens, entropy=True, top=3)
+    g = torch.randn(n, generator=gen, device="cuda")
+    grad = ap().april_logprobs_grad(logits, tokens, got, grad_logprob=g, grad_entropy=g)
+    for r in (0, 14133, 14134, 14140, n - 1):                # (2^31 elements end in row 14134)
+        x, t = host(logits[r:r + 1]), host(tokens[r:r + 1])
+        lp, ent, _, best, ids = tr.logprobs(x, t, 1.0, 3)
+        near(host(got.logprob[r:r + 1]), lp, U * 300)
+        near(host(got.entropy[r:r + 1]), ent, U * 3000)
+        assert np.array_equal(host(got.top_ids[r:r + 1]), ids)
+        want, size = tr.logprobs_grad(x, t, 1.0, host(g[r:r + 1]), host(g[r:r + 1]))
+        near(host(grad[r:r + 1]), want, size * U * 1000 + half("bf16") * np.abs(want) + 2.0 ** -133)
+    ap().april_logprobs_grad(logits, tokens, got, grad_logprob=g, grad_entropy=g, out=logits)
+    assert torch.equal(logits, grad)
+
+
+def test_rows_of_more_elements_than_31_bits_count():
+    import torch
+    vocab, d, n = 270000, 8192, 40
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    table = torch.empty((vocab, d), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    tokens = torch.randint(vocab, (n,), generator=gen, device="cuda")
+    tokens[:4] = torch.tensor([0, vocab - 1, 262143, 262144])
+    out = ap().april_embed(table, tokens)
+    assert torch.equal(out, table[tokens])
+    grad = ap().april_embed_grad(out, tokens, vocab)
+    want, _, rows = tr.embed_grad(host(out), host(tokens), vocab)
+    there = np.nonzero(rows)[0]
+    near(host(grad[torch.as_tensor(there).cuda()]), want[there], half("bf16") * np.abs(want[there]))
+    assert int((grad != 0).any(1).sum()) == len(there)
+    del grad
+    # as packed rows: the token's row at its own place
+    rows = ap().ExpertRows(torch.zeros(2, dtype=torch.int32, device="cuda"), torch.full((vocab,), -1, dtype=torch.int32, device="cuda"), tokens.int()[:, None].contiguous())
+    rows.source[tokens] = torch.arange(n, dtype=torch.int32, device="cuda")
+    assert torch.equal(ap().april_expert_combine(table, rows), out)
+    packed = ap().april_expert_gather(out, rows)
+    assert torch.equal(packed[tokens], out) and int((packed != 0).any(1).sum()) == len(there)
+    g_packed, g_weights = ap().april_expert_combine_grad(out, table, rows)
+    assert torch.equal(g_packed, packed)
+    near(host(g_weights[:, 0]), (host(out) ** 2).sum(1), d * U * (host(out) ** 2).sum(1))
+
+
+def test_sorts_of_many_tiles():
+    """More tiles than a workgroup adds up by itself."""
+    import torch
+    n, k, e = 150001, 8, 300
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    ids = torch.randint(-3, e + 3, (n, k), generator=gen, device="cuda")
+    rows = ap().april_expert_sort(ids, e, align=8)
+    flat = ids.reshape(-1).cpu().numpy()
+    there = (flat >= 0) & (flat < e)
+    count = np.bincount(flat[there], minlength=e)
+    starts = np.concatenate(([0], np.cumsum((count + 7) // 8 * 8)))
+    assert np.array_equal(host(rows.starts), starts)
+    order = np.argsort(np.where(there, flat, e), kind="stable")[: there.sum()]
+    place_of = starts[flat[order]] + np.arange(len(order)) - np.concatenate(([0], np.cumsum(count)))[flat[order]]
+    source, position = np.full(rows.source.shape[0], -1), np.full(n * k, -1)
+    source[place_of], position[order] = order, place_of
+    assert np.array_equal(host(rows.source), source) and np.array_equal(host(rows.position).reshape(-1), position)
+    n, vocab, d = 1100003, 5003, 5
+    tokens = torch.randint(-20, vocab + 20, (n,), generator=gen, device="cuda")
+    tokens[torch.rand(n, generator=gen, device="cuda") < 0.4] = 77
+    g = torch.randint(-8, 9, (n, d), generator=gen, device="cuda").float()     # (sums of whole numbers are exact)
+    got = ap().april_embed_grad(g, tokens, vocab)
+    want = torch.zeros((vocab, d), dtype=torch.float64)
+    keep = (tokens >= 0) & (tokens < vocab)
+    want.index_add_(0, tokens[keep].cpu(), g[keep].double().cpu())
+    assert torch.equal(got.double().cpu(), want)
+
+
 # --- together ----------------------------------------------------------------------------------------------------------------
 
 
