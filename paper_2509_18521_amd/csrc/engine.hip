@@ -4,6 +4,7 @@
 // buffering continuations, prioritized resumption).
 #include <algorithm>
 #include <chrono>
+#include <climits>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -18,6 +19,7 @@
 #include "../../include/april.h"
 #include "cache.h"
 #include "kernels.h"
+#include "train.h"
 
 using namespace april;
 
@@ -207,6 +209,7 @@ struct april_ctx {
   float *router_out = nullptr, *moe_wts = nullptr, *moe_out = nullptr;
   int *moe_ids = nullptr, *moe_pos = nullptr, *moe_cnt = nullptr, *moe_base = nullptr, *moe_src = nullptr, *moe_group = nullptr;
   bf16_t* moe_act = nullptr;
+  char* moe_hist = nullptr;     // workspace of a prefill's dispatch
   int64_t expert_bytes = 0;    // bytes of one expert's three matrices
   // one decode iteration (scheduler + forward + sample) captured as a HIP graph, keyed by
   // the launch geometry (row bound, attention split bound)
@@ -770,9 +773,19 @@ void forward(april_ctx* c, RowCtx rows, RowCtx srows, const int* gather, double 
       const bool moe_tiled = tile && c->moe_tile;
       const int tall = moe_tiled ? 1 : c->moe_tall_rows;
       const int n_groups = moe_group_count(rows.max_rows, tk, E, moe_tile_rows());
-      launch_moe_dispatch(st, rows, c->moe_ids, E, tk, c->moe_cnt, c->moe_base, c->moe_pos, c->moe_src, c->moe_p_cap,
-                          rows.ctl == reinterpret_cast<const int2*>(c->d_ctrl) ? c->d_ctrl : nullptr, tall,
-                          c->moe_group);
+      // (a prefill's row count is the host's; one workgroup dispatches up to 4096 assignments, 111 k of them took it 120 us, the sort 15)
+      if (gather != nullptr && (long long)rows.max_rows * tk > 4096) {
+        ExpertSort s{};
+        s.n = rows.max_rows * tk; s.n_experts = E; s.align = moe_group_rows(rows.max_rows, tall); s.per_row = tk;
+        s.n_groups = moe_group_count(rows.max_rows, tk, E, s.align); s.n_packed = std::min(c->moe_p_cap, s.n_groups * s.align);
+        s.ids = c->moe_ids; s.starts = c->moe_base; s.source = c->moe_src; s.position = c->moe_pos; s.counts = c->moe_cnt; s.groups = c->moe_group;
+        s.ws = c->moe_hist;
+        launch_expert_sort(st, s);
+      } else {
+        launch_moe_dispatch(st, rows, c->moe_ids, E, tk, c->moe_cnt, c->moe_base, c->moe_pos, c->moe_src, c->moe_p_cap,
+                            rows.ctl == reinterpret_cast<const int2*>(c->d_ctrl) ? c->d_ctrl : nullptr, tall,
+                            c->moe_group);
+      }
       const double hit = std::min<double>(E, B * tk);   // bookkeeping estimate: experts that receive a token
       {
         ProfScope p(c, KC_MOE_GATEUP, hit * 2.0 * Fe * d * e + B * tk * (d + Fe) * e, 4.0 * B * tk * Fe * d);
@@ -1166,6 +1179,9 @@ int april_init(const april_model_cfg* cfg, const april_tensor* weights, int32_t 
     TRY(dev_alloc(c, &c->moe_ids, M * tk)); TRY(dev_alloc(c, &c->moe_wts, M * tk)); TRY(dev_alloc(c, &c->moe_pos, M * tk));
     TRY(dev_alloc(c, &c->moe_cnt, E)); TRY(dev_alloc(c, &c->moe_base, E + 1)); TRY(dev_alloc(c, &c->moe_src, c->moe_p_cap));
     TRY(dev_alloc(c, &c->moe_group, c->moe_p_cap / 64 + 1));
+    ExpertSort most{};
+    most.n = (int)std::min<size_t>(M * tk, INT_MAX - 4096);
+    TRY(dev_alloc(c, &c->moe_hist, std::max<size_t>(expert_sort_workspace(most), 16)));
     TRY(dev_alloc(c, &c->moe_act, (size_t)c->moe_p_cap * Fe));
     TRY(dev_alloc(c, &c->moe_out, (size_t)c->moe_p_cap * d));
     TRY(dev_alloc(c, &c->h_rows, M * d));

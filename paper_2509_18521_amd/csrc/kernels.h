@@ -259,6 +259,7 @@ void launch_moe_dispatch(hipStream_t st, RowCtx rc, const int* ids, int E, int t
                          int* pos_of, int* src_row, int p_cap, Ctrl* ctrl, int tall_rows, int* group_expert);
 // upper bound on the row groups (of `align` rows) of a launch over at most max_rows rows
 int moe_group_count(int max_rows, int top_k, int E, int align);
+int moe_group_rows(int max_rows, int tall_rows);      // rows of a GEMM workgroup, to a multiple of which the dispatch aligns the experts' segments
 // tall_rows: row bound from which a GEMM workgroup takes 4 m-tiles of an expert instead of 2
 // (the dispatch aligns the expert segments accordingly: pass the same value to all three)
 // LDS-tiled expert GEMMs for prefill passes (kernels_gemm_tile.hip): row groups of moe_tile_rows()

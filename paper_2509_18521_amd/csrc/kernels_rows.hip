@@ -227,7 +227,7 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_tile_kernel(SortIn in, int*
 }
 
 // Experts: one pass places them.  Expert e's rows begin at a multiple of `align`; what lies behind its last one and behind the last expert's is no row.
-__global__ __launch_bounds__(SORT_THREADS) void expert_place_kernel(SortIn in, int tiles, const int* hist, int align, int n_packed, int* starts, int* source, int* position) {
+__global__ __launch_bounds__(SORT_THREADS) void expert_place_kernel(SortIn in, int tiles, const int* hist, ExpertSort a) {
   __shared__ SortShared sh;
   __shared__ int end_of[BINS + 1], first_of[BINS + 1];
   const int tid = threadIdx.x, tile = blockIdx.x, n_experts = in.limit;
@@ -240,11 +240,14 @@ __global__ __launch_bounds__(SORT_THREADS) void expert_place_kernel(SortIn in, i
     all = tid < BINS ? t.total(sh) : 0;
     before = 0;
   }
-  const int room = tid < n_experts ? (all + align - 1) / align * align : 0, first = sum_before(room);
+  const int room = tid < n_experts ? (all + a.align - 1) / a.align * a.align : 0, first = sum_before(room);
   if (tid < BINS) {
     first_of[tid] = first;
     end_of[tid] = first + (tid < n_experts ? all : 0);
-    if (tid <= n_experts && tile == 0) starts[tid] = first;
+    if (tile == 0) {
+      if (tid <= n_experts) a.starts[tid] = first;
+      if (a.counts != nullptr && tid < n_experts) a.counts[tid] = all;
+    }
   }
   t.place_from(sh, 0, first + before);
 #pragma unroll
@@ -252,14 +255,24 @@ __global__ __launch_bounds__(SORT_THREADS) void expert_place_kernel(SortIn in, i
     if (t.key[s] >= 0) {
       const int i = (int)((long long)tile * SORT_TILE + t.place(s));
       const bool there = t.key[s] < n_experts;
-      position[i] = there ? t.rank[s] : -1;
-      if (there) source[t.rank[s]] = i;
+      a.position[i] = there ? t.rank[s] : -1;
+      if (there) a.source[t.rank[s]] = a.per_row == 1 ? i : i / a.per_row;
     }
+  // (n_experts is at most 511: entry n_experts begins where the last one's room ends)
   // a wavefront fills the room behind an expert's last row, all threads what lies behind the last expert's
   const int lane = tid & 63;
   for (int e = tile * SORT_WAVES + (tid >> 6); e < n_experts; e += gridDim.x * SORT_WAVES)
-    for (int p = end_of[e] + lane; p < first_of[e + 1]; p += 64) source[p] = -1;
-  for (long long p = end_of[n_experts] + (long long)tile * SORT_THREADS + tid; p < n_packed; p += (long long)gridDim.x * SORT_THREADS) source[p] = -1;
+    for (int p = end_of[e] + lane; p < first_of[e + 1]; p += 64) a.source[p] = -1;
+  for (long long p = end_of[n_experts] + (long long)tile * SORT_THREADS + tid; p < a.n_packed; p += (long long)gridDim.x * SORT_THREADS) a.source[p] = -1;
+  for (int g = tile * SORT_THREADS + tid; g < a.n_groups; g += gridDim.x * SORT_THREADS) {
+    int lo = 0, hi = n_experts;                              // the last expert that begins at the group's first row or before
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (first_of[mid] <= g * a.align) lo = mid;
+      else hi = mid - 1;
+    }
+    a.groups[g] = lo < n_experts ? lo : -1;
+  }
 }
 
 int blocks_of(long long n, int per) { return (int)((n + per - 1) / per); }
@@ -710,7 +723,7 @@ hipError_t launch_expert_sort(hipStream_t st, const ExpertSort& a) {
   hipError_t e = hipSuccess;
   if (tiles > 1) e = enqueue(sort_count_kernel, dim3(tiles), dim3(SORT_THREADS), st, in, 0, tiles, hist, Zeros{});
   if (tiles > ADD_TILES && e == hipSuccess) e = enqueue(sort_add_kernel, dim3(BINS / 64), dim3(64), st, hist, tiles);
-  return e == hipSuccess ? enqueue(expert_place_kernel, dim3(tiles), dim3(SORT_THREADS), st, in, tiles, (const int*)hist, a.align, a.n_packed, a.starts, a.source, a.position) : e;
+  return e == hipSuccess ? enqueue(expert_place_kernel, dim3(tiles), dim3(SORT_THREADS), st, in, tiles, (const int*)hist, a) : e;
 }
 
 hipError_t launch_expert_gather(hipStream_t st, const ExpertRows& a) { return a.f32 ? expert_gather<float>(st, a) : expert_gather<bf16_t>(st, a); }

@@ -69,6 +69,12 @@ struct ExpertSort {
   const void* ids;
   int *starts, *source, *position;
   void* ws;
+  // the engine's dispatch: source[p] is the assignment divided by `per_row`, an expert's assignments are counted, and groups[g] is the expert that owns packed rows
+  // [g * align, (g + 1) * align), -1 past the end
+  int per_row = 1;
+  int* counts = nullptr;
+  int* groups = nullptr;
+  int n_groups = 0;
 };
 size_t expert_sort_workspace(const ExpertSort& a);
 hipError_t launch_expert_sort(hipStream_t st, const ExpertSort& a);
