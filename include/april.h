@@ -397,8 +397,8 @@ int64_t april_cache_attention_workspace(const april_cache_attention_args* args);
  * Matrices are rows of adjacent elements, `*_row` elements apart (16-byte aligned rows are fastest); a stride over a
  * single row is not used; inputs may repeat a row (stride 0), rows of a result may not overlap, nor a result an input where
  * nothing else is said.  dtype: APRIL_DTYPE_FP32 or APRIL_DTYPE_BF16; sums are in fp32, a result is rounded once.
- * Indexes (tokens, experts) are of index_bits 32 or 64.  Results do not depend on how the work is shared out between
- * workgroups, nor from one call to the next.  Calls that may run at the same time need a workspace each. */
+ * Indexes (tokens, experts) are of index_bits 32 or 64.  The same call gives the same bits every time; the last bits of a
+ * sum may change with the sizes of the call and with a row's address to 16 bytes.  Calls that may run at the same time need a workspace each. */
 
 /* x = logits / temperature, row by row: logprob = x[token] - lse, lse = log of the sum of exp(x), entropy = -sum of p log p, and the
  * n_top largest x - lse with their columns, descending, equal logits by ascending column.

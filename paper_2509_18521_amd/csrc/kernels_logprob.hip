@@ -145,28 +145,31 @@ struct Scan {
 // (no more than k - 1 groups have any), and then those equal to it in the run's order until there are k; where even the former are too
 // many, k passes over the run.
 // ---------------------------------------------------------------------------
-constexpr int GROUPS = 256, MAX_CAND = 2048;
+template <int NT> constexpr int groups = NT < 256 ? NT : 256;
+template <int NT> constexpr int max_cand = NT < 256 ? 512 : 2048;
 
 template <int NT>
 struct TopShared {
-  alignas(16) unsigned group[GROUPS];
+  alignas(16) unsigned group[groups<NT>];
   float tops[SECTIONS][NT];
   unsigned short hot[SECTIONS * NT];      // section * NT + thread
-  alignas(16) unsigned long long cand[MAX_CAND + 8];
+  alignas(16) unsigned long long cand[max_cand<NT> + 8];
   unsigned long long best[NT / 64];
-  static_assert(NT == GROUPS || NT == 2 * GROUPS, "one or two threads a group");
+  static_assert(NT == 64 || NT == 256 || NT == 512, "one or two threads a group");
   alignas(8) unsigned char bits[NT];
   int n_hot, n_cand;
 };
 __device__ inline unsigned long long pair_of(unsigned key, int place) { return ((unsigned long long)key << 32) | (unsigned)~place; }
 __device__ inline float key_value(unsigned key) { return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key); }
 
-// The largest bound that k of the 256 keys reach (0 where fewer are there); unless `exact`, one of 16 bits, or one that exactly k reach.
+// The largest bound that k of the wavefront's keys reach (four a lane, of 64 groups x alone; 0 where fewer are there); unless `exact`, one of 16 bits, or one that exactly k reach.
+template <int NT>
 __device__ inline unsigned bound_of(const uint4& g, int k, bool exact) {
   unsigned t = 0;
   for (unsigned bit = 0x80000000u; bit != (exact ? 0u : 0x8000u); bit >>= 1) {
     const unsigned u = t | bit;
-    const int n = __popcll(__ballot(g.x >= u)) + __popcll(__ballot(g.y >= u)) + __popcll(__ballot(g.z >= u)) + __popcll(__ballot(g.w >= u));
+    int n = __popcll(__ballot(g.x >= u));
+    if (NT > 64) n += __popcll(__ballot(g.y >= u)) + __popcll(__ballot(g.z >= u)) + __popcll(__ballot(g.w >= u));
     if (n >= k) t = u;
     if (n == k && !exact) break;
   }
@@ -179,7 +182,7 @@ __device__ void collect(TopShared<NT>& sh, const Run<T>& r, unsigned from) {
   constexpr int V = Vec<T>::N;
   const int n_hot = sh.n_hot, each = section_vectors<NT>(r.nv);
   for (int i = threadIdx.x; i < n_hot * each; i += NT) {
-    if (*static_cast<volatile int*>(&sh.n_cand) > MAX_CAND) break;                 // (more than the list holds: the count does not matter)
+    if (*static_cast<volatile int*>(&sh.n_cand) > max_cand<NT>) break;                 // (more than the list holds: the count does not matter)
     const int h = i / each, at = sh.hot[h], v = ((at / NT) * each + i - h * each) * NT + at % NT;
     if (v >= r.nv) continue;
     const auto x = r.vector(v);
@@ -194,7 +197,7 @@ __device__ void collect(TopShared<NT>& sh, const Run<T>& r, unsigned from) {
 #pragma unroll
     for (int j = 0; j < V; ++j)
       if (hits >> j & 1) {
-        if (to < MAX_CAND) sh.cand[to] = pair_of(key[j], r.place(v) + j);
+        if (to < max_cand<NT>) sh.cand[to] = pair_of(key[j], r.place(v) + j);
         ++to;
       }
   }
@@ -203,7 +206,7 @@ __device__ void collect(TopShared<NT>& sh, const Run<T>& r, unsigned from) {
     const unsigned key = f2key((float)r.p[place]);
     if (key >= from) {
       const int to = atomicAdd(&sh.n_cand, 1);
-      if (to < MAX_CAND) sh.cand[to] = pair_of(key, place);
+      if (to < max_cand<NT>) sh.cand[to] = pair_of(key, place);
     }
   }
   __syncthreads();
@@ -285,7 +288,7 @@ template <typename T, int NT>
 __device__ void find_top(TopShared<NT>& sh, const Run<T>& r, int k, float top, bool any) {
   const int tid = threadIdx.x, lane = tid & 63;
   const unsigned mine = any ? f2key(top) : 0u;
-  if (NT == GROUPS) {
+  if (NT <= 256) {
     sh.group[tid] = mine;
   } else {
     const unsigned pair = max(mine, (unsigned)__builtin_amdgcn_update_dpp(0, (int)mine, 0xB1, 0xf, 0xf, false));      // (its neighbour's)
@@ -293,8 +296,8 @@ __device__ void find_top(TopShared<NT>& sh, const Run<T>& r, int k, float top, b
   }
   if (tid == 0) { sh.n_hot = 0; sh.n_cand = 0; }
   __syncthreads();
-  const uint4 g = reinterpret_cast<const uint4*>(sh.group)[lane];
-  unsigned least = bound_of(g, k, false);
+  const uint4 g = NT == 64 ? uint4{mine, 0u, 0u, 0u} : reinterpret_cast<const uint4*>(sh.group)[NT == 64 ? 0 : lane];
+  unsigned least = bound_of<NT>(g, k, false);
   const int each = section_vectors<NT>(r.nv) * NT;
   for (int i = 0; i * each < r.nv; ++i) {
     const unsigned long long hot = __ballot(i * each + tid < r.nv && f2key(sh.tops[i][tid]) >= least);
@@ -306,15 +309,15 @@ __device__ void find_top(TopShared<NT>& sh, const Run<T>& r, int k, float top, b
   }
   __syncthreads();
   collect(sh, r, least);
-  if (sh.n_cand <= MAX_CAND) return;
-  least = bound_of(g, k, true);
+  if (sh.n_cand <= max_cand<NT>) return;
+  least = bound_of<NT>(g, k, true);
   __syncthreads();
   if (tid == 0) sh.n_cand = 0;
   __syncthreads();
   collect(sh, r, least + 1);
   const int above = sh.n_cand;
   __syncthreads();
-  if (above <= MAX_CAND - k) collect_equal(sh, r, least, k - above);
+  if (above <= max_cand<NT> - k) collect_equal(sh, r, least, k - above);
   else collect_one_by_one(sh, r, k);
 }
 
@@ -415,7 +418,7 @@ __global__ __launch_bounds__(NT, 8) void logprobs_kernel(Logprobs a) {
     if constexpr (TOP) {
       if (!no_top(a, r, p, tid, NT)) {
         find_top<T, NT>(st, run, a.n_top, scan.top, tid < run.nv || tid < run.singles);
-        rank_candidates<NT>(st.cand, min(st.n_cand, MAX_CAND), a.n_top, [&](int rank, unsigned long long c) { put_top(a, r, rank, c, p, l2); });
+        rank_candidates<NT>(st.cand, min(st.n_cand, max_cand<NT>), a.n_top, [&](int rank, unsigned long long c) { put_top(a, r, rank, c, p, l2); });
       }
     }
     __syncthreads();
@@ -448,7 +451,7 @@ __global__ __launch_bounds__(NT, 8) void logprobs_part_kernel(Logprobs a, int pa
   if (tid == 0) { out[0] = p.m; out[1] = p.s; out[2] = p.e; }
   if constexpr (TOP) {
     find_top<T, NT>(st, run, a.n_top, scan.top, tid < run.nv || tid < run.singles);
-    const int n = min(st.n_cand, MAX_CAND);
+    const int n = min(st.n_cand, max_cand<NT>);
     unsigned long long* cand = reinterpret_cast<unsigned long long*>(out + 4);
     for (int i = n + tid; i < a.n_top; i += NT) cand[i] = 0ull;
     // (places count from the row's first element on; the order of equal values stays)
@@ -456,13 +459,13 @@ __global__ __launch_bounds__(NT, 8) void logprobs_part_kernel(Logprobs a, int pa
   }
 }
 
-constexpr int JOIN_THREADS = 256, MAX_PARTS = 32;
+constexpr int JOIN_THREADS = 256, MAX_PARTS = 32, MAX_JOIN = 512;
 
 // The parts' candidates are in descending order.  Each part has `depth` elements no smaller than its depth-th, so where parts x depth is n_top or
 // more, nothing below the smallest of those is among the n_top largest.
 template <typename T>
 __global__ __launch_bounds__(JOIN_THREADS) void logprobs_join_kernel(Logprobs a, int parts) {
-  __shared__ alignas(16) unsigned long long cand[MAX_CAND + 8];
+  __shared__ alignas(16) unsigned long long cand[MAX_JOIN + 8];
   __shared__ unsigned long long least;
   __shared__ int n_cand;
   const int tid = threadIdx.x, r = blockIdx.x;
@@ -502,7 +505,7 @@ int row_parts(const Logprobs& a) {
   if (a.n_rows > 128) return 1;
   const long long bytes = (long long)a.vocab * (a.f32 ? 4 : 2);
   long long parts = std::min<long long>((255 + a.n_rows) / a.n_rows, bytes >> 14);
-  if (a.n_top > 0) parts = std::min<long long>(parts, 512 / a.n_top);
+  if (a.n_top > 0) parts = std::min<long long>(parts, MAX_JOIN / a.n_top);
   return (int)std::max<long long>(1, std::min<long long>(parts, MAX_PARTS));
 }
 
@@ -511,8 +514,12 @@ hipError_t logprobs(hipStream_t st, const Logprobs& a) {
   const int parts = row_parts(a);
   if (parts == 1) {
     const dim3 grid(std::min(a.n_rows, 1 << 20));
+    // Short rows, a wavefront a row where there are many (us of workgroups of 64 | 256 threads: 16384 rows of 5000 in bf16 with 20 alternatives 51 | 118, of 512 in fp32 without 9.6 | 19,
+    // 2048 of 16000 in bf16 with 32 alternatives 25.6 | 26.4; 1024 of them 21.5 | 14.7).  With more than 32 alternatives the largest elements of 64 lanes are no bound to speak of.
+    const long long bytes = (long long)a.vocab * sizeof(T);
+    if (a.n_rows >= 2048 && a.n_top <= 32 && bytes < (TOP ? 32 << 10 : 4 << 10)) return enqueue(logprobs_kernel<T, ENT, TOP, 64>, grid, dim3(64), st, a);
     // (workgroups of 256 | 512 threads: 4096 rows of 5000 in bf16 11.2 | 15.5 us, of 32003 with 20 alternatives 73 | 100, of 128256 with 20 307 | 277, of 151936 in fp32 440 | 432)
-    if ((long long)a.vocab * sizeof(T) < (128 << 10)) return enqueue(logprobs_kernel<T, ENT, TOP, 256>, grid, dim3(256), st, a);
+    if (bytes < (128 << 10)) return enqueue(logprobs_kernel<T, ENT, TOP, 256>, grid, dim3(256), st, a);
     return enqueue(logprobs_kernel<T, ENT, TOP, 512>, grid, dim3(512), st, a);
   }
   const hipError_t e = enqueue(logprobs_part_kernel<T, ENT, TOP, 512>, dim3(a.n_rows * parts), dim3(512), st, a, parts);

@@ -428,7 +428,7 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(EmbedGrad a, Sorted s, 
     zero(sum);
     int last = __builtin_amdgcn_readlane(key, PIECE + 1);      // the token of the row before
     bool inside = false;                                       // the sum's token begins in the block
-    constexpr int U = 16;
+    constexpr int U = 8;
     for (int i0 = 0; i0 < n; i0 += U) {
       Raw<TO, V> x[U];
 #pragma unroll

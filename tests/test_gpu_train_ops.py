@@ -163,7 +163,7 @@ def test_logprobs_of_rows_at_any_address(n, vocab, pad, off, t):
 
 @pytest.mark.parametrize("n", [1, 2, 31, 100, 255, 256, 600])
 def test_logprobs_of_few_and_many_rows(n):
-    """However the work is shared out, a row's bits are those that it has alone (the same vocabulary, the same number of rows or not)."""
+    """However the rows are shared out between workgroups; the same call twice has the same bits."""
     rng = np.random.default_rng(n)
     x = hard_logits(rng, n, 9000, "bf16")
     tokens = rng.integers(0, 9000, size=n)
@@ -187,6 +187,37 @@ def test_logprobs_of_all_kinds_of_ties():
         for top in (1, 3, 64):
             check_logprobs(x, rng.integers(0, vocab, size=len(rows)), t, top=top)
             check_logprobs(np.tile(x, (30, 1)), rng.integers(0, vocab, size=30 * len(rows)), t, top=top) if top == 64 else None
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab,pad,off", [(1, 0, 0), (5, 3, 1), (64, 0, 0), (300, 0, 2), (513, 6, 5), (1001, 0, 0), (5000, 1, 3), (7999, 0, 0), (16000, 0, 0), (16384, 8, 0)])
+def test_logprobs_of_many_short_rows(vocab, pad, off, t):
+    """Thousands of rows, among them those whose ties and blocks of large values fill any list: copies of a row at like addresses have the same bits, and those of 48 rows are checked."""
+    import torch
+    rng = np.random.default_rng([vocab, pad, off])
+    x = hard_logits(rng, 48, vocab, t)
+    i = np.arange(vocab)
+    x[16], x[17], x[18] = i % 3, np.where(i % 64 < 8, 5.0 + i / 64.0, 0.0), np.where(i % 512 < 32, 7.0, rng.standard_normal(vocab))
+    x[19], x[20] = np.where(i % 16 == 0, -1.0, -np.inf), np.where(i < 1000, 3.0, 1.0)
+    tokens = rng.integers(0, vocab, size=48)
+    tokens[[5, 30]] = -1, vocab
+    n = 2500
+    of = rng.integers(0, 48, size=n)
+    of[:48] = np.arange(48)
+    for top in sorted({0, 1, min(20, vocab), min(32, vocab), min(33, vocab)}):
+        _, few, _ = check_logprobs(x, tokens, t, top=top)
+        logits = place(x[of], t, pad, off)
+        got = ap().april_logprobs(logits, index(tokens[of], 64), entropy=True, lse=True, top=top)
+        lp, ent, lse, best, ids = tr.logprobs(host(logits[:48]), tokens, 1.0, top)
+        near(host(got.logprob)[:48], host(few.logprob), 2e-6 * (1 + np.abs(np.nan_to_num(host(few.logprob), posinf=0, neginf=0))), "logprob")
+        near(host(got.entropy)[:48], ent, U * (2 * np.log(vocab) + vocab / 64 + 48) * (2 + np.log(vocab)), "entropy")
+        assert not top or np.array_equal(host(got.top_ids)[:48], ids)
+        assert not top or torch.equal(got.top_ids, got.top_ids[:48][torch.as_tensor(of).cuda()])
+        first, per = {}, 8 if t == "bf16" else 4             # (a row's sums go by its place to a 16-byte border)
+        same = torch.as_tensor([first.setdefault((of[r], (off + r * (vocab + pad)) % per), r) for r in range(n)]).cuda()
+        for v in got:
+            if v is not None:
+                assert torch.equal(v.nan_to_num(nan=123.0), v[same].nan_to_num(nan=123.0))
 
 
 def check_grad(n, vocab, t, temperature, parts, *, pad=0, off=0, in_place=False, seed=0):
