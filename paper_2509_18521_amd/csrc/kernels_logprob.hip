@@ -50,7 +50,9 @@ struct Run {
     singles = n - nv * V;
   }
   __device__ int single(int e) const { return e < head ? e : e + nv * V; }      // its place in the run
-  __device__ typename Vec<T>::type vector(int v) const { return *reinterpret_cast<const typename Vec<T>::type*>(p + head + (size_t)v * V); }
+  __device__ const typename Vec<T>::type* at(int v) const { return reinterpret_cast<const typename Vec<T>::type*>(p + head + (size_t)v * V); }
+  template <bool STREAM = false>
+  __device__ typename Vec<T>::type vector(int v) const { return STREAM ? __builtin_nontemporal_load(at(v)) : *at(v); }
   __device__ int place(int v) const { return head + v * V; }                    // of a vector's first element
 };
 
@@ -69,7 +71,7 @@ __device__ inline int section_vectors(int nv) {
   return each <= 4 ? 4 : (each + 7) / 8 * 8;
 }
 
-template <typename T, bool ENT, int NT>
+template <typename T, bool ENT, int NT, bool STREAM>
 struct Scan {
   static constexpr int V = Vec<T>::N, U = 32 / V;      // vectors of a thread in flight
   Part p;
@@ -101,11 +103,11 @@ struct Scan {
     for (; v + (U - 1) * NT < end; v += U * NT) {
       vec x[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) x[u] = r.vector(v + u * NT);
+      for (int u = 0; u < U; ++u) x[u] = r.template vector<STREAM>(v + u * NT);
       feed(x);
     }
     for (; v < end; v += NT) {
-      const vec x[1] = {r.vector(v)};
+      const vec x[1] = {r.template vector<STREAM>(v)};
       feed(x);
     }
   }
@@ -394,9 +396,10 @@ __device__ inline bool no_top(const Logprobs& a, int r, const Part& p, int tid, 
   return true;
 }
 
-// One workgroup a row, one pass over it.  Bound by HBM: 8192 rows of 128256 in bf16 395 us (5.3 TB/s), 192 of 151936 in fp32 22 (5.2).
-template <typename T, bool ENT, bool TOP, int NT>
-__global__ __launch_bounds__(NT, 8) void logprobs_kernel(Logprobs a) {
+// One workgroup a row, one pass over it.  Bound by HBM: 12288 rows of 151936 in bf16 544 us (6.9 TB/s), 192 in fp32 27
+// (4.3; 22 where they lie in the last cache).
+template <typename T, bool ENT, bool TOP, int NT, bool STREAM>
+__global__ __launch_bounds__(NT, 5) void logprobs_kernel(Logprobs a) {
   __shared__ RowShared<NT> sh;
   __shared__ std::conditional_t<TOP, TopShared<NT>, int> st;
   const int tid = threadIdx.x;
@@ -408,7 +411,7 @@ __global__ __launch_bounds__(NT, 8) void logprobs_kernel(Logprobs a) {
       continue;
     }
     const Run<T> run(row, a.vocab);
-    Scan<T, ENT, NT> scan;
+    Scan<T, ENT, NT, STREAM> scan;
     scan.c2 = a.c2;
     if constexpr (TOP) scan.run(run, tid, st);
     else scan.run(run, tid);
@@ -442,7 +445,7 @@ __global__ __launch_bounds__(NT, 8) void logprobs_part_kernel(Logprobs a, int pa
   const int v0 = (int)((long long)whole.nv * part / parts), v1 = (int)((long long)whole.nv * (part + 1) / parts);
   const int from = part == 0 ? 0 : whole.place(v0), to = part == parts - 1 ? a.vocab : whole.place(v1);
   const Run<T> run(row + from, to - from);
-  Scan<T, ENT, NT> scan;
+  Scan<T, ENT, NT, false> scan;
   scan.c2 = a.c2;
   if constexpr (TOP) scan.run(run, tid, st);
   else scan.run(run, tid);
@@ -514,13 +517,16 @@ hipError_t logprobs(hipStream_t st, const Logprobs& a) {
   const int parts = row_parts(a);
   if (parts == 1) {
     const dim3 grid(std::min(a.n_rows, 1 << 20));
+    // (streaming loads: 8192 rows of 128256 in bf16 348 -> 325 us; what the last cache holds may lie there already, and still when the gradient reads it again)
+    const bool stream = streams((long long)a.n_rows * a.vocab * (long long)sizeof(T) / 2);
+    auto rows = [&](auto kernel, auto streaming, int nt) { return enqueue(stream ? streaming : kernel, grid, dim3(nt), st, a); };
     // Short rows, a wavefront a row where there are many (us of workgroups of 64 | 256 threads: 16384 rows of 5000 in bf16 with 20 alternatives 51 | 118, of 512 in fp32 without 9.6 | 19,
     // 2048 of 16000 in bf16 with 32 alternatives 25.6 | 26.4; 1024 of them 21.5 | 14.7).  With more than 32 alternatives the largest elements of 64 lanes are no bound to speak of.
     const long long bytes = (long long)a.vocab * sizeof(T);
-    if (a.n_rows >= 2048 && a.n_top <= 32 && bytes < (TOP ? 32 << 10 : 4 << 10)) return enqueue(logprobs_kernel<T, ENT, TOP, 64>, grid, dim3(64), st, a);
+    if (a.n_rows >= 2048 && a.n_top <= 32 && bytes < (TOP ? 32 << 10 : 4 << 10)) return rows(logprobs_kernel<T, ENT, TOP, 64, false>, logprobs_kernel<T, ENT, TOP, 64, true>, 64);
     // (workgroups of 256 | 512 threads: 4096 rows of 5000 in bf16 11.2 | 15.5 us, of 32003 with 20 alternatives 73 | 100, of 128256 with 20 307 | 277, of 151936 in fp32 440 | 432)
-    if (bytes < (128 << 10)) return enqueue(logprobs_kernel<T, ENT, TOP, 256>, grid, dim3(256), st, a);
-    return enqueue(logprobs_kernel<T, ENT, TOP, 512>, grid, dim3(512), st, a);
+    if (bytes < (128 << 10)) return rows(logprobs_kernel<T, ENT, TOP, 256, false>, logprobs_kernel<T, ENT, TOP, 256, true>, 256);
+    return rows(logprobs_kernel<T, ENT, TOP, 512, false>, logprobs_kernel<T, ENT, TOP, 512, true>, 512);
   }
   const hipError_t e = enqueue(logprobs_part_kernel<T, ENT, TOP, 512>, dim3(a.n_rows * parts), dim3(512), st, a, parts);
   return e == hipSuccess ? enqueue(logprobs_join_kernel<T>, dim3(a.n_rows), dim3(JOIN_THREADS), st, a, parts) : e;
@@ -528,7 +534,7 @@ hipError_t logprobs(hipStream_t st, const Logprobs& a) {
 
 // ---------------------------------------------------------------------------
 // Gradient: one pass, every element by itself.  A workgroup takes four vectors a thread of one row.  Bound by HBM: 16384 rows of 151936 in bf16, a quarter of
-// them padding (not read), 1646 us (5.3 TB/s).
+// them padding (not read), 1520 us (5.7 TB/s).
 // ---------------------------------------------------------------------------
 constexpr int GRAD_THREADS = 256, GRAD_VECS = 4;
 
@@ -542,7 +548,7 @@ struct GradRow {
   }
 };
 
-template <typename T, bool ENT>
+template <typename T, bool ENT, bool STREAM>
 __global__ __launch_bounds__(GRAD_THREADS) void logprobs_grad_kernel(LogprobsGrad a, int chunks) {
   typedef typename Vec<T>::type vec;
   typedef vec at_element __attribute__((aligned(sizeof(T))));     // (grad's rows may lie to a 16-byte border otherwise than the logits')
@@ -569,7 +575,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void logprobs_grad_kernel(LogprobsGra
     if (!pad) {
 #pragma unroll
       for (int u = 0; u < GRAD_VECS; ++u)
-        if (v0 + u * GRAD_THREADS < run.nv) x[u] = run.vector(v0 + u * GRAD_THREADS);
+        if (v0 + u * GRAD_THREADS < run.nv) x[u] = run.template vector<STREAM>(v0 + u * GRAD_THREADS);
     }
 #pragma unroll
     for (int u = 0; u < GRAD_VECS; ++u) {
@@ -586,7 +592,9 @@ __global__ __launch_bounds__(GRAD_THREADS) void logprobs_grad_kernel(LogprobsGra
             if (i == at) y[i] = (T)(f((float)x[u][i]) + f.add);
         }
       }
-      *reinterpret_cast<at_element*>(to + (size_t)v * V) = y;
+      at_element* place = reinterpret_cast<at_element*>(to + (size_t)v * V);
+      if (STREAM) __builtin_nontemporal_store(y, place);
+      else *place = y;
     }
     if (chunk == 0 && (int)threadIdx.x < run.singles) single(run.single(threadIdx.x));
   }
@@ -596,7 +604,10 @@ template <typename T, bool ENT>
 hipError_t logprobs_grad(hipStream_t st, const LogprobsGrad& a) {
   const int per = GRAD_THREADS * GRAD_VECS * Vec<T>::N, chunks = std::max(1, (a.vocab - 1) / per + 1);
   const dim3 grid((unsigned)std::min<long long>((long long)a.n_rows * chunks, 1 << 22));
-  return enqueue(logprobs_grad_kernel<T, ENT>, grid, dim3(GRAD_THREADS), st, a, chunks);
+  // (streaming accesses: 16384 rows of 151936 in bf16, a quarter of them padding, 1570 -> 1520 us, and 740 -> 650 for the
+  // forward pass behind it)
+  const bool stream = streams((long long)a.n_rows * a.vocab * (long long)sizeof(T));
+  return enqueue(stream ? logprobs_grad_kernel<T, ENT, true> : logprobs_grad_kernel<T, ENT, false>, grid, dim3(GRAD_THREADS), st, a, chunks);
 }
 
 }  // namespace

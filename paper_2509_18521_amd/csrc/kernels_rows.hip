@@ -35,6 +35,7 @@ struct SortIn {
 // adjacent rows 64 KB.
 struct Zeros {
   char* p;
+  bool streaming;
   long long unit, stride, total, first, end;      // bytes of a unit, from one to the next, of all (-1: every unit is whole); units
 };
 __device__ inline void write_zeros(const Zeros& z, int group, int groups) {
@@ -45,7 +46,12 @@ __device__ inline void write_zeros(const Zeros& z, int group, int groups) {
     const int head = (int)min(n, (long long)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15));
     const long long body = (n - head) / 16 * 16;
     for (int i = 2 * tid; i < head; i += 2 * nt) *reinterpret_cast<short*>(p + i) = 0;
-    for (long long i = 16 * tid; i < body; i += 16 * nt) *reinterpret_cast<int4*>(p + head + i) = int4{0, 0, 0, 0};
+    typedef int vec __attribute__((ext_vector_type(4)));
+    vec* at = reinterpret_cast<vec*>(p + head);
+    if (z.streaming)
+      for (long long i = tid; i < body / 16; i += nt) __builtin_nontemporal_store(vec{0, 0, 0, 0}, at + i);
+    else
+      for (long long i = tid; i < body / 16; i += nt) at[i] = vec{0, 0, 0, 0};
     for (long long i = head + body + 2 * tid; i < n; i += 2 * nt) *reinterpret_cast<short*>(p + i) = 0;
   }
 }
@@ -291,10 +297,14 @@ struct Raw {
 #pragma unroll
     for (int i = 0; i < PARTS; ++i) v[i] = vec{};
   }
+  template <bool STREAM = false>
   __device__ __forceinline__ void load(const T* p, int n = V) {
     if (n == V) {
 #pragma unroll
-      for (int i = 0; i < PARTS; ++i) v[i] = *reinterpret_cast<const at_element*>(p + i * N);
+      for (int i = 0; i < PARTS; ++i) {
+        const at_element* q = reinterpret_cast<const at_element*>(p + i * N);
+        v[i] = STREAM ? __builtin_nontemporal_load(q) : *q;
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < V; ++i) v[i / N][i % N] = i < n ? p[i] : (T)0.f;
@@ -316,10 +326,10 @@ struct Raw {
   }
   __device__ __forceinline__ float operator[](int i) const { return (float)v[i / N][i % N]; }
 };
-template <typename T, int V>
+template <typename T, int V, bool STREAM = false>
 __device__ inline void load(float (&x)[V], const T* p, int n) {
   Raw<T, V> r;
-  r.load(p, n);
+  r.template load<STREAM>(p, n);
 #pragma unroll
   for (int i = 0; i < V; ++i) x[i] = r[i];
 }
@@ -364,7 +374,7 @@ dim3 vector_grid(long long rows, int per_row) {
 // ---------------------------------------------------------------------------
 // Embedding: rows of the table, scaled.
 // ---------------------------------------------------------------------------
-template <typename TT, typename TO, int V, bool TAIL>
+template <typename TT, typename TO, int V, bool TAIL, bool STREAM>
 __global__ __launch_bounds__(ROWS_THREADS) void embed_kernel(Embed a, int per_row) {
   FOR_VECTORS(a.n_rows, per_row) {
     const long long tok = index_at(a.tokens, a.i64, at.row);
@@ -375,7 +385,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void embed_kernel(Embed a, int per_ro
 #pragma unroll
     for (int i = 0; i < V; ++i) x[i] = tok < a.vocab ? x[i] * a.scale : NAN;
     if (tok < 0) zero(x);
-    store<TO, V>(static_cast<TO*>(a.out) + at.row * a.out_row + (long long)at.col * V, x, n);
+    store<TO, V, STREAM>(static_cast<TO*>(a.out) + at.row * a.out_row + (long long)at.col * V, x, n);
   }
 }
 
@@ -383,7 +393,10 @@ template <typename TT, typename TO>
 hipError_t embed(hipStream_t st, const Embed& a) {
   constexpr int V = wide<TT, TO>();
   const int per_row = blocks_of(a.d, V);
-  return enqueue(a.d % V == 0 ? embed_kernel<TT, TO, V, false> : embed_kernel<TT, TO, V, true>, vector_grid(a.n_rows, per_row), dim3(ROWS_THREADS), st, a, per_row);
+  // (streaming stores here and of the gradient's zeros: 32768 rows of 2560 and a table of 151936, lookup and gradient 277 -> 264 us; either alone nothing; in the sums too 257)
+  const bool stream = streams((long long)a.n_rows * a.d * (long long)sizeof(TO)), whole = a.d % V == 0;
+  const auto kernel = stream ? (whole ? embed_kernel<TT, TO, V, false, true> : embed_kernel<TT, TO, V, true, true>) : (whole ? embed_kernel<TT, TO, V, false, false> : embed_kernel<TT, TO, V, true, false>);
+  return enqueue(kernel, vector_grid(a.n_rows, per_row), dim3(ROWS_THREADS), st, a, per_row);
 }
 
 // ---------------------------------------------------------------------------
@@ -399,7 +412,7 @@ struct Sorted {
   float* partial;                      // [blocks][2][d]: of the token that goes on from the block before; of the one that begins and goes on behind
 };
 
-template <typename TT, int V>
+template <typename TT, int V, bool STREAM = false>
 __device__ inline void put_sum(const EmbedGrad& a, int token, int col, const float (&sum)[V], int n) {
   TT* to = static_cast<TT*>(a.grad_table) + (long long)token * a.table_row + (long long)col * V;
   float x[V];
@@ -407,10 +420,10 @@ __device__ inline void put_sum(const EmbedGrad& a, int token, int col, const flo
   if (a.accumulate) load<TT, V>(x, to, n);
 #pragma unroll
   for (int j = 0; j < V; ++j) x[j] += a.scale * sum[j];
-  store<TT, V>(to, x, n);
+  store<TT, V, STREAM>(to, x, n);
 }
 
-template <typename TO, typename TT, int V, bool TAIL>
+template <typename TO, typename TT, int V, bool TAIL, bool STREAM>
 __global__ __launch_bounds__(256) void embed_sums_kernel(EmbedGrad a, Sorted s, int per_row, int chunks) {
   const int lane = threadIdx.x & 63;
   for (long long id = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);; id += (long long)gridDim.x * 4) {
@@ -434,7 +447,7 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(EmbedGrad a, Sorted s, 
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         x[u].clear();
-        if (i0 + u < n && mine) x[u].load(g + (long long)__builtin_amdgcn_readlane(row, i0 + u) * a.out_row, here);
+        if (i0 + u < n && mine) x[u].template load<STREAM>(g + (long long)__builtin_amdgcn_readlane(row, i0 + u) * a.out_row, here);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -451,7 +464,7 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(EmbedGrad a, Sorted s, 
         if (token == __builtin_amdgcn_readlane(key, i + 1)) {  // it goes on, in the block or behind it
           if (i == PIECE - 1 && mine) store<float, V>(s.partial + ((size_t)block * 2 + (inside ? 1 : 0)) * a.d + (size_t)col * V, sum, here);
         } else if (mine) {
-          if (inside) put_sum<TT, V>(a, token, col, sum, here);
+          if (inside) put_sum<TT, V, STREAM>(a, token, col, sum, here);
           else store<float, V>(s.partial + (size_t)block * 2 * a.d + (size_t)col * V, sum, here);
         }
       }
@@ -533,7 +546,7 @@ hipError_t embed_grad(hipStream_t st, const EmbedGrad& a) {
   const int launches = tiles > 1 ? 2 * passes : 1;
   // the table's zeros, in as many shares as there are launches
   const long long row = (long long)a.d * sizeof(TT), stride = a.table_row * (long long)sizeof(TT);
-  Zeros z{static_cast<char*>(a.grad_table), row, stride, -1, 0, 0};
+  Zeros z{static_cast<char*>(a.grad_table), streams(row * a.vocab), row, stride, -1, 0, 0};
   long long units = a.vocab;
   if (a.table_row == a.d || a.vocab == 1) {
     z.unit = z.stride = 64 << 10;
@@ -569,7 +582,9 @@ hipError_t embed_grad(hipStream_t st, const EmbedGrad& a) {
   const int per_row = blocks_of(a.d, V), chunks = blocks_of(per_row, 64), blocks = blocks_of(a.n_rows, PIECE);
   const long long groups = (long long)blocks * chunks;
   auto most = [](long long n) { return dim3((unsigned)std::min<long long>(n, 1 << 22)); };
-  run(whole ? embed_sums_kernel<TO, TT, V, false> : embed_sums_kernel<TO, TT, V, true>, most((groups + 3) / 4), dim3(256), st, a, s, per_row, chunks);
+  const auto sums = streams((long long)a.n_rows * a.d * (long long)sizeof(TO)) ? (whole ? embed_sums_kernel<TO, TT, V, false, true> : embed_sums_kernel<TO, TT, V, true, true>)
+                                                                              : (whole ? embed_sums_kernel<TO, TT, V, false, false> : embed_sums_kernel<TO, TT, V, true, false>);
+  run(sums, most((groups + 3) / 4), dim3(256), st, a, s, per_row, chunks);
   if (a.n_rows > PIECE) run(whole ? embed_join_kernel<TT, V, false> : embed_join_kernel<TT, V, true>, most(groups), dim3(256), st, a, s, per_row, chunks);
   return e;
 }
@@ -578,7 +593,7 @@ hipError_t embed_grad(hipStream_t st, const EmbedGrad& a) {
 // Tokens' rows in their experts' batches.
 // ---------------------------------------------------------------------------
 // The tokens' rows, each read once and stored at its k places; workgroups behind those write zeros to the packed rows of no assignment, a wavefront 16 of them.
-template <typename T, int V, bool TAIL>
+template <typename T, int V, bool TAIL, bool STREAM>
 __global__ __launch_bounds__(ROWS_THREADS) void expert_gather_kernel(ExpertRows a, int per_row, int row_groups) {
   T* out = static_cast<T*>(a.out);
   if ((int)blockIdx.x >= row_groups) {
@@ -589,7 +604,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_gather_kernel(ExpertRows 
       float x[V];
       zero(x);
       for (unsigned long long none = __ballot(lane < 16 && p0 + lane < a.n_packed && (from < 0 || from >= n)); none != 0; none &= none - 1)
-        for (int col = lane; col < per_row; col += 64) store<T, V>(out + (p0 + __ffsll((long long)none) - 1) * a.packed_row + (long long)col * V, x, elements<V, TAIL>(a.d, col));
+        for (int col = lane; col < per_row; col += 64) store<T, V, STREAM>(out + (p0 + __ffsll((long long)none) - 1) * a.packed_row + (long long)col * V, x, elements<V, TAIL>(a.d, col));
     }
     return;
   }
@@ -606,13 +621,13 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_gather_kernel(ExpertRows 
       for (int j = 0; j < 8; ++j) to[j] = j0 + j < a.k ? position[j0 + j] : -1;
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (to[j] >= 0 && to[j] < a.n_packed) x.store(out + (long long)to[j] * a.packed_row + (long long)at.col * V, n);
+        if (to[j] >= 0 && to[j] < a.n_packed) x.template store<STREAM>(out + (long long)to[j] * a.packed_row + (long long)at.col * V, n);
     }
   }
 }
 
 // Eight of a token's packed rows in flight, added in order.
-template <typename T, int V, bool TAIL>
+template <typename T, int V, bool TAIL, bool STREAM>
 __global__ __launch_bounds__(ROWS_THREADS) void expert_combine_kernel(ExpertRows a, int per_row) {
   FOR_VECTORS(a.n_rows, per_row) {
     const int n = elements<V, TAIL>(a.d, at.col);
@@ -632,7 +647,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_combine_kernel(ExpertRows
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (from[j] >= 0 && from[j] < a.n_packed) x[j].load(packed + (long long)from[j] * a.packed_row, n);
+        if (from[j] >= 0 && from[j] < a.n_packed) x[j].template load<STREAM>(packed + (long long)from[j] * a.packed_row, n);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
         if (from[j] >= 0 && from[j] < a.n_packed) {
@@ -640,7 +655,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_combine_kernel(ExpertRows
           for (int i = 0; i < V; ++i) sum[i] = fmaf(w[j], x[j][i], sum[i]);
         }
     }
-    store<T, V>(static_cast<T*>(a.out) + at.row * a.row + (long long)at.col * V, sum, n);
+    store<T, V, STREAM>(static_cast<T*>(a.out) + at.row * a.row + (long long)at.col * V, sum, n);
   }
 }
 
@@ -667,7 +682,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_combine_grad_kernel(Exper
       if (there) {
         load<T, V>(g, static_cast<const T*>(a.rows) + (long long)(from / a.k) * a.row + (long long)col * V, here);
         if (a.grad_weights) {
-          load<T, V>(y, static_cast<const T*>(a.packed) + p * a.packed_row + (long long)col * V, here);
+          load<T, V, STREAM>(y, static_cast<const T*>(a.packed) + p * a.packed_row + (long long)col * V, here);
 #pragma unroll
           for (int i = 0; i < V; ++i) dot = fmaf(g[i], y[i], dot);
         }
@@ -681,30 +696,32 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_combine_grad_kernel(Exper
   }
 }
 
+// The packed rows are streamed, read or written, where they are many (13900 tokens of 2048 in bf16 with 8 experts each, gathered and summed, 249 -> 204 us, 16384 with all gradients
+// 583 -> 525; only the gradients' 562, only the stores 548).
+template <typename T>
+bool streamed(const ExpertRows& a) { return streams((long long)a.n_packed * a.d * (long long)sizeof(T)); }
+#define EXPERT_KERNEL(name, T, V) \
+  (streamed<T>(a) ? (a.d % V == 0 ? name<T, V, false, true> : name<T, V, true, true>) : (a.d % V == 0 ? name<T, V, false, false> : name<T, V, true, false>))
+
 template <typename T>
 hipError_t expert_gather(hipStream_t st, const ExpertRows& a) {
   constexpr int V = wide<T>();
   const int per_row = blocks_of(a.d, V), row_groups = a.n_rows > 0 ? (int)vector_grid(a.n_rows, per_row).x : 0;
   const dim3 grid(row_groups + std::min(blocks_of(a.n_packed, 64), 1 << 20));
-  return enqueue(a.d % V == 0 ? expert_gather_kernel<T, V, false> : expert_gather_kernel<T, V, true>, grid, dim3(ROWS_THREADS), st, a, per_row, row_groups);
+  return enqueue(EXPERT_KERNEL(expert_gather_kernel, T, V), grid, dim3(ROWS_THREADS), st, a, per_row, row_groups);
 }
 template <typename T>
 hipError_t expert_combine(hipStream_t st, const ExpertRows& a) {
   constexpr int V = wide<T>();
   const int per_row = blocks_of(a.d, V);
-  return enqueue(a.d % V == 0 ? expert_combine_kernel<T, V, false> : expert_combine_kernel<T, V, true>, vector_grid(a.n_rows, per_row), dim3(ROWS_THREADS), st, a, per_row);
+  return enqueue(EXPERT_KERNEL(expert_combine_kernel, T, V), vector_grid(a.n_rows, per_row), dim3(ROWS_THREADS), st, a, per_row);
 }
 template <typename T>
 hipError_t expert_combine_grad(hipStream_t st, const ExpertRows& a) {
   constexpr int V = wide<T>();
   const int row_groups = std::min(blocks_of(a.n_packed, 4), 1 << 22);
   const dim3 grid(row_groups + (a.grad_weights ? std::min(blocks_of((long long)a.n_rows * a.k, ROWS_THREADS), 1 << 16) : 0));
-  // more than the last cache holds is written past it: its lines would be written back among the reads (16384 tokens of 2048 with 8 experts each, forward and
-  // backward, 583 -> 562 us; the same in the other two kernels changed nothing)
-  const bool stream = (long long)a.n_packed * a.d * (long long)sizeof(T) > (256ll << 20), whole = a.d % V == 0;
-  const auto kernel = stream ? (whole ? expert_combine_grad_kernel<T, V, false, true> : expert_combine_grad_kernel<T, V, true, true>)
-                             : (whole ? expert_combine_grad_kernel<T, V, false, false> : expert_combine_grad_kernel<T, V, true, false>);
-  return enqueue(kernel, grid, dim3(ROWS_THREADS), st, a, blocks_of(a.d, V), row_groups);
+  return enqueue(EXPERT_KERNEL(expert_combine_grad_kernel, T, V), grid, dim3(ROWS_THREADS), st, a, blocks_of(a.d, V), row_groups);
 }
 
 }  // namespace

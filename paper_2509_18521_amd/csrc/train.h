@@ -17,6 +17,10 @@ __device__ inline long long index_at(const void* p, bool i64, size_t i) {
   return i64 ? static_cast<const long long*>(p)[i] : (long long)static_cast<const int*>(p)[i];
 }
 
+// Whether an array of so many bytes is read or written past the last cache (256 MB): whoever reads a result of more than half of it writes as much again and finds little there,
+// and its lines are written back among the next kernels' reads.
+inline bool streams(long long bytes) { return bytes > (128ll << 20); }
+
 // Element types are template arguments of the kernels; `f32`, `i64` say which one an argument is.
 struct Logprobs {
   int n_rows, vocab, n_top;

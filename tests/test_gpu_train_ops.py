@@ -588,6 +588,38 @@ def test_rows_of_more_elements_than_31_bits_count():
     near(host(g_weights[:, 0]), (host(out) ** 2).sum(1), d * U * (host(out) ** 2).sum(1))
 
 
+@pytest.mark.parametrize("d", [8192, 8191])
+def test_rows_past_the_last_cache(d):
+    """Sizes whose accesses are streamed, whole vectors and rows with a tail; whole numbers, whose sums are exact."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    whole = lambda *s: torch.randint(-8, 9, s, generator=gen, device="cuda").bfloat16()  # noqa: E731
+    n, vocab, k, e = 9000, 9500, 8, 16
+    table, g, tokens = whole(vocab, d), whole(n, d), torch.randint(-5, vocab, (n,), generator=gen, device="cuda")
+    tokens[::9] = 123
+    keep = tokens >= 0
+    assert torch.equal(ap().april_embed(table, tokens), torch.where(keep[:, None], table[tokens.clamp(min=0)], 0))
+    want = torch.zeros((vocab, d), device="cuda").index_add_(0, tokens[keep], g[keep].float()).bfloat16()
+    assert torch.equal(ap().april_embed_grad(g, tokens, vocab), want)
+    start = table.clone()
+    ap().april_embed_grad(g, tokens, vocab, out=start, accumulate=True)
+    assert torch.equal(start, (table.float() + torch.zeros((vocab, d), device="cuda").index_add_(0, tokens[keep], g[keep].float())).bfloat16())
+    del table, start, want
+    x = g[:1200]
+    ids = torch.randint(-1, e, (1200, k), generator=gen, device="cuda")
+    rows = ap().april_expert_sort(ids, e, align=64)
+    there, token = rows.source >= 0, rows.source.clamp(min=0).long() // k
+    packed = ap().april_expert_gather(x, rows)
+    assert torch.equal(packed, torch.where(there[:, None], x[token], 0))
+    position = rows.position.long()
+    want = (x.float() * (position >= 0).sum(1)[:, None]).bfloat16()
+    assert torch.equal(ap().april_expert_combine(packed, rows), want)
+    w = torch.randint(1, 4, (1200, k), generator=gen, device="cuda").float()
+    g_packed, g_weights = ap().april_expert_combine_grad(x, packed, rows, w)
+    assert torch.equal(g_packed, torch.where(there[:, None], x[token].float() * w.reshape(-1)[rows.source.clamp(min=0).long()][:, None], 0).bfloat16())
+    assert torch.equal(g_weights, torch.where(position >= 0, x.float().square().sum(1)[:, None], 0))
+
+
 def test_sorts_of_many_tiles():
     """More tiles than a workgroup adds up by itself."""
     import torch
