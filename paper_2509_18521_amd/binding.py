@@ -779,6 +779,7 @@ def _function(name):
         t = _torch
         once = t.autograd.function.once_differentiable
         whole = lambda g: None if g is None else g.contiguous()  # noqa: E731
+        adjacent = lambda g: g if g.stride(1) == 1 or g.shape[1] == 1 else g.contiguous()  # noqa: E731
 
         class AprilLogprobs(t.autograd.Function):
             @staticmethod
@@ -809,35 +810,33 @@ def _function(name):
             @once
             def backward(ctx, g):
                 vocab, dtype, scale = ctx.of
-                g = g if g.stride(1) == 1 or g.shape[1] == 1 else g.contiguous()
-                return april_embed_grad(g, *ctx.saved_tensors, vocab, scale=scale, dtype=dtype), None, None, None
+                return april_embed_grad(adjacent(g), *ctx.saved_tensors, vocab, scale=scale, dtype=dtype), None, None, None
 
         class AprilExpertGather(t.autograd.Function):
             @staticmethod
-            def forward(ctx, x, starts, source, position):
-                ctx.save_for_backward(starts, source, position)
-                return _expert_gather(x, ExpertRows(starts, source, position), None)
+            def forward(ctx, x, source, position):
+                ctx.save_for_backward(position)
+                return _expert_gather(x, source, position, None)
 
             @staticmethod
             @once
             def backward(ctx, g):
-                g = g if g.stride(1) == 1 or g.shape[1] == 1 else g.contiguous()
-                return _expert_combine(g, ExpertRows(*ctx.saved_tensors), None, None), None, None, None
+                position, = ctx.saved_tensors
+                return _combine(adjacent(g), position, None, None), None, None
 
         class AprilExpertCombine(t.autograd.Function):
             @staticmethod
-            def forward(ctx, packed, starts, source, position, weights):
-                ctx.save_for_backward(packed, starts, source, position, weights)
-                return _expert_combine(packed, ExpertRows(starts, source, position), weights, None)
+            def forward(ctx, packed, source, position, weights):
+                ctx.save_for_backward(packed, source, position, weights)
+                return _expert_combine(packed, source, position, weights, None)
 
             @staticmethod
             @once
             def backward(ctx, g):
-                packed, starts, source, position, weights = ctx.saved_tensors
-                g = g if g.stride(1) == 1 or g.shape[1] == 1 else g.contiguous()
-                of_packed, of_weights = april_expert_combine_grad(g, packed, ExpertRows(starts, source, position), weights, of_packed=ctx.needs_input_grad[0],
-                                                                  of_weights=ctx.needs_input_grad[4])
-                return of_packed, None, None, None, of_weights
+                packed, source, position, weights = ctx.saved_tensors
+                of_packed, _, _, of_weights = ctx.needs_input_grad
+                of_packed, of_weights = _combine_grad(adjacent(g), packed, source, position, weights, of_packed, of_weights)
+                return of_packed, None, None, of_weights
 
         _functions.update(logprobs=AprilLogprobs, embed=AprilEmbed, gather=AprilExpertGather, combine=AprilExpertCombine)
     return _functions[name]
@@ -973,24 +972,26 @@ def april_expert_sort(ids, n_experts: int, *, align: int = 1) -> ExpertRows:
     return rows
 
 
-def _expert_sizes(rows, dev):
-    """(rows, experts of a row, packed rows, pointer of source, of position)."""
-    n, k = _two("rows.position", rows.position)
-    if len(rows.source.shape) != 1:
+def _expert_sizes(source, position, dev):
+    """(rows, experts of a row, packed rows)."""
+    n, k = _two("rows.position", position)
+    if len(source.shape) != 1:
         _refuse("rows.source: one dimension wanted")
-    m = rows.source.shape[0]
-    return n, k, m, _ptr("rows.source", rows.source, _torch.int32, (m,), dev), _ptr("rows.position", rows.position, _torch.int32, (n, k), dev)
+    m = source.shape[0]
+    _ptr("rows.source", source, _torch.int32, (m,), dev)
+    _ptr("rows.position", position, _torch.int32, (n, k), dev)
+    return n, k, m
 
 
-def _expert_gather(x, rows, out):
+def _expert_gather(x, source, position, out):
     d = _two("x", x)[1]
     dev, dtype = _gpu("x", x), _dtype("x", x.dtype)
-    n, k, m, source, position = _expert_sizes(rows, dev)
+    n, k, m = _expert_sizes(source, position, dev)
     if out is None:
         out = _torch.empty((m, d), dtype=x.dtype, device=x.device)
     p, row = _matrix("x", x, x.dtype, (n, d), dev)
     op, o_row = _matrix("out", out, x.dtype, (m, d), dev)
-    _enqueue(_call("april_expert_gather"), dev, _PACK_EXPERT_GATHER, n, k, d, m, dtype, 0, row, o_row, p, source, position, op)
+    _enqueue(_call("april_expert_gather"), dev, _PACK_EXPERT_GATHER, n, k, d, m, dtype, 0, row, o_row, p, source.data_ptr(), position.data_ptr(), op)
     return out
 
 
@@ -1000,20 +1001,30 @@ def april_expert_gather(x, rows: ExpertRows, *, out=None):
     if _records(x, out):
         if out is not None:
             _differentiable("x" if x.requires_grad else "out")
-        return _function("gather").apply(x, *rows)
-    return _expert_gather(x, rows, out)
+        return _function("gather").apply(x, rows.source, rows.position)
+    return _expert_gather(x, rows.source, rows.position, out)
 
 
-def _expert_combine(packed, rows, weights, out):
-    m, d = _two("packed", packed)
-    dev, dtype = _gpu("packed", packed), _dtype("packed", packed.dtype)
-    n, k, m, _, position = _expert_sizes(rows, dev)
+def _combine(packed, position, weights, out):
+    """(The arguments are checked.)"""
+    (m, d), (n, k) = packed.shape, position.shape
     if out is None:
         out = _torch.empty((n, d), dtype=packed.dtype, device=packed.device)
-    p, row = _matrix("packed", packed, packed.dtype, (m, d), dev)
-    op, o_row = _matrix("out", out, packed.dtype, (n, d), dev)
-    _enqueue(_call("april_expert_combine"), dev, _PACK_EXPERT_COMBINE, n, k, d, m, dtype, 0, row, o_row, p, position, _float_ptr("weights", weights, (n, k), dev), op)
+    _enqueue(_call("april_expert_combine"), packed.get_device(), _PACK_EXPERT_COMBINE, n, k, d, m, APRIL_DTYPE_FP32 if packed.dtype is _torch.float32 else APRIL_DTYPE_BF16, 0,
+             packed.stride(0), out.stride(0), packed.data_ptr(), position.data_ptr(), 0 if weights is None else weights.data_ptr(), out.data_ptr())
     return out
+
+
+def _expert_combine(packed, source, position, weights, out):
+    d = _two("packed", packed)[1]
+    dev = _gpu("packed", packed)
+    _dtype("packed", packed.dtype)
+    n, k, m = _expert_sizes(source, position, dev)
+    _matrix("packed", packed, packed.dtype, (m, d), dev)
+    if out is not None:
+        _matrix("out", out, packed.dtype, (n, d), dev)
+    _float_ptr("weights", weights, (n, k), dev)
+    return _combine(packed, position, weights, out)
 
 
 def april_expert_combine(packed, rows: ExpertRows, weights=None, *, out=None):
@@ -1022,23 +1033,32 @@ def april_expert_combine(packed, rows: ExpertRows, weights=None, *, out=None):
     if _records(packed, weights, out):
         if out is not None:
             _differentiable("packed" if packed.requires_grad else "weights" if weights is not None and weights.requires_grad else "out")
-        return _function("combine").apply(packed, *rows, weights)
-    return _expert_combine(packed, rows, weights, out)
+        return _function("combine").apply(packed, rows.source, rows.position, weights)
+    return _expert_combine(packed, rows.source, rows.position, weights, out)
+
+
+def _combine_grad(grad_out, packed, source, position, weights, of_packed, of_weights):
+    """(The arguments are checked.)"""
+    (m, d), (n, k) = packed.shape, position.shape
+    g_packed = _torch.empty((m, d), dtype=packed.dtype, device=packed.device) if of_packed else None
+    g_weights = _torch.empty((n, k), dtype=_torch.float32, device=packed.device) if of_weights else None
+    _enqueue(_call("april_expert_combine_grad"), packed.get_device(), _PACK_EXPERT_COMBINE_GRAD, n, k, d, m,
+             APRIL_DTYPE_FP32 if packed.dtype is _torch.float32 else APRIL_DTYPE_BF16, 0, grad_out.stride(0), packed.stride(0), d, grad_out.data_ptr(), packed.data_ptr(),
+             source.data_ptr(), position.data_ptr(), 0 if weights is None else weights.data_ptr(), g_packed.data_ptr() if of_packed else 0, g_weights.data_ptr() if of_weights else 0)
+    return g_packed, g_weights
 
 
 def april_expert_combine_grad(grad_out, packed, rows: ExpertRows, weights=None, *, of_packed: bool = True, of_weights: bool = True):
     """(gradient of packed, gradient of weights) for the gradient [n_rows, d] of april_expert_combine's result; None where not asked for.  Not differentiable."""
     _no_gradient(grad_out=grad_out, packed=packed, weights=weights)
     d = _two("grad_out", grad_out)[1]
-    dev, dtype = _gpu("grad_out", grad_out), _dtype("grad_out", grad_out.dtype)
-    n, k, m, source, position = _expert_sizes(rows, dev)
-    g, row = _matrix("grad_out", grad_out, grad_out.dtype, (n, d), dev)
-    p, p_row = _matrix("packed", packed, grad_out.dtype, (m, d), dev)
-    g_packed = _torch.empty((m, d), dtype=packed.dtype, device=packed.device) if of_packed else None
-    g_weights = _torch.empty((n, k), dtype=_torch.float32, device=packed.device) if of_weights else None
-    _enqueue(_call("april_expert_combine_grad"), dev, _PACK_EXPERT_COMBINE_GRAD, n, k, d, m, dtype, 0, row, p_row, d, g, p, source, position,
-             _float_ptr("weights", weights, (n, k), dev), g_packed.data_ptr() if of_packed else 0, g_weights.data_ptr() if of_weights else 0)
-    return g_packed, g_weights
+    dev = _gpu("grad_out", grad_out)
+    _dtype("grad_out", grad_out.dtype)
+    n, k, m = _expert_sizes(rows.source, rows.position, dev)
+    _matrix("grad_out", grad_out, grad_out.dtype, (n, d), dev)
+    _matrix("packed", packed, grad_out.dtype, (m, d), dev)
+    _float_ptr("weights", weights, (n, k), dev)
+    return _combine_grad(grad_out, packed, rows.source, rows.position, weights, of_packed, of_weights)
 
 
 # ---------------------------------------------------------------------------
