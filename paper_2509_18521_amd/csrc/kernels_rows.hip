@@ -592,22 +592,25 @@ hipError_t embed_grad(hipStream_t st, const EmbedGrad& a) {
 // ---------------------------------------------------------------------------
 // Tokens' rows in their experts' batches.
 // ---------------------------------------------------------------------------
-// The tokens' rows, each read once and stored at its k places; workgroups behind those write zeros to the packed rows of no assignment, a wavefront 16 of them.
+// Zeros in the packed rows of no assignment, a wavefront 16 of them, on the workgroups behind the tokens'.
+template <typename T, int V, bool TAIL, bool STREAM>
+__device__ inline void write_zero_rows(const ExpertRows& a, T* out, long long row, int per_row, int row_groups) {
+  const long long n = (long long)a.n_rows * a.k;
+  const int lane = threadIdx.x & 63;
+  for (long long p0 = ((long long)(blockIdx.x - row_groups) * 4 + (threadIdx.x >> 6)) * 16; p0 < a.n_packed; p0 += (long long)(gridDim.x - row_groups) * 64) {
+    const int from = lane < 16 && p0 + lane < a.n_packed ? a.source[p0 + lane] : 0;
+    float x[V];
+    zero(x);
+    for (unsigned long long none = __ballot(lane < 16 && p0 + lane < a.n_packed && (from < 0 || from >= n)); none != 0; none &= none - 1)
+      for (int col = lane; col < per_row; col += 64) store<T, V, STREAM>(out + (p0 + __ffsll((long long)none) - 1) * row + (long long)col * V, x, elements<V, TAIL>(a.d, col));
+  }
+}
+
+// The tokens' rows, each read once and stored at its k places.
 template <typename T, int V, bool TAIL, bool STREAM>
 __global__ __launch_bounds__(ROWS_THREADS) void expert_gather_kernel(ExpertRows a, int per_row, int row_groups) {
   T* out = static_cast<T*>(a.out);
-  if ((int)blockIdx.x >= row_groups) {
-    const long long n = (long long)a.n_rows * a.k;
-    const int lane = threadIdx.x & 63;
-    for (long long p0 = ((long long)(blockIdx.x - row_groups) * 4 + (threadIdx.x >> 6)) * 16; p0 < a.n_packed; p0 += (long long)(gridDim.x - row_groups) * 64) {
-      const int from = lane < 16 && p0 + lane < a.n_packed ? a.source[p0 + lane] : 0;
-      float x[V];
-      zero(x);
-      for (unsigned long long none = __ballot(lane < 16 && p0 + lane < a.n_packed && (from < 0 || from >= n)); none != 0; none &= none - 1)
-        for (int col = lane; col < per_row; col += 64) store<T, V, STREAM>(out + (p0 + __ffsll((long long)none) - 1) * a.packed_row + (long long)col * V, x, elements<V, TAIL>(a.d, col));
-    }
-    return;
-  }
+  if ((int)blockIdx.x >= row_groups) return write_zero_rows<T, V, TAIL, STREAM>(a, out, a.packed_row, per_row, row_groups);
   for (long long first = (long long)blockIdx.x * ROWS_THREADS; first < (long long)a.n_rows * per_row; first += (long long)row_groups * ROWS_THREADS) {
     const At at = vector_at(first, threadIdx.x, per_row);
     if (at.row >= a.n_rows) continue;
@@ -659,40 +662,74 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_combine_kernel(ExpertRows
   }
 }
 
-// One wavefront a packed row: its gradient, and its weight's.  Workgroups behind those write the weights' of assignments that are nowhere.  Bound by HBM: 16384 tokens of
-// 2048 in bf16 with 8 experts each 206 us (5.2 TB/s).
-template <typename T, int V, bool TAIL, bool STREAM>
+// A token's rows again: its gradient is read once and stored at its k places, eight packed rows in flight for the weights' gradients.  WAVES wavefronts a token.  Bound by HBM:
+// 16384 tokens of 2048 in bf16 with 8 experts each 185 us (5.8 TB/s); by packed rows, which read a token's gradient k times, 208.
+template <typename T, int V, bool TAIL, bool STREAM, int WAVES>
 __global__ __launch_bounds__(ROWS_THREADS) void expert_combine_grad_kernel(ExpertRows a, int per_row, int row_groups) {
-  const int lane = threadIdx.x & 63;
-  const long long n = (long long)a.n_rows * a.k;
-  if ((int)blockIdx.x >= row_groups) {
-    for (long long i = (long long)(blockIdx.x - row_groups) * ROWS_THREADS + threadIdx.x; i < n; i += (long long)(gridDim.x - row_groups) * ROWS_THREADS)
-      if (a.position[i] < 0 || a.position[i] >= a.n_packed) a.grad_weights[i] = 0.f;
-    return;
-  }
-  for (long long p = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); p < a.n_packed; p += (long long)row_groups * 4) {
-    const int from = a.source[p];
-    const bool there = from >= 0 && from < n;
-    const float w = there && a.weights ? a.weights[from] : 1.f;
-    float dot = 0.f;
-    for (int col = lane; col < per_row; col += 64) {
-      const int here = elements<V, TAIL>(a.d, col);
-      float g[V], y[V];
-      zero(g);
-      if (there) {
-        load<T, V>(g, static_cast<const T*>(a.rows) + (long long)(from / a.k) * a.row + (long long)col * V, here);
-        if (a.grad_weights) {
-          load<T, V, STREAM>(y, static_cast<const T*>(a.packed) + p * a.packed_row + (long long)col * V, here);
+  T* out = static_cast<T*>(a.grad_packed);
+  if ((int)blockIdx.x >= row_groups) return write_zero_rows<T, V, TAIL, STREAM>(a, out, a.grad_row, per_row, row_groups);
+  constexpr int ROWS = ROWS_THREADS / 64 / WAVES;            // of a workgroup at a time
+  __shared__ float part[4][8];
+  const int tid = threadIdx.x & (64 * WAVES - 1), wave = threadIdx.x >> 6;
+  for (long long r0 = (long long)blockIdx.x * ROWS; r0 < a.n_rows; r0 += (long long)row_groups * ROWS) {
+    const long long r = r0 + wave / WAVES;
+    const bool row = r < a.n_rows;
+    for (int j0 = 0; j0 < a.k; j0 += 8) {
+      int at[8];
+      float w[8], dot[8];
 #pragma unroll
-          for (int i = 0; i < V; ++i) dot = fmaf(g[i], y[i], dot);
+      for (int j = 0; j < 8; ++j) {
+        at[j] = row && j0 + j < a.k ? a.position[r * a.k + j0 + j] : -1;
+        if (at[j] >= a.n_packed) at[j] = -1;
+        w[j] = a.weights != nullptr && at[j] >= 0 ? a.weights[r * a.k + j0 + j] : 1.f;
+        dot[j] = 0.f;
+      }
+      for (int col = tid; row && col < per_row; col += 64 * WAVES) {
+        const int n = elements<V, TAIL>(a.d, col);
+        float g[V];
+        load<T, V>(g, static_cast<const T*>(a.rows) + r * a.row + (long long)col * V, n);
+        if (a.grad_weights) {
+          Raw<T, V> y[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (at[j] >= 0) y[j].template load<STREAM>(static_cast<const T*>(a.packed) + at[j] * a.packed_row + (long long)col * V, n);
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (at[j] >= 0) {
+#pragma unroll
+              for (int i = 0; i < V; ++i) dot[j] = fmaf(g[i], y[j][i], dot[j]);
+            }
+        }
+        if (out != nullptr) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (at[j] >= 0) {
+              float x[V];
+#pragma unroll
+              for (int i = 0; i < V; ++i) x[i] = w[j] * g[i];
+              store<T, V, STREAM>(out + at[j] * a.grad_row + (long long)col * V, x, n);
+            }
         }
       }
+      if (!a.grad_weights) continue;
 #pragma unroll
-      for (int i = 0; i < V; ++i) g[i] *= w;
-      if (a.grad_packed) store<T, V, STREAM>(static_cast<T*>(a.grad_packed) + p * a.grad_row + (long long)col * V, g, here);
+      for (int j = 0; j < 8; ++j) dot[j] = wave_sum_f32(dot[j]);
+      if (WAVES > 1) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) part[wave][j] = dot[j];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dot[j] = (part[0][j] + part[1][j]) + (part[2][j] + part[3][j]);
+      }
+      if (row && tid == 0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j0 + j < a.k) a.grad_weights[r * a.k + j0 + j] = at[j] >= 0 ? dot[j] : 0.f;
+      }
     }
-    dot = wave_sum_f32(dot);
-    if (there && a.grad_weights && lane == 0) a.grad_weights[from] = dot;
   }
 }
 
@@ -719,9 +756,19 @@ hipError_t expert_combine(hipStream_t st, const ExpertRows& a) {
 template <typename T>
 hipError_t expert_combine_grad(hipStream_t st, const ExpertRows& a) {
   constexpr int V = wide<T>();
-  const int row_groups = std::min(blocks_of(a.n_packed, 4), 1 << 22);
-  const dim3 grid(row_groups + (a.grad_weights ? std::min(blocks_of((long long)a.n_rows * a.k, ROWS_THREADS), 1 << 16) : 0));
-  return enqueue(EXPERT_KERNEL(expert_combine_grad_kernel, T, V), grid, dim3(ROWS_THREADS), st, a, blocks_of(a.d, V), row_groups);
+  const int per_row = blocks_of(a.d, V), waves = per_row > 64 ? 4 : 1;
+  const int row_groups = std::min(blocks_of(a.n_rows, 4 / waves), 1 << 22), zeros = a.grad_packed ? std::min(blocks_of(a.n_packed, 64), 1 << 20) : 0;
+  auto run = [&](auto whole, auto tail, auto whole_streamed, auto tail_streamed) {
+    return enqueue(streamed<T>(a) ? (a.d % V == 0 ? whole_streamed : tail_streamed) : (a.d % V == 0 ? whole : tail), dim3(row_groups + zeros), dim3(ROWS_THREADS), st, a, per_row, row_groups);
+  };
+#define KERNEL(TAIL, STREAM) expert_combine_grad_kernel<T, V, TAIL, STREAM, W>
+  if (waves == 4) {
+    constexpr int W = 4;
+    return run(KERNEL(false, false), KERNEL(true, false), KERNEL(false, true), KERNEL(true, true));
+  }
+  constexpr int W = 1;
+  return run(KERNEL(false, false), KERNEL(true, false), KERNEL(false, true), KERNEL(true, true));
+#undef KERNEL
 }
 
 }  // namespace
