@@ -142,7 +142,7 @@ struct Scan {
 // ---------------------------------------------------------------------------
 // The k largest of a run, by value and then by index.  256 groups of threads have a largest element each; where k of those reach a bound, so do k
 // elements, and only sections of a thread whose own largest reaches it have candidates: their vectors are read again, one to a thread
-// (4 to 40 of 16 bytes in lines of their own: whole threads' vectors instead of sections cost 4096 rows of 128256 in bf16 277 us, these 226, no search 209).  The
+// (4 to 40 of 16 bytes in lines of their own: whole threads' vectors instead of sections cost 4096 rows of 128256 in bf16 277 us where these took 226: now 210, and 174 without a search).  The
 // bound is searched bit by bit in registers, by every wavefront for itself.  More candidates than the list holds: those above the exact k-th largest of the groups
 // (no more than k - 1 groups have any), and then those equal to it in the run's order until there are k; where even the former are too
 // many, k passes over the run.
