@@ -397,7 +397,8 @@ __device__ inline bool no_top(const Logprobs& a, int r, const Part& p, int tid, 
 }
 
 // One workgroup a row, one pass over it.  Bound by HBM: 12288 rows of 151936 in bf16 544 us (6.9 TB/s), 192 in fp32 27
-// (4.3; 22 where they lie in the last cache).
+// (4.3; 22 where they lie in the last cache).  Registers before wavefronts: with 8 a SIMD the scan of bf16 spills, and 8192 rows of 128256 take 389 us instead of 350 (before
+// their loads were streamed).
 template <typename T, bool ENT, bool TOP, int NT, bool STREAM>
 __global__ __launch_bounds__(NT, 5) void logprobs_kernel(Logprobs a) {
   __shared__ RowShared<NT> sh;

@@ -827,3 +827,42 @@ def test_on_another_stream():
     side.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+def test_two_streams_at_once():
+    """The same work on two streams, each call with its own workspace, side by side."""
+    import torch
+    rng = np.random.default_rng(23)
+    n, vocab, d, e, k = 90, 60001, 96, 16, 4
+    logits, grad, table = place(rng.standard_normal((n, vocab)), "f32"), place(rng.standard_normal((6000, d)), "bf16"), place(rng.standard_normal((vocab, d)), "bf16")
+    tokens, many = index(rng.integers(0, vocab, size=n), 64), index(tokens_of(rng, 6000, vocab, "skewed"), 64)
+    ids, w, g = index(expert_ids(rng, 6000, k, e, True), 32), f32(rng.random((6000, k))), f32(rng.standard_normal(n))
+
+    def work():
+        got = ap().april_logprobs(logits, tokens, entropy=True, top=9)
+        rows = ap().april_expert_sort(ids, e, align=8)
+        packed = ap().april_expert_gather(grad, rows)
+        return [got.logprob, got.entropy, got.top_ids, ap().april_logprobs_grad(logits, tokens, got, grad_logprob=g, grad_entropy=g), *rows, packed, ap().april_expert_combine(packed, rows, w),
+                *ap().april_expert_combine_grad(grad, packed, rows, w), ap().april_embed(table, many), ap().april_embed_grad(grad, many, vocab)]
+    want = work()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(3):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = work()
+    torch.cuda.synchronize()
+    for side in got:
+        for a, b in zip(side, want):
+            assert torch.equal(a.nan_to_num(), b.nan_to_num())      # (a token beyond the table: a row of NaN)
+
+
+def test_no_second_derivative():
+    """A gradient of a gradient is refused by autograd, not silently zero."""
+    import torch
+    x = torch.randn((4, 9), device="cuda", requires_grad=True)
+    t = index([1, 2, -1, 0], 64)
+    (g,) = torch.autograd.grad(ap().april_logprobs(x, t).logprob.sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
