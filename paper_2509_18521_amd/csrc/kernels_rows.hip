@@ -12,11 +12,13 @@ namespace {
 // Stable sort of n small keys: passes over digits of 9 bits, in tiles of 4096 keys.  A wavefront ranks 64 keys at a time: the lanes
 // with an equal digit by nine ballots, those of earlier steps by its own counters in LDS.  A pass is two launches, digits counted for each tile, then moved: a
 // tile's workgroup adds up the other tiles' counts itself (up to 256 tiles; beyond, a launch between does).  One tile is sorted in one launch.
-// Bound by latency: 32768 tokens 15 us a pass, 111 k experts' ids 14, 3072 9.
+// Bound by latency: 32768 tokens 15 us a pass, 111 k experts' ids 14, one tile of them 9.
 // ---------------------------------------------------------------------------
 constexpr int BITS = 9, BINS = 1 << BITS;
 constexpr int SORT_THREADS = 1024, SORT_WAVES = 16, SORT_STEPS = 4, SORT_TILE = SORT_THREADS * SORT_STEPS;
 constexpr int ADD_TILES = 256;
+// Passes over keys up to `limit` (four from 2^27 on; a shift by 36 is none).
+__host__ __device__ inline int sort_passes(int limit) { return limit >> BITS == 0 ? 1 : limit >> 2 * BITS == 0 ? 2 : limit >> 3 * BITS == 0 ? 3 : 4; }
 
 struct SortIn {
   const void* ids;         // the caller's, where keys is null; one outside 0 .. limit - 1 counts as limit
@@ -214,7 +216,7 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_tile_kernel(SortIn in, int*
   int row[SORT_STEPS];
 #pragma unroll
   for (int s = 0; s < SORT_STEPS; ++s) row[s] = (int)t.place(s);
-  for (int shift = 0; shift == 0 || in.limit >> shift > 0; shift += BITS) {
+  for (int shift = 0, end = sort_passes(in.limit) * BITS; shift < end; shift += BITS) {
     t.count(sh, shift);
     const int tid = threadIdx.x;
     t.place_from(sh, shift, sum_before(tid < BINS ? t.total(sh) : 0));
@@ -268,7 +270,7 @@ __global__ __launch_bounds__(SORT_THREADS) void expert_place_kernel(SortIn in, i
   // a wavefront fills the room behind an expert's last row, all threads what lies behind the last expert's
   const int lane = tid & 63;
   for (int e = tile * SORT_WAVES + (tid >> 6); e < n_experts; e += gridDim.x * SORT_WAVES)
-    for (int p = end_of[e] + lane; p < first_of[e + 1]; p += 64) a.source[p] = -1;
+    for (long long p = end_of[e] + lane; p < first_of[e + 1]; p += 64) a.source[p] = -1;      // (the last rows may end within 64 of 2^31)
   for (long long p = end_of[n_experts] + (long long)tile * SORT_THREADS + tid; p < a.n_packed; p += (long long)gridDim.x * SORT_THREADS) a.source[p] = -1;
   for (int g = tile * SORT_THREADS + tid; g < a.n_groups; g += gridDim.x * SORT_THREADS) {
     int lo = 0, hi = n_experts;                              // the last expert that begins at the group's first row or before
@@ -540,9 +542,7 @@ struct GradSpace {
 template <typename TO, typename TT>
 hipError_t embed_grad(hipStream_t st, const EmbedGrad& a) {
   const GradSpace w(a);
-  const int tiles = blocks_of(a.n_rows, SORT_TILE);
-  int passes = 1;
-  while (a.vocab >> (passes * BITS) > 0) ++passes;
+  const int tiles = blocks_of(a.n_rows, SORT_TILE), passes = sort_passes(a.vocab);
   const int launches = tiles > 1 ? 2 * passes : 1;
   // the table's zeros, in as many shares as there are launches
   const long long row = (long long)a.d * sizeof(TT), stride = a.table_row * (long long)sizeof(TT);

@@ -866,3 +866,19 @@ def test_no_second_derivative():
     (g,) = torch.autograd.grad(ap().april_logprobs(x, t).logprob.sum(), x, create_graph=True)
     with pytest.raises(RuntimeError):
         g.sum().backward()
+
+
+@pytest.mark.parametrize("n", [40, 5000])
+@pytest.mark.parametrize("vocab", [(1 << 27) - 1, 1 << 27, (1 << 27) + 77])
+def test_embed_grad_of_the_largest_tables(vocab, n):
+    """Tokens of 27 bits and 28: one more digit of the sort, and no more than four."""
+    import torch
+    rng = np.random.default_rng(24)
+    few = np.concatenate([rng.integers(0, vocab, size=12), [0, vocab - 1, vocab >> 1, (1 << 26) + 5, 5, vocab]])
+    tokens = few[rng.integers(0, len(few), size=n)]
+    grad = rng.integers(-8, 9, size=(n, 1)).astype(np.float64)      # (sums of few bits: exact)
+    got = ap().april_embed_grad(place(grad, "f32"), index(tokens, 32), vocab)
+    want = {int(t): grad[tokens == t, 0].sum() for t in few if t < vocab}
+    for t, v in want.items():
+        assert float(got[t, 0]) == v, t
+    assert float(got.double().abs().sum()) == sum(abs(v) for v in want.values())
