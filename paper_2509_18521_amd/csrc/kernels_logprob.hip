@@ -542,10 +542,10 @@ constexpr int GRAD_THREADS = 256, GRAD_VECS = 4;
 template <typename T, bool ENT>
 struct GradRow {
   float m, c2, l2, q, hl, add;
-  // d logits = p * (q + hl * log2 p), and `add` at the token
+  // d logits = p * (q + hl * log2 p), and `add` at the token.  (p is 0 long before log2 p is -1024, and hl * 1024 is finite for any gradient that a sum of them could be)
   __device__ __forceinline__ float operator()(float x) const {
     const float lp = (x - m) * c2 - l2, p = __builtin_amdgcn_exp2f(lp);
-    return ENT ? p * fmaf(hl, fmaxf(lp, -1e30f), q) : p * q;
+    return ENT ? p * fmaf(hl, fmaxf(lp, -1024.f), q) : p * q;
   }
 };
 

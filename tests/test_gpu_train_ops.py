@@ -882,3 +882,17 @@ def test_embed_grad_of_the_largest_tables(vocab, n):
     for t, v in want.items():
         assert float(got[t, 0]) == v, t
     assert float(got.double().abs().sum()) == sum(abs(v) for v in want.values())
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_large_gradients_of_the_entropy_leave_masked_tokens_alone(t):
+    """The gradient is linear in the entropy's own, and by a power of two to the bit: also where a logit is masked, at 2^60."""
+    rng = np.random.default_rng(25)
+    x = rng.standard_normal((9, 3001))
+    x[:, 1::3] = -np.inf
+    x[:, 2::7] = -3e38
+    logits, tokens = place(x, t), index(np.zeros(9), 64)
+    got = ap().april_logprobs(logits, tokens, entropy=True)
+    one, large = (ap().april_logprobs_grad(logits, tokens, got, grad_entropy=f32(np.full(9, h))) for h in (1.0, 2.0 ** 60))
+    assert np.array_equal(host(one) * 2.0 ** 60, host(large))
+    assert (host(large)[x < -1e30] == 0).all() and (host(large) != 0).sum() > 9 * 1000
