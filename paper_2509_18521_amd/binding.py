@@ -766,6 +766,12 @@ def _no_gradient(**tensors):
             _differentiable(name)
 
 
+def _wrote(out):
+    """The caller's `out`, which autograd now knows to be changed: where it was kept for a gradient, that backward pass is refused."""
+    _torch.autograd.graph.increment_version(out)
+    return out
+
+
 def _space(call, pack, fields, device):
     """(tensor, pointer, bytes) of the workspace that the call asks for."""
     need = _check(None, _call(call)(_bytes(pack, *fields, 0, 0, 0)))
@@ -900,7 +906,8 @@ def april_logprobs_grad(logits, tokens, made: Logprobs, *, grad_logprob=None, gr
     entropy = None if grad_entropy is None else made.entropy
     for name, t in (("made.entropy", entropy), ("grad_logprob", grad_logprob), ("grad_entropy", grad_entropy), ("grad_lse", grad_lse)):
         _float_ptr(name, t, (n,), dev)
-    return _logprobs_grad(logits, tokens, made.norm, entropy, grad_logprob, grad_entropy, grad_lse, temperature, out)
+    got = _logprobs_grad(logits, tokens, made.norm, entropy, grad_logprob, grad_entropy, grad_lse, temperature, out)
+    return got if out is None else _wrote(out)
 
 
 def _embed(table, tokens, scale, dtype, out):
@@ -928,13 +935,15 @@ def april_embed(table, tokens, *, scale: float = 1.0, dtype=None, out=None):
         if out is not None:
             _differentiable("table" if table.requires_grad else "out")
         return _function("embed").apply(table, tokens, scale, dtype)
-    return _embed(table, tokens, scale, dtype, out)
+    got = _embed(table, tokens, scale, dtype, out)
+    return got if out is None else _wrote(out)
 
 
 def april_embed_grad(grad_out, tokens, vocab: int, *, scale: float = 1.0, dtype=None, out=None, accumulate: bool = False):
     """Gradient [vocab, d] of april_embed's table (of type dtype or out's; else of grad_out's) for the gradient [n_rows, d] of its result.  accumulate: added to
     `out`, of which the rows of no token are not touched.  Not differentiable."""
     _no_gradient(grad_out=grad_out, out=out)
+    given = out is not None
     n, d = _two("grad_out", grad_out)
     dev, of = _gpu("grad_out", grad_out), _dtype("grad_out", grad_out.dtype)
     if out is None:
@@ -952,7 +961,7 @@ def april_embed_grad(grad_out, tokens, vocab: int, *, scale: float = 1.0, dtype=
     fields = n, vocab, d, of, to, bits, scale, 1 if accumulate else 0, row, o_row, p, tp, op
     space, at, need = _space("april_embed_grad_workspace", _PACK_EMBED_GRAD, fields, grad_out.device)
     _enqueue(_call("april_embed_grad"), dev, _PACK_EMBED_GRAD, *fields, at, need)
-    return out
+    return _wrote(out) if given else out
 
 
 def april_expert_sort(ids, n_experts: int, *, align: int = 1) -> ExpertRows:
@@ -1002,7 +1011,8 @@ def april_expert_gather(x, rows: ExpertRows, *, out=None):
         if out is not None:
             _differentiable("x" if x.requires_grad else "out")
         return _function("gather").apply(x, rows.source, rows.position)
-    return _expert_gather(x, rows.source, rows.position, out)
+    got = _expert_gather(x, rows.source, rows.position, out)
+    return got if out is None else _wrote(out)
 
 
 def _combine(packed, position, weights, out):
@@ -1034,7 +1044,8 @@ def april_expert_combine(packed, rows: ExpertRows, weights=None, *, out=None):
         if out is not None:
             _differentiable("packed" if packed.requires_grad else "weights" if weights is not None and weights.requires_grad else "out")
         return _function("combine").apply(packed, rows.source, rows.position, weights)
-    return _expert_combine(packed, rows.source, rows.position, weights, out)
+    got = _expert_combine(packed, rows.source, rows.position, weights, out)
+    return got if out is None else _wrote(out)
 
 
 def _combine_grad(grad_out, packed, source, position, weights, of_packed, of_weights):

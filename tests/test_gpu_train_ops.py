@@ -896,3 +896,22 @@ def test_large_gradients_of_the_entropy_leave_masked_tokens_alone(t):
     one, large = (ap().april_logprobs_grad(logits, tokens, got, grad_entropy=f32(np.full(9, h))) for h in (1.0, 2.0 ** 60))
     assert np.array_equal(host(one) * 2.0 ** 60, host(large))
     assert (host(large)[x < -1e30] == 0).all() and (host(large) != 0).sum() > 9 * 1000
+
+
+def test_a_written_out_is_known_to_autograd():
+    """What is overwritten after autograd kept it makes the backward pass an error, not a wrong gradient."""
+    import torch
+    tokens, ids = index([1, 0, 2, -1], 64), index([[0], [1], [1], [0]], 32)
+    rows = ap().april_expert_sort(ids, 2)
+    table, x = f32(np.ones((5, 8))), f32(np.ones((4, 8)))
+    logits = f32(np.ones((4, 8)))
+    made = ap().april_logprobs(logits, tokens)
+    for call in (lambda out: ap().april_embed(table, tokens, out=out), lambda out: ap().april_expert_gather(x, rows, out=out), lambda out: ap().april_expert_combine(x, rows, out=out),
+                 lambda out: ap().april_embed_grad(x, tokens, 4, out=out), lambda out: ap().april_embed_grad(x, tokens, 4, out=out, accumulate=True),
+                 lambda out: ap().april_logprobs_grad(logits, tokens, made, grad_logprob=f32(np.ones(4)), out=out)):
+        kept = torch.zeros((4, 8), device="cuda")
+        leaf = torch.ones((4, 8), device="cuda", requires_grad=True)
+        y = (leaf * kept).sum()
+        assert call(kept) is kept
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
