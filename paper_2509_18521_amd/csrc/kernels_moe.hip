@@ -2,8 +2,8 @@
 // expert dispatch lists, grouped expert GEMMs on v_mfma_f32_32x32x16_bf16.
 //
 // Per token: r = softmax over all E router logits; the top_k largest r (ties: lower
-// expert index) are kept and renormalised to sum 1; y = sum_k w_k * expert_k(h), added to
-// the residual stream in the fixed order k = 0..top_k-1 (descending r) by the following
+// expert index) are kept and renormalised to sum 1 (a row whose soft-max is NaN keeps experts 0 .. top_k - 1 with
+// weights of NaN); y = sum_k w_k * expert_k(h), added to the residual stream in the fixed order k = 0..top_k-1 (descending r) by the following
 // add/RMSNorm kernel, so the result does not depend on where a token lands in an expert's
 // batch.
 #include "kernels.h"
@@ -60,10 +60,13 @@ __global__ __launch_bounds__(64) void moe_route_kernel(RowCtx rc, const float* l
       const int e = lane + 64 * j;
       if (e < E && v[j] > lv) { lv = v[j]; li = e; }      // ascending e within the lane
     }
+    // Logits with a NaN or +infinity, or nothing but -infinity, make a soft-max of NaN, of which no lane has a largest: the dispatch and the
+    // sum of the experts' outputs index by these numbers, so each is an expert's.
     const float bv = wave_max_f32(lv);
-    const int bi = wave_min_i32(lv == bv ? li : 0x7fffffff);
+    const bool none = bv < 0.f;
+    const int bi = none ? k : wave_min_i32(lv == bv ? li : 0x7fffffff);
     kept += bv;
-    if (lane == k) { myw = bv; myid = bi; }
+    if (lane == k) { myw = none ? NAN : bv; myid = bi; }
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = bi == lane + 64 * j ? -2.f : v[j];   // remove the winner
   }
