@@ -404,7 +404,8 @@ __global__ __launch_bounds__(NT, 5) void logprobs_kernel(Logprobs a) {
   __shared__ RowShared<NT> sh;
   __shared__ std::conditional_t<TOP, TopShared<NT>, int> st;
   const int tid = threadIdx.x;
-  for (int r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
+  for (long long at = blockIdx.x; at < a.n_rows; at += gridDim.x) {      // (a row past the last may have a number beyond 2^31)
+    const int r = (int)at;
     const T* row = static_cast<const T*>(a.logits) + (long long)r * a.row;
     const long long tok = index_at(a.tokens, a.i64, r);
     if (tok < 0) {

@@ -915,3 +915,18 @@ def test_a_written_out_is_known_to_autograd():
         assert call(kept) is kept
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             y.backward()
+
+
+def test_logprobs_of_as_many_rows_as_31_bits_count():
+    """One row of logits, repeated 2^31 - 1 times, nearly all padding: workgroups take a row every 2^20, and the last ones' next would be 2^31 and more."""
+    import torch
+    n = 2 ** 31 - 1
+    rows = [0, 1, 2 ** 20, 2 ** 30 + 7, n - 2 ** 20 - 1, n - 2 ** 20, n - 1]
+    x = np.array([[0.25, -1.5, 3.0]])
+    tokens = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    tokens[rows] = torch.arange(len(rows), dtype=torch.int32, device="cuda") % 3
+    got = ap().april_logprobs(f32(x).expand(n, 3), tokens)
+    want = tr.logprobs(np.repeat(x, len(rows), 0), host(tokens[rows]))[0]
+    near(host(got.logprob[rows]), want, U * (2 * np.log(3) + 3 + 48) + 4 * U * 5)
+    assert int(torch.count_nonzero(got.logprob)) == len(rows)
+    assert int(torch.count_nonzero(got.norm[:, 0])) == len(rows)
