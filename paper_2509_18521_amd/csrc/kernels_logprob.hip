@@ -542,11 +542,12 @@ constexpr int GRAD_THREADS = 256, GRAD_VECS = 4;
 
 template <typename T, bool ENT>
 struct GradRow {
-  float m, c2, l2, q, hl, add;
-  // d logits = p * (q + hl * log2 p), and `add` at the token.  (p is 0 long before log2 p is -1024, and hl * 1024 is finite for any gradient that a sum of them could be)
-  __device__ __forceinline__ float operator()(float x) const {
+  float m, c2, l2, q, hl, add, inv_t, none;
+  // d logits = (p * (q + hl * log2 p) + `add` at the token) / T.  The temperature comes last: gradients over a small one may be infinite, their difference and their product with a p of 0 are not.
+  // Where p is 0, log2 p may be -infinity: `none`, which is 0 for finite gradients.  (A p above 0 keeps hl * log2 p finite for gradients of the entropy up to 3e36.)
+  __device__ __forceinline__ float operator()(float x, float at_token = 0.f) const {
     const float lp = (x - m) * c2 - l2, p = __builtin_amdgcn_exp2f(lp);
-    return ENT ? p * fmaf(hl, fmaxf(lp, -1024.f), q) : p * q;
+    return ((p == 0.f ? none : ENT ? p * fmaf(hl, lp, q) : p * q) + at_token) * inv_t;
   }
 };
 
@@ -565,9 +566,9 @@ __global__ __launch_bounds__(GRAD_THREADS) void logprobs_grad_kernel(LogprobsGra
     const float2 norm = reinterpret_cast<const float2*>(a.norm)[r];
     const float g = tok < a.vocab ? (a.g_logprob ? a.g_logprob[r] : 0.f) : NAN, z = a.g_lse ? a.g_lse[r] : 0.f;
     const float h = ENT ? a.g_entropy[r] : 0.f, ent = ENT ? a.entropy[r] : 0.f;
-    const GradRow<T, ENT> f{norm.x, a.c2, norm.y, a.inv_t * (z - g - h * ent), -a.inv_t * h * LN2, a.inv_t * g};
+    const GradRow<T, ENT> f{norm.x, a.c2, norm.y, z - g - h * ent, -h * LN2, g, a.inv_t, 0.f + (g * 0.f + (h * 0.f + z * 0.f))};
     auto single = [&](int i) {
-      const float v = pad ? 0.f : f((float)row[i]) + (i == tok ? f.add : 0.f);
+      const float v = pad ? 0.f : f((float)row[i], i == tok ? f.add : 0.f);
       out[i] = (T)v;
     };
     const Run<T> run(row, a.vocab);
@@ -591,7 +592,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void logprobs_grad_kernel(LogprobsGra
         if (at >= 0 && at < V) {
 #pragma unroll
           for (int i = 0; i < V; ++i)
-            if (i == at) y[i] = (T)(f((float)x[u][i]) + f.add);
+            if (i == at) y[i] = (T)f((float)x[u][i], f.add);
         }
       }
       at_element* place = reinterpret_cast<at_element*>(to + (size_t)v * V);

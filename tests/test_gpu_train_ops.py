@@ -930,3 +930,33 @@ def test_logprobs_of_as_many_rows_as_31_bits_count():
     near(host(got.logprob[rows]), want, U * (2 * np.log(3) + 3 + 48) + 4 * U * 5)
     assert int(torch.count_nonzero(got.logprob)) == len(rows)
     assert int(torch.count_nonzero(got.norm[:, 0])) == len(rows)
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("parts", ["g", "gz", "h", "ghz"])
+@pytest.mark.parametrize("temperature,size", [(1e-36, 1.0), (1e-30, 1e6), (1e-30, 1e12), (5e-39, 5.0)])
+def test_gradients_at_small_temperatures(temperature, size, parts, t):
+    """Gradients that are infinite over the temperature, or nearly: tokens of probability 0 (masked ones, and all but the largest here) have none, certain ones neither."""
+    rng = np.random.default_rng(26)
+    n, vocab = 24, 1003
+    x = np.round(4 * rng.standard_normal((n, vocab)))
+    x[:, 5::9] = -np.inf
+    x[:, 700] = 50.0
+    x[::3, 20] = 50.0                                        # two equal ones
+    tokens = np.where(np.arange(n) % 2, 700, 3)
+    tokens[4] = -1
+    logits = place(x, t)
+    got = ap().april_logprobs(logits, index(tokens, 64), temperature=temperature, entropy=True)
+    temperature = float(np.float32(temperature))
+    g, h, z = (np.float32(size * rng.choice([-1.0, 1.0, 0.5], size=n)) if c in parts else None for c in "ghz")
+    grad = ap().april_logprobs_grad(logits, index(tokens, 64), got, grad_logprob=None if g is None else f32(g), grad_entropy=None if h is None else f32(h),
+                                    grad_lse=None if z is None else f32(z), temperature=temperature)
+    want, terms = tr.logprobs_grad(x, tokens, temperature, *(None if v is None else v.astype(np.float64) for v in (g, h, z)))
+    # probabilities are 0, 1/2 and 1: what is left is a few products and differences, the log of 2, 1 / T, and bf16
+    tol = 16 * U * terms + half(t) * np.abs(want)
+    if h is not None and size / temperature > 1e37:          # (a difference of two equal numbers of that size: what rounding leaves of it may be infinite, too)
+        pair = (np.arange(n) % 3 == 0)[:, None] & (x == 50.0)
+        want, tol, grad = (np.where(pair, 0.0, v) for v in (want, tol, host(grad)))
+        near(grad, want, tol, "gradient")
+    else:
+        near(host(grad), want, tol, "gradient")
