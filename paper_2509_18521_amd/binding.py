@@ -550,6 +550,20 @@ def _differentiable(name):
         _refuse("%s requires a gradient, and the operator has none: call it under torch.no_grad(), or on %s.detach()", name, name)
 
 
+def _duals():
+    """Whether tensors may carry forward-mode tangents now."""
+    if _torch is None:
+        _need_torch()
+    return _torch.autograd.forward_ad._current_level >= 0
+
+
+def _no_tangent(**tensors):
+    """Refuses tensors with a forward-mode tangent, which a result would be without: its derivative would be zero in silence."""
+    for name, t in tensors.items():
+        if t is not None and _torch.autograd.forward_ad.unpack_dual(t).tangent is not None:
+            _refuse("%s has a tangent, and the operator has no forward-mode derivative: call it on torch.autograd.forward_ad.unpack_dual(%s).primal", name, name)
+
+
 def _gpu(name, t):
     dev = t.get_device()
     if dev < 0:
@@ -635,6 +649,8 @@ def april_cache_append(pool, k, v, slot_map, k_values=None, v_values=None) -> No
         _differentiable("k_values")
     if v_values is not None and v_values.requires_grad:
         _differentiable("v_values")
+    if _duals():
+        _no_tangent(k=k, v=v, k_values=k_values, v_values=v_values)
     p, pages, heads, dh, dev = _pool(pool)
     t = k.dtype
     if t is not _torch.bfloat16 and t is not _torch.float32:
@@ -663,6 +679,8 @@ def april_cache_attention(q, pool, block_table, lens, max_len: int, *, q_start=N
         _differentiable("out")
     if lse is not None and lse.requires_grad:
         _differentiable("lse")
+    if _duals():
+        _no_tangent(q=q, out=out, lse=lse)
     p, pages, heads, dh, dev = _pool(pool)
     bf16, i32 = _torch.bfloat16, _torch.int32
     shape = q.shape
@@ -690,8 +708,9 @@ def april_cache_attention(q, pool, block_table, lens, max_len: int, *, q_start=N
 # ---------------------------------------------------------------------------
 # Operators that score rollouts and train on them, on torch tensors of one GPU, each with its gradient: where autograd would record one of
 # logits, table, x, packed or weights, the result carries it, else the call is the library's alone.  They run on torch's current stream and may
-# be captured into a graph.  What torch itself asks of a captured backward pass holds here too: no autograd graph of the
-# same leaf tensors that was recorded outside the capture may be alive meanwhile.  The gradients' own calls (april_*_grad) have no such bound.
+# be captured into a graph.  Forward-mode derivatives there are none: a tensor with a tangent is refused.  What torch itself asks of a captured
+# backward pass holds here too: no autograd graph of the same leaf tensors that was recorded outside the capture may be alive meanwhile.  The
+# gradients' own calls (april_*_grad) have no such bound.
 # ---------------------------------------------------------------------------
 class Logprobs(NamedTuple):
     """What april_logprobs leaves, see april.h (None: not asked for)."""
@@ -750,17 +769,19 @@ def _two(name, t):
     return t.shape
 
 
-def _records(*tensors):
-    """Whether autograd would record a gradient of one of them."""
-    for t in tensors:
+def _records(**tensors):
+    """Whether autograd would record a gradient of one of them (one with a tangent is refused)."""
+    if _duals():
+        _no_tangent(**tensors)
+    for t in tensors.values():
         if t is not None and t.requires_grad:
-            if _torch is None:
-                _need_torch()
             return _torch.is_grad_enabled()
     return False
 
 
 def _no_gradient(**tensors):
+    if _duals():
+        _no_tangent(**tensors)
     for name, t in tensors.items():
         if t is not None and t.requires_grad:
             _differentiable(name)
@@ -802,6 +823,8 @@ def _function(name):
             def backward(ctx, g, h, z, *_):
                 if g is None and h is None and z is None:
                     return (None,) * 6
+                if _duals():
+                    _no_tangent(grad_logprob=g, grad_entropy=h, grad_lse=z)
                 logits, tokens, norm, entropy = ctx.saved_tensors
                 return _logprobs_grad(logits, tokens, norm, None if h is None else entropy, whole(g), whole(h), whole(z), ctx.temperature), None, None, None, None, None
 
@@ -827,6 +850,8 @@ def _function(name):
             @staticmethod
             @once
             def backward(ctx, g):
+                if _duals():
+                    _no_tangent(grad_out=g)
                 position, = ctx.saved_tensors
                 return _combine(adjacent(g), position, None, None), None, None
 
@@ -839,6 +864,8 @@ def _function(name):
             @staticmethod
             @once
             def backward(ctx, g):
+                if _duals():
+                    _no_tangent(grad_out=g)
                 packed, source, position, weights = ctx.saved_tensors
                 of_packed, _, _, of_weights = ctx.needs_input_grad
                 of_packed, of_weights = _combine_grad(adjacent(g), packed, source, position, weights, of_packed, of_weights)
@@ -872,7 +899,7 @@ def april_logprobs(logits, tokens, *, temperature: float = 1.0, entropy: bool = 
     """log softmax(logits / temperature)[token] of each row of logits [n_rows, vocab] (bf16 or fp32), tokens [n_rows] (int32 or int64; below zero: a
     padding row, zeros), and as asked for the entropy, the log of the sum of exponentials, and the `top` (at most 64) most likely tokens with their
     log-probabilities.  Differentiable: logprob, entropy, lse."""
-    if _records(logits):
+    if _records(logits=logits):
         return Logprobs(*_function("logprobs").apply(logits, tokens, temperature, entropy, lse, top))
     return _logprobs(logits, tokens, temperature, entropy, lse, top)
 
@@ -931,7 +958,7 @@ def _embed(table, tokens, scale, dtype, out):
 def april_embed(table, tokens, *, scale: float = 1.0, dtype=None, out=None):
     """scale * table[tokens] [n_rows, d] (bf16 or fp32, as dtype or out says; else of the table's type) for tokens [n_rows] (int32 or int64; below zero:
     padding, zeros).  Differentiable in the table, but not into an `out`."""
-    if _records(table, out):
+    if _records(table=table, out=out):
         if out is not None:
             _differentiable("table" if table.requires_grad else "out")
         return _function("embed").apply(table, tokens, scale, dtype)
@@ -1007,7 +1034,7 @@ def _expert_gather(x, source, position, out):
 def april_expert_gather(x, rows: ExpertRows, *, out=None):
     """The tokens' rows x [n_rows, d] (bf16 or fp32) in the order of their experts; packed rows of no assignment are zeros.  Differentiable in x, but not
     into an `out`."""
-    if _records(x, out):
+    if _records(x=x, out=out):
         if out is not None:
             _differentiable("x" if x.requires_grad else "out")
         return _function("gather").apply(x, rows.source, rows.position)
@@ -1040,7 +1067,7 @@ def _expert_combine(packed, source, position, weights, out):
 def april_expert_combine(packed, rows: ExpertRows, weights=None, *, out=None):
     """What the experts made of their rows, packed [source.shape[0], d] (bf16 or fp32), summed for each token by weights [n_rows, k] (fp32; None: 1), in the order
     of the token's experts.  Differentiable in packed and weights, but not into an `out`."""
-    if _records(packed, weights, out):
+    if _records(packed=packed, weights=weights, out=out):
         if out is not None:
             _differentiable("packed" if packed.requires_grad else "weights" if weights is not None and weights.requires_grad else "out")
         return _function("combine").apply(packed, rows.source, rows.position, weights)

@@ -960,3 +960,20 @@ def test_gradients_at_small_temperatures(temperature, size, parts, t):
         near(grad, want, tol, "gradient")
     else:
         near(host(grad), want, tol, "gradient")
+
+
+def test_no_tangent_is_lost_in_a_backward_pass():
+    """Forward mode over a recorded backward pass: refused where a tangent reaches it, right where none does."""
+    import torch
+    import torch.autograd.forward_ad as fw
+    x, t, rows = f32(np.ones((4, 8))), index([1, 0, 2, -1], 64), ap().april_expert_sort(index([[0], [1], [1], [0]], 32), 2)
+    w = f32(np.ones((4, 1)))
+    for call in (lambda v: ap().april_logprobs(v, t).logprob, lambda v: ap().april_embed(v, t), lambda v: ap().april_expert_gather(v, rows), lambda v: ap().april_expert_combine(v, rows, w)):
+        leaf = x.clone().requires_grad_()
+        y = call(leaf)
+        with fw.dual_level():
+            dual = fw.make_dual(torch.ones_like(y), torch.ones_like(y))
+            with pytest.raises(Exception, match="has a tangent"):
+                torch.autograd.grad((y * dual).sum(), leaf, retain_graph=True)
+            (g,) = torch.autograd.grad(y.sum(), leaf)
+            assert fw.unpack_dual(g).tangent is None and g.shape == x.shape

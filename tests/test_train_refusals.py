@@ -127,3 +127,38 @@ def test_python_refusals():
                  lambda: ap.april_expert_gather(y, rows, out=x), lambda: ap.april_expert_combine(x, rows, out=y), lambda: ap.april_expert_combine_grad(x, y, rows)):
         with pytest.raises(ap.AprilError, match="requires a gradient"):
             call()
+
+
+def test_forward_mode_derivatives_are_refused_and_not_silently_zero():
+    """A dual tensor requires no gradient and has an address: its tangent would be lost."""
+    import torch
+    import torch.autograd.forward_ad as fw
+    t, c = torch.zeros(3, dtype=torch.int64), torch.zeros((3, 8))
+    made = ap.Logprobs(None, None, None, None, None, torch.zeros((3, 2)))
+    rows = ap.ExpertRows(torch.zeros(3, dtype=torch.int32), torch.zeros(6, dtype=torch.int32), torch.zeros((3, 2), dtype=torch.int32))
+    bf16, pool = torch.bfloat16, torch.zeros((2, 2, 544), dtype=torch.uint8)
+    q, table, lens = torch.zeros((3, 2, 32), dtype=bf16), torch.zeros((3, 4), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    with fw.dual_level():
+        x, w, d = (fw.make_dual(v, torch.ones_like(v)) for v in (c, torch.zeros((3, 2)), q))
+        y = fw.make_dual(c.clone().requires_grad_(), torch.ones_like(c))
+        g = fw.make_dual(torch.zeros(3), torch.ones(3))
+        calls = [("logits", lambda: ap.april_logprobs(x, t)), ("logits", lambda: ap.april_logprobs(y, t)), ("table", lambda: ap.april_embed(x, t)), ("out", lambda: ap.april_embed(c, t, out=x)),
+                 ("x", lambda: ap.april_expert_gather(x, rows)), ("out", lambda: ap.april_expert_gather(c, rows, out=x)), ("packed", lambda: ap.april_expert_combine(x, rows)),
+                 ("weights", lambda: ap.april_expert_combine(c, rows, w)), ("out", lambda: ap.april_expert_combine(c, rows, out=x)),
+                 ("logits", lambda: ap.april_logprobs_grad(x, t, made)), ("grad_logprob", lambda: ap.april_logprobs_grad(c, t, made, grad_logprob=g)),
+                 ("grad_entropy", lambda: ap.april_logprobs_grad(c, t, made, grad_entropy=g)), ("grad_lse", lambda: ap.april_logprobs_grad(c, t, made, grad_lse=g)),
+                 ("out", lambda: ap.april_logprobs_grad(c, t, made, out=x)), ("grad_out", lambda: ap.april_embed_grad(x, t, 5)), ("out", lambda: ap.april_embed_grad(c, t, 5, out=x)),
+                 ("grad_out", lambda: ap.april_expert_combine_grad(x, c, rows)), ("packed", lambda: ap.april_expert_combine_grad(c, x, rows)),
+                 ("weights", lambda: ap.april_expert_combine_grad(c, c, rows, w)),
+                 ("q", lambda: ap.april_cache_attention(d, pool, table, lens, 60)), ("out", lambda: ap.april_cache_attention(q, pool, table, lens, 60, out=d)),
+                 ("lse", lambda: ap.april_cache_attention(q, pool, table, lens, 60, lse=w)), ("k", lambda: ap.april_cache_append(pool, d, q, t)),
+                 ("v", lambda: ap.april_cache_append(pool, q, d, t)), ("k_values", lambda: ap.april_cache_append(pool, q, q, t, k_values=d)),
+                 ("v_values", lambda: ap.april_cache_append(pool, q, q, t, v_values=d))]
+        for name, call in calls:
+            for on in (torch.enable_grad, torch.no_grad):
+                with on(), pytest.raises(ap.AprilError, match="^april error -1: %s has a tangent" % name):
+                    call()
+        with pytest.raises(ap.AprilError, match="not on a GPU"):        # a tensor without one goes on
+            ap.april_logprobs(c, t)
+        with pytest.raises(ap.AprilError, match="not on a GPU"):
+            ap.april_logprobs(fw.unpack_dual(x).primal, t)
