@@ -801,7 +801,7 @@ def _space(call, pack, fields, device):
 
 
 def _function(name):
-    """autograd's class of an operator."""
+    """autograd's class of an operator.  (A backward pass checks what it gets back of its tensors: hooks for saved ones may return others.)"""
     if not _functions:
         t = _torch
         once = t.autograd.function.once_differentiable
@@ -905,14 +905,15 @@ def april_logprobs(logits, tokens, *, temperature: float = 1.0, entropy: bool = 
 
 
 def _logprobs_grad(logits, tokens, norm, entropy, g, h, z, temperature, out=None):
-    """(The arguments are checked.)"""
-    n, vocab = logits.shape
+    n, vocab = _two("logits", logits)
+    dev, dtype = _gpu("logits", logits), _dtype("logits", logits.dtype)
+    p, row = _matrix("logits", logits, logits.dtype, (n, vocab), dev)
+    tp, bits = _index("tokens", tokens, (n,), dev)
     if out is None:
         out = _torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
-    ptr = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
-    _enqueue(_call("april_logprobs_grad"), logits.get_device(), _PACK_LOGPROBS_GRAD, n, vocab, APRIL_DTYPE_FP32 if logits.dtype is _torch.float32 else APRIL_DTYPE_BF16,
-             64 if tokens.dtype is _torch.int64 else 32, temperature, 0, logits.stride(0), out.stride(0), logits.data_ptr(), tokens.data_ptr(), norm.data_ptr(), ptr(entropy),
-             ptr(g), ptr(h), ptr(z), out.data_ptr())
+    op, o_row = _matrix("out", out, logits.dtype, (n, vocab), dev)
+    _enqueue(_call("april_logprobs_grad"), dev, _PACK_LOGPROBS_GRAD, n, vocab, dtype, bits, temperature, 0, row, o_row, p, tp, _float_ptr("made.norm", norm, (n, 2), dev),
+             _float_ptr("made.entropy", entropy, (n,), dev), _float_ptr("grad_logprob", g, (n,), dev), _float_ptr("grad_entropy", h, (n,), dev), _float_ptr("grad_lse", z, (n,), dev), op)
     return out
 
 
@@ -920,20 +921,9 @@ def april_logprobs_grad(logits, tokens, made: Logprobs, *, grad_logprob=None, gr
     """Gradient of the logits, of their type.  made: april_logprobs' of the same arguments (its norm, and its entropy for grad_entropy); grad_*
     [n_rows]: fp32, None is zero.  out may be the logits themselves, which are then overwritten.  Not differentiable."""
     _no_gradient(logits=logits, grad_logprob=grad_logprob, grad_entropy=grad_entropy, grad_lse=grad_lse, out=out)
-    n, vocab = _two("logits", logits)
-    dev = _gpu("logits", logits)
-    _dtype("logits", logits.dtype)
-    _matrix("logits", logits, logits.dtype, (n, vocab), dev)
-    _index("tokens", tokens, (n,), dev)
-    if out is not None:
-        _matrix("out", out, logits.dtype, (n, vocab), dev)
     if grad_entropy is not None and made.entropy is None:
         _refuse("grad_entropy: april_logprobs was not asked for the entropy")
-    _float_ptr("made.norm", made.norm, (n, 2), dev)
-    entropy = None if grad_entropy is None else made.entropy
-    for name, t in (("made.entropy", entropy), ("grad_logprob", grad_logprob), ("grad_entropy", grad_entropy), ("grad_lse", grad_lse)):
-        _float_ptr(name, t, (n,), dev)
-    got = _logprobs_grad(logits, tokens, made.norm, entropy, grad_logprob, grad_entropy, grad_lse, temperature, out)
+    got = _logprobs_grad(logits, tokens, made.norm, None if grad_entropy is None else made.entropy, grad_logprob, grad_entropy, grad_lse, temperature, out)
     return got if out is None else _wrote(out)
 
 
@@ -1008,26 +998,30 @@ def april_expert_sort(ids, n_experts: int, *, align: int = 1) -> ExpertRows:
     return rows
 
 
-def _expert_sizes(source, position, dev):
-    """(rows, experts of a row, packed rows)."""
-    n, k = _two("rows.position", position)
+def _packed_rows(source, dev):
+    """(pointer, packed rows)."""
     if len(source.shape) != 1:
         _refuse("rows.source: one dimension wanted")
     m = source.shape[0]
-    _ptr("rows.source", source, _torch.int32, (m,), dev)
-    _ptr("rows.position", position, _torch.int32, (n, k), dev)
-    return n, k, m
+    return _ptr("rows.source", source, _torch.int32, (m,), dev), m
+
+
+def _positions(position, dev):
+    """(pointer, rows, experts of a row)."""
+    n, k = _two("rows.position", position)
+    return _ptr("rows.position", position, _torch.int32, (n, k), dev), n, k
 
 
 def _expert_gather(x, source, position, out):
     d = _two("x", x)[1]
     dev, dtype = _gpu("x", x), _dtype("x", x.dtype)
-    n, k, m = _expert_sizes(source, position, dev)
+    sp, m = _packed_rows(source, dev)
+    at, n, k = _positions(position, dev)
     if out is None:
         out = _torch.empty((m, d), dtype=x.dtype, device=x.device)
     p, row = _matrix("x", x, x.dtype, (n, d), dev)
     op, o_row = _matrix("out", out, x.dtype, (m, d), dev)
-    _enqueue(_call("april_expert_gather"), dev, _PACK_EXPERT_GATHER, n, k, d, m, dtype, 0, row, o_row, p, source.data_ptr(), position.data_ptr(), op)
+    _enqueue(_call("april_expert_gather"), dev, _PACK_EXPERT_GATHER, n, k, d, m, dtype, 0, row, o_row, p, sp, at, op)
     return out
 
 
@@ -1043,24 +1037,21 @@ def april_expert_gather(x, rows: ExpertRows, *, out=None):
 
 
 def _combine(packed, position, weights, out):
-    """(The arguments are checked.)"""
-    (m, d), (n, k) = packed.shape, position.shape
+    m, d = _two("packed", packed)
+    dev, dtype = _gpu("packed", packed), _dtype("packed", packed.dtype)
+    at, n, k = _positions(position, dev)
     if out is None:
         out = _torch.empty((n, d), dtype=packed.dtype, device=packed.device)
-    _enqueue(_call("april_expert_combine"), packed.get_device(), _PACK_EXPERT_COMBINE, n, k, d, m, APRIL_DTYPE_FP32 if packed.dtype is _torch.float32 else APRIL_DTYPE_BF16, 0,
-             packed.stride(0), out.stride(0), packed.data_ptr(), position.data_ptr(), 0 if weights is None else weights.data_ptr(), out.data_ptr())
+    p, row = _matrix("packed", packed, packed.dtype, (m, d), dev)
+    op, o_row = _matrix("out", out, packed.dtype, (n, d), dev)
+    _enqueue(_call("april_expert_combine"), dev, _PACK_EXPERT_COMBINE, n, k, d, m, dtype, 0, row, o_row, p, at, _float_ptr("weights", weights, (n, k), dev), op)
     return out
 
 
 def _expert_combine(packed, source, position, weights, out):
-    d = _two("packed", packed)[1]
     dev = _gpu("packed", packed)
-    _dtype("packed", packed.dtype)
-    n, k, m = _expert_sizes(source, position, dev)
-    _matrix("packed", packed, packed.dtype, (m, d), dev)
-    if out is not None:
-        _matrix("out", out, packed.dtype, (n, d), dev)
-    _float_ptr("weights", weights, (n, k), dev)
+    if packed.shape[0] != _packed_rows(source, dev)[1]:
+        _refuse("packed: %d rows wanted, not %d", source.shape[0], packed.shape[0])
     return _combine(packed, position, weights, out)
 
 
@@ -1076,26 +1067,23 @@ def april_expert_combine(packed, rows: ExpertRows, weights=None, *, out=None):
 
 
 def _combine_grad(grad_out, packed, source, position, weights, of_packed, of_weights):
-    """(The arguments are checked.)"""
-    (m, d), (n, k) = packed.shape, position.shape
+    d = _two("grad_out", grad_out)[1]
+    dev, dtype = _gpu("grad_out", grad_out), _dtype("grad_out", grad_out.dtype)
+    sp, m = _packed_rows(source, dev)
+    at, n, k = _positions(position, dev)
+    g, row = _matrix("grad_out", grad_out, grad_out.dtype, (n, d), dev)
+    p, p_row = _matrix("packed", packed, grad_out.dtype, (m, d), dev)
+    wp = _float_ptr("weights", weights, (n, k), dev)
     g_packed = _torch.empty((m, d), dtype=packed.dtype, device=packed.device) if of_packed else None
     g_weights = _torch.empty((n, k), dtype=_torch.float32, device=packed.device) if of_weights else None
-    _enqueue(_call("april_expert_combine_grad"), packed.get_device(), _PACK_EXPERT_COMBINE_GRAD, n, k, d, m,
-             APRIL_DTYPE_FP32 if packed.dtype is _torch.float32 else APRIL_DTYPE_BF16, 0, grad_out.stride(0), packed.stride(0), d, grad_out.data_ptr(), packed.data_ptr(),
-             source.data_ptr(), position.data_ptr(), 0 if weights is None else weights.data_ptr(), g_packed.data_ptr() if of_packed else 0, g_weights.data_ptr() if of_weights else 0)
+    _enqueue(_call("april_expert_combine_grad"), dev, _PACK_EXPERT_COMBINE_GRAD, n, k, d, m, dtype, 0, row, p_row, d, g, p, sp, at, wp,
+             g_packed.data_ptr() if of_packed else 0, g_weights.data_ptr() if of_weights else 0)
     return g_packed, g_weights
 
 
 def april_expert_combine_grad(grad_out, packed, rows: ExpertRows, weights=None, *, of_packed: bool = True, of_weights: bool = True):
     """(gradient of packed, gradient of weights) for the gradient [n_rows, d] of april_expert_combine's result; None where not asked for.  Not differentiable."""
     _no_gradient(grad_out=grad_out, packed=packed, weights=weights)
-    d = _two("grad_out", grad_out)[1]
-    dev = _gpu("grad_out", grad_out)
-    _dtype("grad_out", grad_out.dtype)
-    n, k, m = _expert_sizes(rows.source, rows.position, dev)
-    _matrix("grad_out", grad_out, grad_out.dtype, (n, d), dev)
-    _matrix("packed", packed, grad_out.dtype, (m, d), dev)
-    _float_ptr("weights", weights, (n, k), dev)
     return _combine_grad(grad_out, packed, rows.source, rows.position, weights, of_packed, of_weights)
 
 

@@ -977,3 +977,50 @@ def test_no_tangent_is_lost_in_a_backward_pass():
                 torch.autograd.grad((y * dual).sum(), leaf, retain_graph=True)
             (g,) = torch.autograd.grad(y.sum(), leaf)
             assert fw.unpack_dual(g).tangent is None and g.shape == x.shape
+
+
+def test_saved_tensors_are_checked_again():
+    """Hooks for saved tensors may give back others than were kept.  Those that serve are read as they are; other types, layouts, places or sizes are refused."""
+    import torch
+    rng = np.random.default_rng(27)
+    n, d, e, k = 12, 16, 4, 2
+    t, ids = index(rng.integers(0, d, size=n), 64), index(rng.integers(0, e, size=(n, k)), 32)
+    rows, x, w = ap().april_expert_sort(ids, e, align=4), f32(rng.standard_normal((n, d))), f32(rng.random((n, k)))
+    y, table, g = f32(rng.standard_normal((rows.source.shape[0], d))), f32(rng.standard_normal((d, 6))), f32(rng.standard_normal(n))
+
+    def wide(v):
+        """The same values in rows that lie apart (a matrix of floats; as they are, others)."""
+        return torch.stack([v, v], 1).view(2 * v.shape[0], v.shape[1])[::2] if v.dim() == 2 and v.shape[1] == d else v
+
+    def float16(v):
+        return v.half() if v.is_floating_point() else v
+
+    def turned(v):
+        return v.t().contiguous().t() if v.dim() == 2 else v.repeat_interleave(2)[::2]
+
+    def away(v):
+        return v.cpu()
+
+    def fewer(v):
+        return v[:-1].contiguous()
+
+    def counted(v):
+        return v if v.is_floating_point() else v.short()
+
+    def grads(leaves, call, hook):
+        leaves = [v.clone().requires_grad_() for v in leaves]
+        with torch.autograd.graph.saved_tensors_hooks(lambda v: v, hook):
+            got = call(*leaves)
+        return torch.autograd.grad(got, leaves, [(g if v.dim() == 1 else g[:, None]).expand(v.shape) if v.shape[0] == n else torch.ones_like(v) for v in got])
+
+    def scored(v):
+        got = ap().april_logprobs(v, t, entropy=True)
+        return got.logprob, got.entropy
+    for leaves, call, kinds in (((x,), scored, (float16, turned, away, fewer, counted)), ((table,), lambda v: (ap().april_embed(v, t),), (turned, away, fewer, counted)),
+                                ((x,), lambda v: (ap().april_expert_gather(v, rows),), (turned, away, fewer, counted)),
+                                ((y, w), lambda v, u: (ap().april_expert_combine(v, rows, u),), (float16, turned, away, fewer, counted))):
+        for a, b in zip(grads(leaves, call, wide), grads(leaves, call, lambda v: v)):
+            assert torch.equal(a, b)
+        for hook in kinds:
+            with pytest.raises(RuntimeError):                # (fewer rows of positions: torch refuses the gradient's shape, else the operator)
+                grads(leaves, call, hook)
