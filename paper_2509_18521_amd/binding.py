@@ -858,7 +858,8 @@ def _function(name):
         class AprilExpertCombine(t.autograd.Function):
             @staticmethod
             def forward(ctx, packed, source, position, weights):
-                ctx.save_for_backward(packed, source, position, weights)
+                # (the values of packed matter to the weights' gradient alone)
+                ctx.save_for_backward(packed if ctx.needs_input_grad[3] else None, source, position, weights)
                 return _expert_combine(packed, source, position, weights, None)
 
             @staticmethod
@@ -1067,15 +1068,16 @@ def april_expert_combine(packed, rows: ExpertRows, weights=None, *, out=None):
 
 
 def _combine_grad(grad_out, packed, source, position, weights, of_packed, of_weights):
+    """(packed may be None where of_weights is false.)"""
     d = _two("grad_out", grad_out)[1]
     dev, dtype = _gpu("grad_out", grad_out), _dtype("grad_out", grad_out.dtype)
     sp, m = _packed_rows(source, dev)
     at, n, k = _positions(position, dev)
     g, row = _matrix("grad_out", grad_out, grad_out.dtype, (n, d), dev)
-    p, p_row = _matrix("packed", packed, grad_out.dtype, (m, d), dev)
+    p, p_row = (0, 0) if packed is None else _matrix("packed", packed, grad_out.dtype, (m, d), dev)
     wp = _float_ptr("weights", weights, (n, k), dev)
-    g_packed = _torch.empty((m, d), dtype=packed.dtype, device=packed.device) if of_packed else None
-    g_weights = _torch.empty((n, k), dtype=_torch.float32, device=packed.device) if of_weights else None
+    g_packed = _torch.empty((m, d), dtype=grad_out.dtype, device=grad_out.device) if of_packed else None
+    g_weights = _torch.empty((n, k), dtype=_torch.float32, device=grad_out.device) if of_weights else None
     _enqueue(_call("april_expert_combine_grad"), dev, _PACK_EXPERT_COMBINE_GRAD, n, k, d, m, dtype, 0, row, p_row, d, g, p, sp, at, wp,
              g_packed.data_ptr() if of_packed else 0, g_weights.data_ptr() if of_weights else 0)
     return g_packed, g_weights

@@ -1024,3 +1024,30 @@ def test_saved_tensors_are_checked_again():
         for hook in kinds:
             with pytest.raises(RuntimeError):                # (fewer rows of positions: torch refuses the gradient's shape, else the operator)
                 grads(leaves, call, hook)
+
+
+@pytest.mark.parametrize("weighted", [False, True])
+def test_packed_rows_are_kept_for_the_weights_gradient_alone(weighted):
+    """Without a gradient of the weights, what the experts made is not held until the backward pass and may be overwritten."""
+    import torch
+    rng = np.random.default_rng(28)
+    n, k, e, d = 30, 2, 5, 24
+    rows = ap().april_expert_sort(index(expert_ids(rng, n, k, e, True), 32), e, align=4)
+    w = f32(rng.random((n, k))) if weighted else None
+    base, g = f32(rng.standard_normal((rows.source.shape[0], d))).requires_grad_(), f32(rng.standard_normal((n, d)))
+    kept = []
+    packed = base * 2.0
+    with torch.autograd.graph.saved_tensors_hooks(lambda v: kept.append(v.data_ptr()) or v, lambda v: v):
+        out = ap().april_expert_combine(packed, rows, w)
+    assert packed.data_ptr() not in kept
+    with torch.no_grad():
+        packed.fill_(float("nan"))
+    (got,) = torch.autograd.grad(out, base, g)
+    want, none = ap().april_expert_combine_grad(g, torch.zeros_like(base), rows, w, of_weights=False)
+    assert none is None and torch.equal(got, want * 2.0)
+    u = f32(rng.random((n, k))).requires_grad_()
+    packed = base.detach() * 2.0
+    out = ap().april_expert_combine(packed, rows, u)
+    packed.zero_()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
