@@ -81,3 +81,25 @@ def test_a_prompt_of_nan_leaves_the_others_alone(experts, top_k, n):
             assert np.isnan(rows[1][rid, i]).all(), i
         else:
             assert np.array_equal(row, rows[1][rid, i]), (rid, i)
+
+
+def test_the_sort_and_the_one_workgroup_dispatch_give_the_same_bits():
+    """The same prompts in a prefill of 4018 assignments, which one workgroup dispatches, and of 4100, which are sorted: experts' rows lie otherwise in their batches, nothing else differs."""
+    import paper_2509_18521_amd as ap
+    shape = ai.ModelShape(2, 128, 4, 2, 32, 0, 512, n_experts=32, experts_per_tok=2, d_expert_ffn=64)
+    rows = []
+    for n in (49, 50):
+        w = ai.Workload("moe_border", shape, 50, 41, n, n, 2, 1.0, 0.1, 2, 2, ai.SAMPLER_GREEDY, 0, 1, 41)
+        reqs = ai.make_requests(w, n)
+        tokens = class_forced_tokens(w, 50)
+        ctx = make_engine(w, ai.make_weights(shape, w.seed), debug=True, max_inflight=60)
+        try:
+            for r in reqs:
+                ap.april_debug_watch(ctx, r.request_id, 0, 2)
+            run_gpu(ctx, reqs, n, n, 2, 1, forced={r.request_id: tokens[r.request_id][:2] for r in reqs})
+            rows.append({r.request_id: ap.april_debug_logits(ctx, r.request_id, 0, 512)[0] for r in reqs})
+        finally:
+            ap.april_destroy(ctx)
+    assert len(rows[0]) == 49
+    for rid, row in rows[0].items():
+        assert np.isfinite(row).all() and np.array_equal(row, rows[1][rid]), rid

@@ -1051,3 +1051,60 @@ def test_packed_rows_are_kept_for_the_weights_gradient_alone(weighted):
     packed.zero_()
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         out.sum().backward()
+
+
+STREAMED = [("bf16", 135000, 1000, 64, 0), ("bf16", 15001, 9001, 64, 20), ("bf16", 6800, 20000, 256, 0), ("bf16", 6803, 20001, 256, 40), ("bf16", 1950, 70000, 512, 9),
+            ("f32", 75000, 900, 64, 0), ("f32", 13501, 5001, 64, 20), ("f32", 3400, 20000, 256, 5), ("f32", 1700, 40000, 512, 0), ("f32", 1701, 40001, 512, 30)]
+
+
+@pytest.mark.parametrize("t,n,vocab,threads,top", STREAMED)
+def test_logprobs_and_gradient_of_arrays_past_the_last_cache(t, n, vocab, threads, top):
+    """Logits of more than 256 MB, whose accesses are streamed, in workgroups of 64, 256 and 512 threads: 48 rows against the plain form, the others copies of them, with the same bits at like
+    addresses.
+
+    A thread adds up V / threads exponentials one after another, and goes over to a new reference at most once for every 32 of them, two roundings each; 6 additions join a wavefront, threads / 64
+    those."""
+    import torch
+    assert n * vocab * (2 if t == "f32" else 1) > 128 << 20
+    rng = np.random.default_rng([n, vocab, top])
+    few = place(hard_logits(rng, 48, vocab, t), t)
+    tokens = rng.integers(0, vocab, size=48)
+    tokens[[5, 30]] = -1, vocab
+    of = rng.integers(0, 48, size=n)
+    of[:48] = np.arange(48)
+    at = torch.as_tensor(of).cuda()
+    logits, idx = few[at], index(tokens[of], 64)
+    got = ap().april_logprobs(logits, idx, entropy=True, lse=True, top=top)
+    x = host(few)
+    lp, ent, lse, best, ids = tr.logprobs(x, tokens, 1.0, top)
+    chain = vocab / threads * (1 + 2 / 32) + 6 + threads / 64
+    m = np.max(np.where(np.isfinite(x), x, -np.inf), axis=1, keepdims=True)
+    with np.errstate(invalid="ignore", over="ignore"):
+        dist = np.array([(m[r, 0] - x[r, k]) if 0 <= k < vocab else 0.0 for r, k in enumerate(tokens)])
+        base = U * (2 * np.log(vocab) + chain + 48)
+        near(host(got.logprob[:48]), lp, base + 4 * U * np.abs(dist), "logprob")
+        near(host(got.entropy[:48]), ent, base * (2 + np.log(vocab)), "entropy")
+        near(host(got.lse[:48]), lse, base + 4 * U * np.abs(lse), "lse")
+        if top:
+            assert np.array_equal(host(got.top_ids[:48]), ids)
+            near(host(got.top_logprobs[:48]), best, base + 4 * U * np.abs(best), "top")
+    first, per = {}, 8 if t == "bf16" else 4                 # (a row's sums go by its place to a 16-byte border)
+    same = torch.as_tensor([first.setdefault((of[r], r * vocab % per), r) for r in range(n)]).cuda()
+    alike = lambda v: torch.equal(v.nan_to_num(nan=123.0), v[same].nan_to_num(nan=123.0))  # noqa: E731
+    assert all(alike(v) for v in got if v is not None)
+    plain = ap().april_logprobs(logits, idx, top=top)        # (without the entropy's sum: the rest as with it)
+    for a, b in zip(plain, got):
+        assert a is None or torch.equal(a.nan_to_num(nan=123.0), b.nan_to_num(nan=123.0))
+    g, h, z = (rng.standard_normal(48).astype(np.float32) for _ in range(3))
+    finite = np.isfinite(x).any(axis=1) & ~np.isnan(x).any(axis=1) & ~(x == np.inf).any(axis=1)
+    keep = finite | (tokens < 0)
+    with np.errstate(invalid="ignore", over="ignore"):
+        dist = np.minimum(np.abs(np.nan_to_num(m - x, nan=0.0, posinf=0.0, neginf=0.0)), 200.0)
+    for with_entropy in (True, False):
+        want, size = tr.logprobs_grad(x, tokens, 1.0, g.astype(np.float64), h.astype(np.float64) if with_entropy else None, z.astype(np.float64))
+        grad = ap().april_logprobs_grad(logits, idx, got, grad_logprob=f32(g)[at], grad_entropy=f32(h)[at] if with_entropy else None, grad_lse=f32(z)[at])
+        # each term: an exponential of that distance, the forward's log of the sum and entropy, a handful of products
+        rel = U * (6 * dist + 4 * np.log(vocab) + chain + 64) * (3 if with_entropy else 1)
+        tol = size * rel + half(t) * np.abs(want) + 1e-37 * (1 + np.nan_to_num(size)) + (2.0 ** -133 if t == "bf16" else 2.0 ** -149)
+        near(host(grad[:48])[keep], want[keep], tol[keep], "gradient")
+        assert alike(grad) and bool(grad[:48][torch.as_tensor(~keep).cuda()].isnan().all())
