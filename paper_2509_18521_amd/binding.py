@@ -491,12 +491,14 @@ class CacheTables(NamedTuple):
 
 
 _torch = None               # imported by the first of these calls (the engine's calls need none)
+_forward = None             # its forward-mode differentiation
 
 
 def _need_torch():
-    global _torch
+    global _torch, _forward
     import torch
-    _torch = torch
+    import torch.autograd.forward_ad
+    _torch, _forward = torch, torch.autograd.forward_ad
 
 
 def _refuse(text, *args):
@@ -554,13 +556,13 @@ def _duals():
     """Whether tensors may carry forward-mode tangents now."""
     if _torch is None:
         _need_torch()
-    return _torch.autograd.forward_ad._current_level >= 0
+    return _forward._current_level >= 0
 
 
 def _no_tangent(**tensors):
     """Refuses tensors with a forward-mode tangent, which a result would be without: its derivative would be zero in silence."""
     for name, t in tensors.items():
-        if t is not None and _torch.autograd.forward_ad.unpack_dual(t).tangent is not None:
+        if t is not None and _forward.unpack_dual(t).tangent is not None:
             _refuse("%s has a tangent, and the operator has no forward-mode derivative: call it on torch.autograd.forward_ad.unpack_dual(%s).primal", name, name)
 
 
@@ -591,7 +593,7 @@ def _bytes(pack, *fields):
 
 def _enqueue(call, dev, pack, *fields):
     """Call with the fields' struct, the stream that torch works on for GPU `dev` last; that GPU is the current one meanwhile."""
-    if _torch.cuda.current_device() == dev:
+    if _torch._C._cuda_getDevice() == dev:                   # (torch.cuda.current_device() makes sure first that there is a GPU; the tensors are on it)
         return _check(None, call(_bytes(pack, *fields, _torch._C._cuda_getCurrentRawStream(dev))))
     with _torch.cuda.device(dev):
         return _check(None, call(_bytes(pack, *fields, _torch._C._cuda_getCurrentRawStream(dev))))
@@ -750,6 +752,19 @@ def _matrix(name, t, dtype, shape, dev):
     return t.data_ptr(), row
 
 
+def _first(name, t):
+    """(rows, columns, GPU, type, pointer, stride of rows) of a call's first matrix.  (One call: in a backward pass, on a thread of torch's, each costs twice its time.)"""
+    shape, of, dev = t.shape, t.dtype, t.get_device()
+    if len(shape) != 2 or dev < 0:
+        _two(name, t)
+        _gpu(name, t)
+    n, d = shape
+    row, col = t.stride()
+    if col != 1 and d > 1:
+        _refuse("%s: the elements of a row have to be adjacent", name)
+    return n, d, dev, APRIL_DTYPE_BF16 if of is _torch.bfloat16 else _dtype(name, of), t.data_ptr(), row
+
+
 def _index(name, t, shape, dev):
     """(pointer, bits) of a contiguous tensor of int32 or int64."""
     if t.dtype is _torch.int64:
@@ -823,7 +838,7 @@ def _function(name):
             def backward(ctx, g, h, z, *_):
                 if g is None and h is None and z is None:
                     return (None,) * 6
-                if _duals():
+                if _forward._current_level >= 0:
                     _no_tangent(grad_logprob=g, grad_entropy=h, grad_lse=z)
                 logits, tokens, norm, entropy = ctx.saved_tensors
                 return _logprobs_grad(logits, tokens, norm, None if h is None else entropy, whole(g), whole(h), whole(z), ctx.temperature), None, None, None, None, None
@@ -850,7 +865,7 @@ def _function(name):
             @staticmethod
             @once
             def backward(ctx, g):
-                if _duals():
+                if _forward._current_level >= 0:
                     _no_tangent(grad_out=g)
                 position, = ctx.saved_tensors
                 return _combine(adjacent(g), position, None, None), None, None
@@ -865,7 +880,7 @@ def _function(name):
             @staticmethod
             @once
             def backward(ctx, g):
-                if _duals():
+                if _forward._current_level >= 0:
                     _no_tangent(grad_out=g)
                 packed, source, position, weights = ctx.saved_tensors
                 of_packed, _, _, of_weights = ctx.needs_input_grad
@@ -877,11 +892,9 @@ def _function(name):
 
 
 def _logprobs(logits, tokens, temperature, entropy, lse, top):
-    n, vocab = _two("logits", logits)
-    dev, dtype = _gpu("logits", logits), _dtype("logits", logits.dtype)
+    n, vocab, dev, dtype, p, row = _first("logits", logits)
     if top < 0:
         _refuse("top: %d is below zero", top)
-    p, row = _matrix("logits", logits, logits.dtype, (n, vocab), dev)
     tp, bits = _index("tokens", tokens, (n,), dev)
     empty, f32, device = _torch.empty, _torch.float32, logits.device
     logprob, norm = empty(n, dtype=f32, device=device), empty((n, 2), dtype=f32, device=device)
@@ -906,15 +919,19 @@ def april_logprobs(logits, tokens, *, temperature: float = 1.0, entropy: bool = 
 
 
 def _logprobs_grad(logits, tokens, norm, entropy, g, h, z, temperature, out=None):
-    n, vocab = _two("logits", logits)
-    dev, dtype = _gpu("logits", logits), _dtype("logits", logits.dtype)
-    p, row = _matrix("logits", logits, logits.dtype, (n, vocab), dev)
-    tp, bits = _index("tokens", tokens, (n,), dev)
+    """(g, h and z are checked.)"""
+    n, vocab, dev, dtype, p, row = _first("logits", logits)
+    f32, i64 = _torch.float32, _torch.int64
+    wide = tokens.dtype is i64
+    tp, np_ = _ptr("tokens", tokens, i64 if wide else _torch.int32, (n,), dev), _ptr("made.norm", norm, f32, (n, 2), dev)
     if out is None:
         out = _torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
-    op, o_row = _matrix("out", out, logits.dtype, (n, vocab), dev)
-    _enqueue(_call("april_logprobs_grad"), dev, _PACK_LOGPROBS_GRAD, n, vocab, dtype, bits, temperature, 0, row, o_row, p, tp, _float_ptr("made.norm", norm, (n, 2), dev),
-             _float_ptr("made.entropy", entropy, (n,), dev), _float_ptr("grad_logprob", g, (n,), dev), _float_ptr("grad_entropy", h, (n,), dev), _float_ptr("grad_lse", z, (n,), dev), op)
+        op, o_row = out.data_ptr(), vocab
+    else:
+        op, o_row = _matrix("out", out, logits.dtype, (n, vocab), dev)
+    _enqueue(_call("april_logprobs_grad"), dev, _PACK_LOGPROBS_GRAD, n, vocab, dtype, 64 if wide else 32, temperature, 0, row, o_row, p, tp, np_,
+             0 if entropy is None else _ptr("made.entropy", entropy, f32, (n,), dev), 0 if g is None else g.data_ptr(), 0 if h is None else h.data_ptr(),
+             0 if z is None else z.data_ptr(), op)
     return out
 
 
@@ -922,8 +939,11 @@ def april_logprobs_grad(logits, tokens, made: Logprobs, *, grad_logprob=None, gr
     """Gradient of the logits, of their type.  made: april_logprobs' of the same arguments (its norm, and its entropy for grad_entropy); grad_*
     [n_rows]: fp32, None is zero.  out may be the logits themselves, which are then overwritten.  Not differentiable."""
     _no_gradient(logits=logits, grad_logprob=grad_logprob, grad_entropy=grad_entropy, grad_lse=grad_lse, out=out)
+    n, dev = _two("logits", logits)[0], _gpu("logits", logits)
     if grad_entropy is not None and made.entropy is None:
         _refuse("grad_entropy: april_logprobs was not asked for the entropy")
+    for name, t in (("grad_logprob", grad_logprob), ("grad_entropy", grad_entropy), ("grad_lse", grad_lse)):
+        _float_ptr(name, t, (n,), dev)
     got = _logprobs_grad(logits, tokens, made.norm, None if grad_entropy is None else made.entropy, grad_logprob, grad_entropy, grad_lse, temperature, out)
     return got if out is None else _wrote(out)
 
@@ -1009,19 +1029,23 @@ def _packed_rows(source, dev):
 
 def _positions(position, dev):
     """(pointer, rows, experts of a row)."""
-    n, k = _two("rows.position", position)
-    return _ptr("rows.position", position, _torch.int32, (n, k), dev), n, k
+    shape = position.shape
+    if len(shape) != 2:
+        _two("rows.position", position)
+    return (_ptr("rows.position", position, _torch.int32, shape, dev), *shape)
 
 
 def _expert_gather(x, source, position, out):
-    d = _two("x", x)[1]
-    dev, dtype = _gpu("x", x), _dtype("x", x.dtype)
+    rows, d, dev, dtype, p, row = _first("x", x)
     sp, m = _packed_rows(source, dev)
     at, n, k = _positions(position, dev)
+    if rows != n:
+        _refuse("x: %d rows wanted, not %d", n, rows)
     if out is None:
         out = _torch.empty((m, d), dtype=x.dtype, device=x.device)
-    p, row = _matrix("x", x, x.dtype, (n, d), dev)
-    op, o_row = _matrix("out", out, x.dtype, (m, d), dev)
+        op, o_row = out.data_ptr(), d
+    else:
+        op, o_row = _matrix("out", out, x.dtype, (m, d), dev)
     _enqueue(_call("april_expert_gather"), dev, _PACK_EXPERT_GATHER, n, k, d, m, dtype, 0, row, o_row, p, sp, at, op)
     return out
 
@@ -1038,20 +1062,20 @@ def april_expert_gather(x, rows: ExpertRows, *, out=None):
 
 
 def _combine(packed, position, weights, out):
-    m, d = _two("packed", packed)
-    dev, dtype = _gpu("packed", packed), _dtype("packed", packed.dtype)
+    m, d, dev, dtype, p, row = _first("packed", packed)
     at, n, k = _positions(position, dev)
     if out is None:
         out = _torch.empty((n, d), dtype=packed.dtype, device=packed.device)
-    p, row = _matrix("packed", packed, packed.dtype, (m, d), dev)
-    op, o_row = _matrix("out", out, packed.dtype, (n, d), dev)
-    _enqueue(_call("april_expert_combine"), dev, _PACK_EXPERT_COMBINE, n, k, d, m, dtype, 0, row, o_row, p, at, _float_ptr("weights", weights, (n, k), dev), op)
+        op, o_row = out.data_ptr(), d
+    else:
+        op, o_row = _matrix("out", out, packed.dtype, (n, d), dev)
+    _enqueue(_call("april_expert_combine"), dev, _PACK_EXPERT_COMBINE, n, k, d, m, dtype, 0, row, o_row, p, at,
+             0 if weights is None else _ptr("weights", weights, _torch.float32, (n, k), dev), op)
     return out
 
 
 def _expert_combine(packed, source, position, weights, out):
-    dev = _gpu("packed", packed)
-    if packed.shape[0] != _packed_rows(source, dev)[1]:
+    if packed.shape[0] != _packed_rows(source, _gpu("packed", packed))[1]:
         _refuse("packed: %d rows wanted, not %d", source.shape[0], packed.shape[0])
     return _combine(packed, position, weights, out)
 
@@ -1069,13 +1093,13 @@ def april_expert_combine(packed, rows: ExpertRows, weights=None, *, out=None):
 
 def _combine_grad(grad_out, packed, source, position, weights, of_packed, of_weights):
     """(packed may be None where of_weights is false.)"""
-    d = _two("grad_out", grad_out)[1]
-    dev, dtype = _gpu("grad_out", grad_out), _dtype("grad_out", grad_out.dtype)
+    rows, d, dev, dtype, g, row = _first("grad_out", grad_out)
     sp, m = _packed_rows(source, dev)
     at, n, k = _positions(position, dev)
-    g, row = _matrix("grad_out", grad_out, grad_out.dtype, (n, d), dev)
+    if rows != n:
+        _refuse("grad_out: %d rows wanted, not %d", n, rows)
     p, p_row = (0, 0) if packed is None else _matrix("packed", packed, grad_out.dtype, (m, d), dev)
-    wp = _float_ptr("weights", weights, (n, k), dev)
+    wp = 0 if weights is None else _ptr("weights", weights, _torch.float32, (n, k), dev)
     g_packed = _torch.empty((m, d), dtype=grad_out.dtype, device=grad_out.device) if of_packed else None
     g_weights = _torch.empty((n, k), dtype=_torch.float32, device=grad_out.device) if of_weights else None
     _enqueue(_call("april_expert_combine_grad"), dev, _PACK_EXPERT_COMBINE_GRAD, n, k, d, m, dtype, 0, row, p_row, d, g, p, sp, at, wp,
