@@ -773,7 +773,7 @@ void forward(april_ctx* c, RowCtx rows, RowCtx srows, const int* gather, double 
       const bool moe_tiled = tile && c->moe_tile;
       const int tall = moe_tiled ? 1 : c->moe_tall_rows;
       const int n_groups = moe_group_count(rows.max_rows, tk, E, moe_tile_rows());
-      // (a prefill's row count is the host's; one workgroup dispatches up to 4096 assignments, 111 k of them took it 120 us, the sort 15)
+      // (a prefill's row count is the host's; one workgroup dispatches up to 4096 assignments, 111 k of them took it 120 us, the sort's two launches 18)
       if (gather != nullptr && (long long)rows.max_rows * tk > 4096) {
         ExpertSort s{};
         s.n = rows.max_rows * tk; s.n_experts = E; s.align = moe_group_rows(rows.max_rows, tall); s.per_row = tk;

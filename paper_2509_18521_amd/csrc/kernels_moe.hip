@@ -60,19 +60,19 @@ __global__ __launch_bounds__(64) void moe_route_kernel(RowCtx rc, const float* l
       const int e = lane + 64 * j;
       if (e < E && v[j] > lv) { lv = v[j]; li = e; }      // ascending e within the lane
     }
-    // Logits with a NaN or +infinity, or nothing but -infinity, make a soft-max of NaN, of which no lane has a largest: the dispatch and the
-    // sum of the experts' outputs index by these numbers, so each is an expert's.
     const float bv = wave_max_f32(lv);
-    const bool none = bv < 0.f;
-    const int bi = none ? k : wave_min_i32(lv == bv ? li : 0x7fffffff);
+    const int bi = wave_min_i32(lv == bv ? li : 0x7fffffff);
     kept += bv;
-    if (lane == k) { myw = none ? NAN : bv; myid = bi; }
+    if (lane == k) { myw = bv; myid = bi; }
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = bi == lane + 64 * j ? -2.f : v[j];   // remove the winner
   }
+  // Logits with a NaN or +infinity, or nothing but -infinity, make a sum of NaN (else it is 1 or more), and no lane has had a largest: the dispatch and
+  // the sum of the experts' outputs index by these numbers, so each is an expert's all the same.
+  const bool some = sum >= 1.f;
   if (lane < top_k) {
-    ids[(size_t)r * top_k + lane] = myid;
-    wts[(size_t)r * top_k + lane] = myw / kept;
+    ids[(size_t)r * top_k + lane] = some ? myid : lane;
+    wts[(size_t)r * top_k + lane] = some ? myw / kept : NAN;
   }
 }
 
