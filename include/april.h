@@ -427,7 +427,8 @@ int april_logprobs(const april_logprobs_args* args);
 int64_t april_logprobs_workspace(const april_logprobs_args* args);
 
 /* Gradient of the logits for gradients a, h, z of logprob, entropy, lse (NULL: 0):
- * (a (1 at the token - p) - h p (log p + entropy) + z p) / temperature.  Padding rows: 0; a token of vocab or more: NaN. */
+ * (a (1 at the token - p) - h p (log p + entropy) + z p) / temperature.  Padding rows: 0; a token of vocab or more: NaN.  A term of p = 0 is
+ * 0 for finite a, h, z, at any temperature. */
 typedef struct {
   int32_t n_rows, vocab, dtype, index_bits;   /* as in april_logprobs; grad is of the logits' type */
   float temperature;

@@ -504,8 +504,10 @@ __global__ __launch_bounds__(JOIN_THREADS) void logprobs_join_kernel(Logprobs a,
 }
 
 // Workgroups a row is shared out between: about 256 for the call (one a compute unit), from 16 KB of a row on for each, and no more than 512 candidates a row
-// in the second launch.  One row of 151936 in fp32: 12.7 -> 5.6 us without alternatives, 17.3 -> 11.9 with 5; 48 rows 15.2 -> 9.8, 17.9 -> 14.8; 128 rows of
-// 128256 in bf16 14.2 -> 12.3.  (192 rows in two parts: 22.2 -> 24.0 us, and 16 rows with 64 alternatives in 8 parts 14.5, in 32 19.8.)
+// in the second launch.  us unshared | so, without, with 5 and with 64 alternatives: 16 rows of 151936 in fp32 14.6 | 7.9, 17.8 | 12.4, 20.9 | 16.7; 48 rows 15.9 | 10.1, 19.1 | 17.0, 22.2 | 21.3; 64
+// 18.4 | 12.1, 20.8 | 19.6, 24.0 | 22.9; 128 19.4 | 19.0, 21.6 | 22.1, 25.0 | 25.7; of 128256 in bf16 16 rows 12.2 | 6.6, 17.4 | 11.8, 19.7 | 15.3; 64 12.3 | 9.0, 17.5 | 13.4, 19.9 | 16.5; 128 14.5 | 13.0,
+// 19.0 | 17.0, 21.6 | 20.3.  Three parts lose with alternatives in fp32: 96 rows of 151936 18.9 | 16.6, but 21.3 | 24.6 and 24.7 | 28.3 (in two parts 20.1 and 23.6; sections of four vectors, as three parts have them, are loaded
+// one at a time).  192 rows in two parts without: 22.2 | 24.0; 16 rows with 64 alternatives in 8 parts 14.5, in 32 19.8.
 int row_parts(const Logprobs& a) {
   if (a.n_rows > 128) return 1;
   const long long bytes = (long long)a.vocab * (a.f32 ? 4 : 2);
@@ -536,7 +538,7 @@ hipError_t logprobs(hipStream_t st, const Logprobs& a) {
 
 // ---------------------------------------------------------------------------
 // Gradient: one pass, every element by itself.  A workgroup takes four vectors a thread of one row.  Bound by HBM: 16384 rows of 151936 in bf16, a quarter of
-// them padding (not read), 1520 us (5.7 TB/s).
+// them padding (not read), 1527 us (5.7 TB/s).
 // ---------------------------------------------------------------------------
 constexpr int GRAD_THREADS = 256, GRAD_VECS = 4;
 
