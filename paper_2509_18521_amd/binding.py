@@ -1075,7 +1075,7 @@ def _combine(packed, position, weights, out):
 
 
 def _expert_combine(packed, source, position, weights, out):
-    if packed.shape[0] != _packed_rows(source, _gpu("packed", packed))[1]:
+    if _two("packed", packed)[0] != _packed_rows(source, _gpu("packed", packed))[1]:
         _refuse("packed: %d rows wanted, not %d", source.shape[0], packed.shape[0])
     return _combine(packed, position, weights, out)
 

@@ -162,3 +162,14 @@ def test_forward_mode_derivatives_are_refused_and_not_silently_zero():
             ap.april_logprobs(c, t)
         with pytest.raises(ap.AprilError, match="not on a GPU"):
             ap.april_logprobs(fw.unpack_dual(x).primal, t)
+
+
+def test_tensors_of_other_dimensions_are_refused():
+    import torch
+    t, made = torch.zeros(3, dtype=torch.int64), ap.Logprobs(None, None, None, None, None, torch.zeros((3, 2)))
+    rows = ap.ExpertRows(torch.zeros(3, dtype=torch.int32), torch.zeros(6, dtype=torch.int32), torch.zeros((3, 2), dtype=torch.int32))
+    for x in (torch.zeros(()), torch.zeros(3), torch.zeros((2, 3, 8))):
+        for call in (lambda: ap.april_logprobs(x, t), lambda: ap.april_logprobs_grad(x, t, made), lambda: ap.april_embed(x, t), lambda: ap.april_embed_grad(x, t, 5),
+                     lambda: ap.april_expert_sort(x, 4), lambda: ap.april_expert_gather(x, rows), lambda: ap.april_expert_combine(x, rows), lambda: ap.april_expert_combine_grad(x, x, rows)):
+            with pytest.raises(ap.AprilError, match="two dimensions wanted"):
+                call()
